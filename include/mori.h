@@ -83,8 +83,10 @@ extern "C" {
 #define MORI_DEV_BAD_BLOCK 0x400u     /* eviction order: type label > 2 or last access >= 2^62 */
 #define MORI_DEV_BAD_STATUS 0x800u    /* incremental policy: status value > 2 */
 #define MORI_DEV_STALL 0x1000u        /* reserved (no kernel waits for another workgroup) */
+#define MORI_DEV_BAD_TOKENS 0x2000u   /* tokens: offsets, a length or a program out of their bounds */
+#define MORI_DEV_NOT_RESIDENT 0x4000u /* tokens: a block they need has no page (MORI_NO_PAGE) */
 /* classes: program data = 0x00F and 0x800, pool state = 0x0F0, capacity = 0x100, swap = 0x200,
-   blocks = 0x400 */
+   blocks = 0x400, tokens = 0x6000 (and PAGE_RANGE) */
 
 /* ---- tiers, table sentinel, flags, copy modes -------------------------- */
 #define MORI_TIER_GPU 0u
@@ -381,6 +383,123 @@ int mori_evict_order(const mori_blocks* blocks, uint32_t tier, uint64_t need_byt
 #define MORI_EVICT_NOALLOC_MAX_BLOCKS 524288u /* 2^19 */
 int mori_evict_order_noalloc(const mori_blocks* blocks, uint32_t tier, uint64_t need_bytes, uint32_t* order,
                              uint64_t* prefix, uint32_t* result, void* stream);
+
+/* ---- tokens: writing and reading the pool's pages for a model ------------ */
+/* The two calls a model makes in every layer, on the pages of the GPU-resident
+ * programs: mori_kv_append writes new tokens' keys and values into the pool,
+ * mori_kv_attend lets their queries attend to everything the program holds.
+ * Both read the same block tables that mori_rank_partition rewrites, in stream
+ * order; neither needs a context, allocates or waits.
+ *
+ * A pool row (row_bytes, one token in one plane) is
+ *   planes 2   plane 0: keys [kv_heads][head_dim], plane 1: values, the same
+ *   planes 1   a compressed latent [head_dim] shared by all query heads: the
+ *              latent part, which is key and value, then the rotated key part
+ * of 16-bit floats.  Layer l has planes l * planes ... l * planes + planes - 1.
+ * Token j of a program is row j % block_tokens of its block j / block_tokens. */
+#define MORI_DT_F16 0u
+#define MORI_DT_BF16 1u
+
+/* A batch: new tokens of some programs, packed one program after the other.
+ * Sequence b is tokens seq_off[b] .. seq_off[b+1]-1 of the batch, the last
+ * n_b of the kv_len[b] tokens that its program holds after the append; token i
+ * of them is at position kv_len[b] - n_b + i of the program.  A token whose
+ * position is negative is padding (kv_len[b] < n_b): nothing is stored for it
+ * and it attends to nothing.  num_tokens, max_new and max_kv are bounds that
+ * the host vouches for (they size the launch): tokens before seq_off[0] or
+ * past seq_off[num_seqs] are left alone.  A program appears once in a batch.
+ * On the device: n_b above max_new, kv_len above max_kv or above the program's
+ * blocks, a program id out of range: MORI_DEV_BAD_TOKENS, and the sequence counts
+ * as all padding; offsets that decrease or pass num_tokens: the same bit, and
+ * that sequence's tokens are left alone.
+ * A block without a page: MORI_DEV_NOT_RESIDENT; a page id past the pool:
+ * MORI_DEV_PAGE_RANGE; such a token is not stored, and what attends to it is
+ * unspecified.  No call touches memory outside the pool and the arrays given. */
+typedef struct {
+  uint32_t num_seqs;        /* B, 1..MORI_MAX_PROGRAMS */
+  uint32_t num_tokens;      /* T, rows of the token arrays */
+  uint32_t max_new;         /* no n_b is larger; 1 for a decode step */
+  uint32_t max_kv;          /* no kv_len is larger; < 2^31 */
+  const uint32_t* seq_off;  /* device [B+1] */
+  const uint32_t* kv_len;   /* device [B] */
+  const uint32_t* program;  /* device [B], or NULL: sequence b is program b */
+  uint32_t num_programs;    /* P */
+  uint32_t tbl_len;         /* entries allocated in tbl */
+  const uint32_t* tbl_off;  /* device [P+1], as in mori_programs */
+  const uint32_t* tbl;      /* device [tbl_len] */
+} mori_tokens;
+
+/* A [tokens][heads][elements] array of 16-bit floats on the device: element e
+ * of head h of token t is at data + 2 * (t * token_stride + h * head_stride + e).
+ * data is 16-B aligned and both strides are multiples of 8 elements. */
+typedef struct {
+  void* data;
+  uint64_t token_stride, head_stride; /* in elements */
+} mori_rows;
+
+#define MORI_ROPE_HALF 0u  /* element i turns with i + rot_dim / 2 */
+#define MORI_ROPE_PAIRS 1u /* element 2i turns with 2i + 1 */
+
+/* What mori_kv_append stores.  The rotation by position p of the pair i:
+ * (a, b) -> (a c - b s, b c + a s) with c = rope[p][i], s = rope[p][rot_dim/2 + i],
+ * computed in 32 bits and rounded once.
+ *   planes 2   k and v [T][kv_heads][head_dim]; the first rot_dim elements of
+ *              every key head are rotated, the rest and the values are copied.
+ *   planes 1   k [T][1][head_dim - rot_dim], the latent part, copied; v
+ *              [T][1][rot_dim], the key part, rotated and stored behind it.
+ *   q          optional (NULL data): the tokens' queries, [T][q_heads][head_dim]
+ *              with planes 2, rotated like the keys; [T][q_heads][rot_dim] with
+ *              planes 1, rotated whole.  Written to q_out (which may be q
+ *              itself, with its strides); padding tokens get zeros. */
+typedef struct {
+  uint32_t dtype;      /* MORI_DT_* */
+  uint32_t kv_heads;   /* 1 with planes 1 */
+  uint32_t head_dim;   /* multiple of 16, <= 4096; kv_heads * head_dim * 2 == row_bytes */
+  uint32_t q_heads;    /* <= 1024; read only with q */
+  uint32_t rot_dim;    /* multiple of 16, <= head_dim (planes 1: 16..head_dim-16); 0: no rotation */
+  uint32_t rope_style; /* MORI_ROPE_* */
+  uint32_t rope_len;   /* positions in rope; a token past them: MORI_DEV_BAD_TOKENS, not stored */
+  const float* rope;   /* device [rope_len][rot_dim], 16-B aligned: cosines, then sines */
+  mori_rows k, v, q, q_out;
+} mori_append;
+
+/* Writes the batch's keys and values of one layer into the pool.  *error
+ * (device, may be NULL) collects MORI_DEV_* bits by OR; the caller clears it.
+ * EINVAL: null pointers, alignment, sizes that do not fit each other. */
+int mori_kv_append(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, const mori_append* append,
+                   uint32_t* error, void* stream);
+
+/* What attends: out[t][h] = sum over the program's tokens j up to and with t's
+ * own position of softmax_j(scale * q[t][h] . key_j) value_j, with head h
+ * reading key head h / (q_heads / kv_heads); an empty sum is 0.
+ *   planes 2   head_dim 64 or 128, value_dim the same
+ *   planes 1   head_dim 576, value_dim 512 (the row's first 512 elements)
+ * Scores, maxima, sums and outputs are kept in 32 bits; the weights are rounded
+ * to dtype for the matrix product with the values. */
+typedef struct {
+  uint32_t dtype;     /* MORI_DT_* */
+  uint32_t q_heads;   /* multiple of kv_heads, <= 1024 */
+  uint32_t kv_heads;  /* kv_heads * head_dim * 2 == row_bytes */
+  uint32_t head_dim, value_dim;
+  float scale;        /* finite */
+  mori_rows q;        /* [T][q_heads][head_dim] */
+  mori_rows out;      /* [T][q_heads][value_dim]; overlaps no input */
+  float* lse;         /* device [T][q_heads] or NULL: log of the sum of exp(scores), -inf for an empty sum */
+} mori_attend;
+
+/* Device workspace mori_kv_attend needs for this batch (0: none; it grows with
+ * num_tokens, num_seqs and the heads, and is bounded by max_new and max_kv). */
+int mori_kv_attend_workspace(const mori_pool* pool, const mori_tokens* tokens, const mori_attend* attend,
+                             uint64_t* bytes);
+
+/* Attention of the batch's tokens in one layer, as above.  workspace: 256-B
+ * aligned device memory of at least mori_kv_attend_workspace bytes, used only
+ * while the call's work runs; its contents before do not matter.  The result is
+ * the same for every call with the same arguments, bit for bit.  error as in
+ * mori_kv_append.  EINVAL: null pointers, alignment, sizes or head dimensions
+ * other than the above, a short workspace. */
+int mori_kv_attend(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, const mori_attend* attend,
+                   void* workspace, uint64_t workspace_bytes, uint32_t* error, void* stream);
 
 /* ---- kernel timing ------------------------------------------------------ */
 /* With profiling on, every gather/scatter kernel launch of the swaps is

@@ -1,0 +1,217 @@
+"""What a model does with the paged KV pool, for torch tensors on the device:
+``kv_append`` writes new tokens' keys and values into the programs' pages (and
+rotates them and their queries by position), ``kv_attend`` lets the queries
+attend to everything the programs hold.  ``TokenBatch`` says which tokens of
+which programs; it is made once a step and used in every layer.
+
+Like ``mori``, this only marshals arguments: the work runs in libmori's kernels,
+on the current stream unless one is given, and nothing here waits for the device
+(but ``TokenBatch.check``).  Arguments that do not fit raise ``MoriError`` before
+anything is enqueued.
+"""
+from __future__ import annotations
+
+import contextlib
+
+import numpy as np
+import torch
+
+from . import mori as M
+from .tiering import MoriError, PoolGeometry, _stream, check
+
+DTYPES = {torch.float16: M.MORI_DT_F16, torch.bfloat16: M.MORI_DT_BF16}
+STYLES = {"half": M.MORI_ROPE_HALF, "pairs": M.MORI_ROPE_PAIRS}
+LATENT_DIM, LATENT_ROPE = 512, 64  # the latent rows kv_attend reads
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise MoriError(what, M.MORI_EINVAL)
+
+
+def rope_table(positions: int, rot_dim: int, theta: float = 10000.0, device="cuda") -> torch.Tensor:
+    """float32 [positions][rot_dim]: the cosines of every pair's angle, then the
+    sines; pair i turns by position * theta^(-2i / rot_dim).  Angles are taken in
+    64 bits, so long contexts keep their precision."""
+    angle = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * \
+        theta ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64, device=device) / rot_dim)
+    return torch.cat([angle.cos(), angle.sin()], 1).float()
+
+
+def _on(stream):
+    """Where this module's own allocations belong: the stream that uses them, so
+    that the allocator hands their memory on in that stream's order."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+class TokenBatch:
+    """New tokens of some programs, packed one program after the other.
+
+    tbl_off, tbl: the pool's block tables (int32, as ``TierPool`` keeps them).
+    seq_off int32 [B+1]: sequence b is tokens seq_off[b] .. seq_off[b+1]-1, the
+    last of the kv_len[b] (int32 [B]) tokens that program[b] (int32 [B]; None:
+    program b) holds once they are appended; tokens before position 0 are padding.
+    num_tokens, max_new, max_kv: the batch's tokens and the most that any sequence
+    brings and holds, as the host knows them (the device checks them).  The
+    tensors may be rewritten between steps, also under a captured graph, as long
+    as these bounds hold.
+
+    ``error`` collects the device's MORI_DEV_* bits; ``check`` waits, reads and
+    clears it."""
+
+    def __init__(self, geom, tbl_off: torch.Tensor, tbl: torch.Tensor, seq_off: torch.Tensor, kv_len: torch.Tensor,
+                 program: torch.Tensor | None = None, *, num_tokens: int, max_new: int, max_kv: int):
+        self.geom = PoolGeometry(geom.layers, geom.planes, geom.block_tokens, geom.row_bytes, geom.num_blocks)
+        self.num_seqs, self.num_tokens = int(kv_len.numel()), int(num_tokens)
+        for name, x, n in (("tbl_off", tbl_off, None), ("tbl", tbl, None), ("seq_off", seq_off, self.num_seqs + 1),
+                           ("kv_len", kv_len, self.num_seqs), ("program", program, self.num_seqs)):
+            if x is None:
+                continue
+            _need(x.dtype == torch.int32 and x.is_contiguous() and x.dim() == 1 and x.device.type == "cuda",
+                  f"TokenBatch: {name} is a contiguous int32 vector on the device")
+            _need(n is None or x.numel() == n, f"TokenBatch: {name} has {x.numel()} entries, not {n}")
+        _need(num_tokens >= 0 and max_new >= 0 and 0 < max_kv < 1 << 31, "TokenBatch: bounds out of range")
+        _need(tbl_off.numel() >= 2, "TokenBatch: tbl_off is empty")
+        self.device = kv_len.device
+        self.error = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._keep = (tbl_off, tbl, seq_off, kv_len, program)
+        self.desc = M.mori_tokens(self.num_seqs, self.num_tokens, int(max_new), int(max_kv), seq_off.data_ptr(),
+                                  kv_len.data_ptr(), program.data_ptr() if program is not None else None,
+                                  tbl_off.numel() - 1, tbl.numel(), tbl_off.data_ptr(), tbl.data_ptr())
+
+    @classmethod
+    def of(cls, tier_pool, programs, new_tokens, kv_len) -> "TokenBatch":
+        """A batch of a ``TierPool``'s programs from host numbers: new_tokens[i] new
+        tokens of programs[i], which then holds kv_len[i]."""
+        n, length = np.asarray(new_tokens, np.int64), np.asarray(kv_len, np.int64)
+        prog = np.asarray(programs, np.int64)
+        _need(n.ndim == 1 and n.shape == length.shape == prog.shape, "TokenBatch: one number per sequence")
+        _need(bool((n >= 0).all() and (length >= 0).all() and (prog >= 0).all() and (prog < tier_pool.P).all()),
+              "TokenBatch: numbers out of range")
+        _need(bool((length <= tier_pool.nblk[prog] * tier_pool.geom.block_tokens).all()),
+              "TokenBatch: more tokens than the program's blocks hold")
+        dev = lambda a: torch.from_numpy(a.astype(np.int32)).to(tier_pool.device)
+        off = np.concatenate([[0], np.cumsum(n)])
+        return cls(tier_pool.geom, tier_pool.tbl_off, tier_pool.tbl, dev(off), dev(length), dev(prog),
+                   num_tokens=int(off[-1]), max_new=int(n.max(initial=0)), max_kv=max(1, int(length.max(initial=1))))
+
+    def check(self) -> None:
+        """Raises MoriError if the device found fault with the batch since the last check."""
+        bits = int(self.error.item())
+        if bits:
+            self.error.zero_()
+            raise MoriError("token batch", M.MORI_EDEVICE, bits)
+
+
+def _pool(pool: torch.Tensor, geom) -> M.mori_pool:
+    _need(pool.is_contiguous() and pool.device.type == "cuda" and
+          pool.numel() * pool.element_size() == geom.layers * geom.planes * geom.num_blocks * geom.block_tokens *
+          geom.row_bytes, "pool does not have its geometry's bytes")
+    return M.mori_pool(geom.layers, geom.planes, geom.block_tokens, geom.row_bytes, geom.num_blocks, pool.data_ptr())
+
+
+def _rows(name: str, x: torch.Tensor, batch: TokenBatch, dtype: torch.dtype, heads: int | None = None,
+          dim: int | None = None, written: bool = False) -> M.mori_rows:
+    """A [tokens][heads][elements] view with its strides; elements are adjacent.
+    Views to write have a place for every element (no broadcast)."""
+    _need(x.dim() == 3 and x.shape[0] == batch.num_tokens and x.dtype == dtype and x.device == batch.device,
+          f"{name}: [{batch.num_tokens}][heads][elements] of {dtype} on {batch.device}")
+    _need((heads is None or x.shape[1] == heads) and (dim is None or x.shape[2] == dim),
+          f"{name}: shape {tuple(x.shape)}, not [tokens][{heads}][{dim}]")
+    _need(x.shape[2] == 0 or x.stride(2) == 1, f"{name}: elements are not adjacent")
+    # a stride over one token or one head is never used; views may carry any value there
+    token = x.stride(0) if x.shape[0] > 1 else 0
+    head = x.stride(1) if x.shape[1] > 1 else 0
+    _need(token >= 0 and head >= 0, f"{name}: strides")
+    _need(not written or ((token > 0 or x.shape[0] < 2) and (head > 0 or x.shape[1] < 2)), f"{name}: broadcast")
+    return M.mori_rows(x.data_ptr() or None, token, head)
+
+
+def kv_append(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, k: torch.Tensor, v: torch.Tensor, *,
+              q: torch.Tensor | None = None, q_out: torch.Tensor | None = None, rope: torch.Tensor | None = None,
+              style: str = "half", stream=None):
+    """Stores the batch's keys and values in one layer of the pool.
+
+    planes 2: k, v [T][kv_heads][head_dim]; the first rope.shape[1] elements of
+    every key head turn with the token's position.  planes 1: k [T][1][latent]
+    copied, v [T][1][rot] rotated behind it.  q, if given, is rotated the same way
+    ([T][q_heads][head_dim], or [T][q_heads][rot] with planes 1) into q_out, which
+    may be q; returns q_out (allocated if not given)."""
+    _need(k.dtype in DTYPES, "kv_append: float16 or bfloat16")
+    _need(style in STYLES, f"kv_append: style {style!r}")
+    _need(k.dim() == 3 and v.dim() == 3, "kv_append: k and v are [tokens][heads][elements]")
+    latent = geom.planes == 1
+    dim = k.shape[2] + v.shape[2] if latent else k.shape[2]
+    rot = 0
+    if rope is not None:
+        _need(rope.dtype == torch.float32 and rope.dim() == 2 and rope.is_contiguous() and rope.device == batch.device,
+              "kv_append: rope is a contiguous float32 [positions][rot_dim] on the batch's device")
+        rot = int(rope.shape[1])
+    kw = dict(batch=batch, dtype=k.dtype)
+    a = M.mori_append(DTYPES[k.dtype], k.shape[1], dim, 0, rot, STYLES[style], 0 if rope is None else rope.shape[0],
+                      None if rope is None else rope.data_ptr())
+    a.k = _rows("k", k, heads=1 if latent else None, **kw)
+    a.v = _rows("v", v, heads=k.shape[1], dim=rot if latent else dim, **kw)
+    if q is not None:
+        a.q = _rows("q", q, dim=rot if latent else dim, **kw)
+        if q_out is None:
+            with _on(stream):
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        a.q_out = _rows("q_out", q_out, heads=q.shape[1], dim=q.shape[2], written=True, **kw)
+        a.q_heads = q.shape[1]
+    check(M.mori_kv_append(_pool(pool, geom), int(layer), batch.desc, a, batch.error.data_ptr(), _stream(stream)),
+          "mori_kv_append")
+    return q_out
+
+
+def _attend_desc(geom, batch: TokenBatch, q: torch.Tensor, scale: float | None):
+    _need(q.dtype in DTYPES and q.dim() == 3, "kv_attend: q is [tokens][heads][elements] of float16 or bfloat16")
+    dim = int(q.shape[2])
+    _need(dim > 0 and geom.row_bytes % (2 * dim) == 0, f"kv_attend: rows of {geom.row_bytes} B hold no heads of {dim}")
+    value = dim - LATENT_ROPE if geom.planes == 1 else dim
+    return M.mori_attend(DTYPES[q.dtype], q.shape[1], geom.row_bytes // (2 * dim), dim, value,
+                         dim ** -0.5 if scale is None else float(scale)), value
+
+
+def _empty_pool(geom) -> M.mori_pool:
+    """The pool as a description only (the workspace call reads no memory)."""
+    return M.mori_pool(geom.layers, geom.planes, geom.block_tokens, geom.row_bytes, geom.num_blocks, 256)
+
+
+def kv_attend_workspace(geom, batch: TokenBatch, q: torch.Tensor) -> torch.Tensor:
+    """Device workspace for kv_attend of this batch, in every layer; calls that may
+    overlap (on other streams) need one each."""
+    a, _ = _attend_desc(geom, batch, q, None)
+    rc, n = M.mori_kv_attend_workspace(_empty_pool(geom), batch.desc, a)
+    check(rc, "mori_kv_attend_workspace")
+    return torch.empty(n, dtype=torch.uint8, device=batch.device)
+
+
+def kv_attend(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, q: torch.Tensor, *, scale: float | None = None,
+              out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+              workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Causal attention of the batch's tokens over their programs' pages in one
+    layer.  q [T][q_heads][head_dim] (latent pools: [T][q_heads][576], in the latent
+    space); scale: head_dim ** -0.5 unless given.  Returns out [T][q_heads]
+    [head_dim] (latent pools: 512), allocated if not given; lse, a float32
+    [T][q_heads] tensor, takes the logarithms of the rows' sums.  The workspace is
+    allocated here unless given."""
+    a, value = _attend_desc(geom, batch, q, scale)
+    a.q = _rows("q", q, batch, q.dtype)
+    if out is None:
+        with _on(stream):
+            out = torch.empty(q.shape[0], q.shape[1], value, dtype=q.dtype, device=q.device)
+    a.out = _rows("out", out, batch, q.dtype, q.shape[1], value, True)
+    if lse is not None:
+        _need(lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2] and
+              lse.device == batch.device, "kv_attend: lse is a contiguous float32 [tokens][heads]")
+        a.lse = lse.data_ptr()
+    desc = _pool(pool, geom)
+    if workspace is None:
+        rc, n = M.mori_kv_attend_workspace(desc, batch.desc, a)
+        check(rc, "mori_kv_attend_workspace")
+        with _on(stream):
+            workspace = torch.empty(n, dtype=torch.uint8, device=batch.device)
+    check(M.mori_kv_attend(desc, int(layer), batch.desc, a, workspace.data_ptr(), workspace.numel(),
+                           batch.error.data_ptr(), _stream(stream)), "mori_kv_attend")
+    return out

@@ -205,14 +205,10 @@ extern "C" int mori_create(const mori_pool* pool, uint32_t max_programs, uint64_
   if (!pool || !out) return MORI_EINVAL;
   *out = nullptr;
   if (flags & ~MORI_CREATE_COPY_STREAMS) return MORI_EINVAL;
-  if (!pool->base || (reinterpret_cast<uintptr_t>(pool->base) & 255u)) return MORI_EINVAL;
-  if (!pool->layers || !pool->planes || !pool->block_tokens || !pool->row_bytes || (pool->row_bytes & 15u))
-    return MORI_EINVAL;
-  if (!pool->num_blocks || pool->num_blocks == MORI_NO_PAGE) return MORI_EINVAL;
+  if (!pool_valid(*pool)) return MORI_EINVAL;
   if (max_programs == 0 || max_programs > MORI_MAX_PROGRAMS) return MORI_EINVAL;
   const uint64_t LC = (uint64_t)pool->layers * pool->planes;
   const uint64_t run = (uint64_t)pool->block_tokens * pool->row_bytes;
-  if (LC > 0xFFFFu || run > (1ull << 31) || LC * run >= (1ull << 32)) return MORI_EINVAL;
   if (staging_bytes == 0) staging_bytes = kDefaultStaging;
   staging_bytes = staging_bytes / (2 * run) * (2 * run);  // two halves of whole runs
   if (staging_bytes == 0) return MORI_EINVAL;

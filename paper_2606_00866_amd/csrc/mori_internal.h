@@ -145,4 +145,14 @@ hipError_t launch_evict(uint32_t N, const uint8_t* type, const uint64_t* last_ac
                         uint64_t unit_bytes, uint32_t tier, uint64_t need, void* workspace, uint32_t* order,
                         uint64_t* prefix, uint32_t* result, hipStream_t s);
 
+// Geometry a pool may have (the calls that take one check it before anything else).
+inline bool pool_valid(const mori_pool& p) {
+  if (!p.base || (reinterpret_cast<uintptr_t>(p.base) & 255u)) return false;
+  if (!p.layers || !p.planes || !p.block_tokens || !p.row_bytes || (p.row_bytes & 15u)) return false;
+  if (!p.num_blocks || p.num_blocks == MORI_NO_PAGE) return false;
+  const uint64_t LC = (uint64_t)p.layers * p.planes;
+  const uint64_t run = (uint64_t)p.block_tokens * p.row_bytes;
+  return LC <= 0xFFFFu && run <= (1ull << 31) && LC * run < (1ull << 32);
+}
+
 }  // namespace mori

@@ -18,6 +18,7 @@ MORI_DEV_BAD_WINDOW, MORI_DEV_BAD_IDLENESS, MORI_DEV_BAD_TIER, MORI_DEV_BAD_TBL_
 MORI_DEV_PAGE_RANGE, MORI_DEV_PAGE_DUP, MORI_DEV_PAGE_LEAK, MORI_DEV_NONRES_PAGE = 0x10, 0x20, 0x40, 0x80
 MORI_DEV_NOSPC, MORI_DEV_HOST_ADDR, MORI_DEV_BAD_BLOCK, MORI_DEV_BAD_STATUS = 0x100, 0x200, 0x400, 0x800
 MORI_DEV_STALL = 0x1000
+MORI_DEV_BAD_TOKENS, MORI_DEV_NOT_RESIDENT = 0x2000, 0x4000
 MORI_TYPE_BUSY, MORI_TYPE_IDLE, MORI_TYPE_INACTIVE = 0, 1, 2
 MORI_TIER_GPU, MORI_TIER_CPU, MORI_TIER_WAIT, MORI_TIER_SSD = 0, 1, 2, 3
 MORI_NO_PAGE = 0xFFFFFFFF
@@ -30,13 +31,16 @@ MORI_CREATE_COPY_STREAMS = 1
 MORI_MAX_PROGRAMS, MORI_MAX_WINDOW, MORI_MAX_RANGES, MORI_MAX_REPLICAS = 4096, 64, 64, 1024
 MORI_ADMIT_BEST_FIT = 1
 MORI_EVICT_NOALLOC_MAX_BLOCKS = 1 << 19
+MORI_DT_F16, MORI_DT_BF16 = 0, 1
+MORI_ROPE_HALF, MORI_ROPE_PAIRS = 0, 1
 MORI_Q_LAST_HIP_ERROR, MORI_Q_DEVICE_ERROR, MORI_Q_LAST_MODE = 1, 2, 3
 MORI_Q_PLAN_EVENT, MORI_Q_OUT_EVENT, MORI_Q_IN_EVENT = 4, 5, 6
 
 EXPORTS = ("mori_create", "mori_destroy", "mori_register", "mori_host_alloc", "mori_host_free",
            "mori_rank_partition", "mori_plan_wait", "mori_kv_swap_out", "mori_kv_swap_in", "mori_query",
            "mori_strerror", "mori_profile", "mori_profile_read", "mori_evict_workspace", "mori_evict_order",
-           "mori_replica_admit", "mori_evict_order_noalloc")
+           "mori_replica_admit", "mori_evict_order_noalloc", "mori_kv_append", "mori_kv_attend_workspace",
+           "mori_kv_attend")
 
 
 class mori_pool(C.Structure):
@@ -58,6 +62,27 @@ class mori_budget(C.Structure):
 class mori_blocks(C.Structure):
     _fields_ = [("num_blocks", C.c_uint32), ("type", C.c_void_p), ("last_access", C.c_void_p),
                 ("size", C.c_void_p), ("unit_bytes", C.c_uint64)]
+
+
+class mori_tokens(C.Structure):
+    _fields_ = [("num_seqs", C.c_uint32), ("num_tokens", C.c_uint32), ("max_new", C.c_uint32), ("max_kv", C.c_uint32),
+                ("seq_off", C.c_void_p), ("kv_len", C.c_void_p), ("program", C.c_void_p), ("num_programs", C.c_uint32),
+                ("tbl_len", C.c_uint32), ("tbl_off", C.c_void_p), ("tbl", C.c_void_p)]
+
+
+class mori_rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_uint64), ("head_stride", C.c_uint64)]
+
+
+class mori_append(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("dtype", "kv_heads", "head_dim", "q_heads", "rot_dim", "rope_style",
+                                          "rope_len")] + [
+        ("rope", C.c_void_p), ("k", mori_rows), ("v", mori_rows), ("q", mori_rows), ("q_out", mori_rows)]
+
+
+class mori_attend(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("dtype", "q_heads", "kv_heads", "head_dim", "value_dim")] + [
+        ("scale", C.c_float), ("q", mori_rows), ("out", mori_rows), ("lse", C.c_void_p)]
 
 
 class mori_plan(C.Structure):
@@ -100,6 +125,10 @@ def lib():
         L.mori_evict_order.argtypes = [C.POINTER(mori_blocks), U32, U64, V, U64, V, V, V, V]
         L.mori_replica_admit.argtypes = [U32, V, V, V, U32, V, U32, V, V]
         L.mori_evict_order_noalloc.argtypes = [C.POINTER(mori_blocks), U32, U64, V, V, V, V]
+        PP, PT = C.POINTER(mori_pool), C.POINTER(mori_tokens)
+        L.mori_kv_append.argtypes = [PP, U32, PT, C.POINTER(mori_append), V, V]
+        L.mori_kv_attend_workspace.argtypes = [PP, PT, C.POINTER(mori_attend), C.POINTER(U64)]
+        L.mori_kv_attend.argtypes = [PP, U32, PT, C.POINTER(mori_attend), V, U64, V, V]
         L.mori_strerror.restype = C.c_char_p
         for name in EXPORTS:
             if name != "mori_strerror":
@@ -189,6 +218,24 @@ def mori_evict_order_noalloc(blocks: mori_blocks, tier: int, need_bytes: int, or
                              result: int, stream: int = 0) -> int:
     """mori_evict_order without a workspace (the library's device array is used)."""
     return lib().mori_evict_order_noalloc(C.byref(blocks), tier, need_bytes, order, prefix or None, result, stream)
+
+
+def mori_kv_append(pool: mori_pool, layer: int, tokens: mori_tokens, append: mori_append, error: int = 0,
+                   stream: int = 0) -> int:
+    """error: device address of the word that collects MORI_DEV_* bits, or 0."""
+    return lib().mori_kv_append(C.byref(pool), layer, C.byref(tokens), C.byref(append), error or None, stream)
+
+
+def mori_kv_attend_workspace(pool: mori_pool, tokens: mori_tokens, attend: mori_attend):
+    b = C.c_uint64()
+    rc = lib().mori_kv_attend_workspace(C.byref(pool), C.byref(tokens), C.byref(attend), C.byref(b))
+    return rc, b.value
+
+
+def mori_kv_attend(pool: mori_pool, layer: int, tokens: mori_tokens, attend: mori_attend, workspace: int,
+                   workspace_bytes: int, error: int = 0, stream: int = 0) -> int:
+    return lib().mori_kv_attend(C.byref(pool), layer, C.byref(tokens), C.byref(attend), workspace or None,
+                                workspace_bytes, error or None, stream)
 
 
 def mori_replica_admit(bytes_, idleness, status, room, flags: int = 0):
