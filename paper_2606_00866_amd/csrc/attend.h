@@ -1,0 +1,248 @@
+// What the attention kernels share: their arguments, the division of a batch into
+// work items, and the running softmax's conventions.
+//
+// Rows.  The query heads that share a key head are stacked: row r of a sequence
+// and a key head is token r / group, query head r % group of the group.  So a
+// decode step's group fills a matrix tile where single heads would leave it
+// empty, and a key is fetched once for all of them.
+//
+// Items.  A sequence's rows are cut into tiles of a kernel's height; each tile's
+// keys into runs of the same whole number c of units, where c follows from the
+// batch on the device:
+//     c = max(least, ceil(sum over tiles of their units / slots)),
+// so that a batch gives about `slots` items however its lengths are spread, and
+// at most slots + tiles.  No scheduling pass precedes the kernel: every
+// wavefront finds its item from the lengths by a scan over the sequences.
+// Tiles of one run write their rows; the others leave partial sums (unnormalised
+// rows, their maxima and sums) that a second kernel joins in a fixed order.
+//
+// Softmax.  Scores are kept in units of log2(e) / scale: weights are
+// exp2(score * c - top).  `top` is at or below the running maximum and follows
+// it only when that has risen by more than RISE, so weights stay at most 2^RISE
+// and most steps leave the accumulators alone.
+#pragma once
+#include "float16.h"
+#include "tokens.h"
+
+namespace mori {
+
+constexpr float NO_TOP = -3.0e38f;  // below any score; finite, so that masked scores (-inf) give weight 0
+constexpr float RISE = 8.0f;
+
+struct AttendArgs {
+  Batch b;
+  Rows q, out;
+  uint32_t heads, kv_heads, group;
+  FastDiv by_group, by_kv;
+  float c;             // |scale| * log2(e) (1 with scale 0)
+  uint32_t q_flip;     // XORed into query pairs: the scale's sign
+  uint32_t q_keep;     // ANDed into query pairs: 0 with scale 0
+  float* lse;
+  uint32_t tile_rows;  // rows of a tile
+  uint32_t unit;       // keys of a unit
+  uint32_t slots, least;
+  uint32_t splits;     // 0: every tile is one run
+  uint32_t items;      // bound on the number of items (grid and workspace)
+  float* part;         // [items * kv_heads][tile_rows][value]
+  float2* part_ml;     // [items * kv_heads][tile_rows]: top, sum
+};
+
+// One sequence as the scan sees it (bounds of its tokens and lengths only).
+struct Share {
+  uint32_t n, units, tiles;
+  bool bad;  // its token range does not fit: it has no rows
+};
+__device__ inline Share share_of(const AttendArgs& a, uint32_t b) {
+  Share s{0, 1, 0, false};
+  const uint32_t lo = a.b.seq_off[b], hi = a.b.seq_off[b + 1], len = a.b.kv_len[b];
+  s.bad = lo > hi || hi > a.b.T;
+  if (s.bad) return s;
+  s.n = hi - lo;
+  s.tiles = (s.n * a.group + a.tile_rows - 1) / a.tile_rows;
+  if (len && len <= a.b.max_kv) s.units = (len + a.unit - 1) / a.unit;
+  return s;
+}
+
+struct Item {
+  uint32_t b;          // sequence
+  uint32_t first;      // index of its first item
+  uint32_t per_tile;   // runs of each of its tiles
+  uint32_t run_units;
+  bool found;
+  bool bad;            // a sequence of this lane has no usable token range
+};
+
+// The sequence that `want(first item, number of items, b)` picks, the same for
+// the whole wavefront (all of whose lanes are active).
+template <typename F>
+__device__ inline Item find_item(const AttendArgs& a, uint32_t lane, F want) {
+  const uint32_t k = (a.b.B + 63) / 64, b0 = lane * k;
+  Share own{0, 1, 0, false};  // the lane's only sequence, for batches of up to 64
+  if (b0 < a.b.B) own = share_of(a, b0);
+  Item it{};
+  it.run_units = 0x7FFFFFFFu;
+  if (a.splits) {
+    uint64_t total = (uint64_t)own.tiles * own.units;
+    for (uint32_t i = 1; i < k && b0 + i < a.b.B; ++i) {
+      const Share s = share_of(a, b0 + i);
+      total += (uint64_t)s.tiles * s.units;
+    }
+    total = wave::sum(total);
+    it.run_units = (uint32_t)max((uint64_t)a.least, (total + a.slots - 1) / a.slots);
+  }
+  const auto count = [&](const Share& s) { return s.tiles * ((s.units + it.run_units - 1) / it.run_units); };
+  uint32_t mine = count(own);
+  for (uint32_t i = 1; i < k && b0 + i < a.b.B; ++i) mine += count(share_of(a, b0 + i));
+  uint32_t first = wave::incl_add(mine) - mine;
+  uint32_t hit = 0xFFFFFFFFu, hit_first = 0, hit_per = 1;
+  Share s = own;
+  for (uint32_t i = 0; i < k && b0 + i < a.b.B; ++i) {
+    if (i) s = share_of(a, b0 + i);
+    const uint32_t n = count(s);
+    it.bad |= s.bad;
+    if (want(first, n, b0 + i)) {
+      hit = b0 + i;
+      hit_first = first;
+      hit_per = (s.units + it.run_units - 1) / it.run_units;
+    }
+    first += n;
+  }
+  const uint64_t who = __ballot(hit != 0xFFFFFFFFu);
+  it.found = who != 0;
+  if (!it.found) return it;
+  const int l = __ffsll((unsigned long long)who) - 1;
+  it.b = (uint32_t)__builtin_amdgcn_readlane((int)hit, l);
+  it.first = (uint32_t)__builtin_amdgcn_readlane((int)hit_first, l);
+  it.per_tile = (uint32_t)__builtin_amdgcn_readlane((int)hit_per, l);
+  return it;
+}
+
+// One workgroup's work: a run of keys of one tile of rows.
+struct Work {
+  Seq s;
+  uint32_t item, kv;       // index of the item, key head
+  uint32_t row0, rows;     // the tile's rows of the sequence: row0 .. row0 + rows - 1
+  uint32_t lo, hi;         // keys; lo >= hi: none
+  uint32_t open;           // keys below this are allowed to every row of the tile
+  uint32_t per_tile;
+  bool first_run, some;
+};
+
+__device__ inline Work work_of(const AttendArgs& a, uint32_t block, uint32_t lane) {
+  Work w{};
+  w.item = divide(block, a.by_kv);
+  w.kv = block - w.item * a.kv_heads;
+  const uint32_t item = w.item;
+  const Item it = find_item(a, lane, [&](uint32_t first, uint32_t n, uint32_t) { return item - first < n; });
+  w.some = it.found;
+  if (block == 0 && it.bad) report(a.b, MORI_DEV_BAD_TOKENS);
+  if (!w.some) return w;
+  w.s = sequence(a.b, it.b);
+  const uint32_t tiles = (w.s.n * a.group + a.tile_rows - 1) / a.tile_rows;
+  const uint32_t k = w.item - it.first, back = k / it.per_tile, run = k - back * it.per_tile;
+  w.per_tile = it.per_tile;
+  w.first_run = run == 0;
+  // the last tile first: with a causal mask it has the most keys
+  w.row0 = (tiles - 1 - back) * a.tile_rows;
+  w.rows = min(a.tile_rows, w.s.n * a.group - w.row0);
+  // keys of the tile's first and last row: up to and with their own positions
+  const int32_t at0 = w.s.position(divide(w.row0, a.by_group)) + 1;
+  const int32_t at1 = w.s.position(divide(w.row0 + w.rows - 1, a.by_group)) + 1;
+  w.open = (uint32_t)max(at0, 0);
+  const uint64_t lo = (uint64_t)run * it.run_units * a.unit, hi = lo + (uint64_t)it.run_units * a.unit;
+  w.lo = (uint32_t)min(lo, (uint64_t)0x7FFFFFFFu);
+  w.hi = (uint32_t)min(hi, (uint64_t)(uint32_t)max(at1, 0));
+  return w;
+}
+
+// Keys a row of the tile may attend to (0 for rows past the tile's).
+__device__ inline uint32_t row_limit(const AttendArgs& a, const Work& w, uint32_t r) {
+  if (r >= w.rows) return 0;
+  return (uint32_t)max(w.s.position(divide(w.row0 + r, a.by_group)) + 1, 0);
+}
+
+// Token and query head of a row of the tile.
+struct RowAt {
+  uint32_t t, h;
+};
+__device__ inline RowAt row_at(const AttendArgs& a, const Work& w, uint32_t r) {
+  const uint32_t x = w.row0 + r, i = divide(x, a.by_group);
+  return {w.s.t0 + i, w.kv * a.group + (x - i * a.group)};
+}
+
+__device__ inline const uint8_t* q_row(const AttendArgs& a, RowAt p) {
+  return a.q.data + p.t * a.q.token + p.h * a.q.head;
+}
+
+// A query chunk with the scale's sign taken in.
+__device__ inline u32x4 q_signed(const AttendArgs& a, u32x4 v) { return (v & a.q_keep) ^ a.q_flip; }
+
+// Row of the pool (page * block_tokens + row in the page) of a key.  The host
+// has checked that a plane has fewer than 2^32 rows.
+__device__ inline uint32_t pool_row(const Batch& b, uint32_t key, uint32_t entry, uint32_t* err) {
+  const uint32_t block = divide(key, b.by_bt);
+  return checked_page(b, entry, err) * b.bt + (key - block * b.bt);
+}
+__device__ inline uint32_t table_entry(const Batch& b, const Seq& s, uint32_t key) {
+  return b.tbl[s.tbl + divide(key, b.by_bt)];
+}
+
+// Where the logarithm of a row's sum goes; top and sum in the kernels' units.
+__device__ inline void store_lse(const AttendArgs& a, RowAt p, float top, float sum, bool none) {
+  if (a.lse) a.lse[(uint64_t)p.t * a.heads + p.h] = none ? -INFINITY : (top + __log2f(sum)) * 0.69314718055994531f;
+}
+
+// Lanes of the wavefront that hold the same row: l ^ 16, l ^ 32 (and both).
+__device__ inline float max_over_32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(bits<uint32_t>(x), bits<uint32_t>(x), false, false);
+  return fmaxf(bits<float>(r[0]), bits<float>(r[1]));
+}
+__device__ inline float max_over_16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(bits<uint32_t>(x), bits<uint32_t>(x), false, false);
+  return fmaxf(bits<float>(r[0]), bits<float>(r[1]));
+}
+__device__ inline float sum_over_32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(bits<uint32_t>(x), bits<uint32_t>(x), false, false);
+  return bits<float>(r[0]) + bits<float>(r[1]);
+}
+__device__ inline float sum_over_16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(bits<uint32_t>(x), bits<uint32_t>(x), false, false);
+  return bits<float>(r[0]) + bits<float>(r[1]);
+}
+
+__device__ inline f32x4 mfma_16x16x32(BF16, u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(bits<BF16::x8>(a), bits<BF16::x8>(b), c, 0, 0, 0);
+}
+__device__ inline f32x4 mfma_16x16x32(F16, u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(bits<F16::x8>(a), bits<F16::x8>(b), c, 0, 0, 0);
+}
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+__device__ inline f32x16 mfma_32x32x16(BF16, u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(bits<BF16::x8>(a), bits<BF16::x8>(b), c, 0, 0, 0);
+}
+__device__ inline f32x16 mfma_32x32x16(F16, u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(bits<F16::x8>(a), bits<F16::x8>(b), c, 0, 0, 0);
+}
+
+template <typename DT>
+__device__ inline uint32_t pair_of(float lo, float hi) {
+  typename DT::x2 h;
+  h[0] = (typename DT::scalar)lo;
+  h[1] = (typename DT::scalar)hi;
+  return bits<uint32_t>(h);
+}
+
+// Whether a pair of 16-bit values holds an infinity or a NaN.
+__device__ inline bool odd_pair(BF16, uint32_t x) {
+  return (x & 0x7F80u) == 0x7F80u || (x & 0x7F800000u) == 0x7F800000u;
+}
+__device__ inline bool odd_pair(F16, uint32_t x) {
+  return (x & 0x7C00u) == 0x7C00u || (x & 0x7C000000u) == 0x7C000000u;
+}
+
+// Launchers, by kernel.  `tile` fills a.tile_rows and a.unit.
+void launch_attend_step(const AttendArgs& a, bool f16, uint32_t dim, uint32_t blocks, hipStream_t s);
+void launch_attend_tile(const AttendArgs& a, bool f16, uint32_t dim, hipStream_t s);
+void launch_attend_join(const AttendArgs& a, bool f16, uint32_t value, hipStream_t s);
+
+}  // namespace mori

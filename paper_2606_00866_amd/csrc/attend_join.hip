@@ -1,0 +1,116 @@
+// Joins the partial sums of tiles whose keys were split into runs:
+//   out = sum_i 2^(top_i - top) part_i / sum_i 2^(top_i - top) sum_i, in run order.
+// A token whose tile was one run has nothing to join.
+#include "attend.h"
+
+namespace mori {
+namespace {
+
+constexpr uint32_t NW = 4;
+
+// WPH wavefronts share a head's runs (4 when there are few rows), else a
+// wavefront takes a head of the token each.
+template <typename DT, int DV, int WPH>
+__global__ __launch_bounds__(64 * NW) void attend_join_kernel(AttendArgs a) {
+  constexpr int W = DV / 64;  // elements of a lane
+  __shared__ float s_y[WPH > 1 ? NW : 1][DV], s_l[NW];
+  const uint32_t lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  constexpr uint32_t heads_wg = NW / WPH;
+  const uint32_t per_token = (a.heads + heads_wg - 1) / heads_wg;
+  const uint32_t t = blockIdx.x / per_token, h = (blockIdx.x - t * per_token) * heads_wg + (WPH > 1 ? 0 : wv);
+  const Item it = find_item(a, lane, [&](uint32_t, uint32_t n, uint32_t b) {
+    return n && a.b.seq_off[b] <= t && t < a.b.seq_off[b + 1];
+  });
+  if (!it.found || it.per_tile < 2) return;
+  if (h >= a.heads) return;  // only with a head per wavefront: no barrier follows
+  const Seq s = sequence(a.b, it.b);
+  const uint32_t kv = h / a.group, x = (t - s.t0) * a.group + (h - kv * a.group);
+  const uint32_t tiles = (s.n * a.group + a.tile_rows - 1) / a.tile_rows, tile = x / a.tile_rows;
+  const uint64_t item = it.first + (uint64_t)(tiles - 1 - tile) * it.per_tile;
+  const uint64_t at0 = (item * a.kv_heads + kv) * a.tile_rows + (x - tile * a.tile_rows);
+  const uint64_t step = (uint64_t)a.kv_heads * a.tile_rows;
+  const uint32_t runs = it.per_tile;
+
+  float top = NO_TOP;
+  for (uint32_t i = lane; i < runs; i += 64) top = fmaxf(top, a.part_ml[at0 + i * step].x);
+  top = max_over_16(max_over_32(top));
+#pragma unroll
+  for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+  float l = 0, y[W] = {};
+  const uint32_t r0 = WPH > 1 ? (uint32_t)((uint64_t)runs * wv / NW) : 0;
+  const uint32_t r1 = WPH > 1 ? (uint32_t)((uint64_t)runs * (wv + 1) / NW) : runs;
+  for (uint32_t i0 = r0; i0 < r1; i0 += 64) {
+    const uint32_t m = min(64u, r1 - i0);
+    float2 ml{NO_TOP, 0};
+    if (lane < m) ml = a.part_ml[at0 + (i0 + lane) * step];
+    const float f = ml.x == NO_TOP ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+    l += f * ml.y;
+    const uint64_t skip = __ballot(ml.x == NO_TOP);
+    for (uint32_t i = 0; i < m; i += 8) {
+      float v[8][W];
+#pragma unroll
+      for (uint32_t u = 0; u < 8; ++u) {
+        const float* src = a.part + (at0 + (i0 + min(i + u, m - 1)) * step) * DV + W * lane;
+#pragma unroll
+        for (int d = 0; d < W; ++d) v[u][d] = src[d];
+      }
+#pragma unroll
+      for (uint32_t u = 0; u < 8; ++u) {
+        if (i + u >= m || (skip >> (i + u) & 1)) continue;  // a run without keys wrote no rows
+        const float fu = bits<float>((uint32_t)__builtin_amdgcn_readlane((int)bits<uint32_t>(f), (int)(i + u)));
+#pragma unroll
+        for (int d = 0; d < W; ++d) y[d] += fu * v[u][d];
+      }
+    }
+  }
+  l = sum_over_16(sum_over_32(l));
+#pragma unroll
+  for (int d = 1; d < 16; d <<= 1) l += __shfl_xor(l, d);
+  if constexpr (WPH > 1) {
+#pragma unroll
+    for (int d = 0; d < W; ++d) s_y[wv][W * lane + d] = y[d];
+    if (lane == 0) s_l[wv] = l;
+    __syncthreads();
+    if (wv) return;
+    l = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < NW; ++i) l += s_l[i];
+#pragma unroll
+    for (int d = 0; d < W; ++d) {
+      y[d] = 0;
+#pragma unroll
+      for (uint32_t i = 0; i < NW; ++i) y[d] += s_y[i][W * lane + d];
+    }
+  }
+  const bool none = s.position(t - s.t0) < 0;
+  const float inv = 1.f / l;
+  typename DT::scalar* out =
+      reinterpret_cast<typename DT::scalar*>(a.out.data + t * a.out.token + h * a.out.head) + W * lane;
+#pragma unroll
+  for (int d = 0; d < W; ++d) out[d] = (typename DT::scalar)(none ? 0.f : y[d] * inv);
+  if (lane == 0) store_lse(a, RowAt{t, h}, top, l, none);
+}
+
+template <typename DT, int DV>
+void launch(const AttendArgs& a, hipStream_t s) {
+  // Few rows: a workgroup each, so that their runs are read by four wavefronts
+  if ((uint64_t)a.b.T * a.heads <= 1024)
+    hipLaunchKernelGGL((attend_join_kernel<DT, DV, NW>), dim3(a.b.T * a.heads), dim3(64 * NW), 0, s, a);
+  else
+    hipLaunchKernelGGL((attend_join_kernel<DT, DV, 1>), dim3(a.b.T * ((a.heads + NW - 1) / NW)), dim3(64 * NW), 0, s, a);
+}
+template <typename DT>
+void launch(const AttendArgs& a, uint32_t value, hipStream_t s) {
+  if (value == 64) launch<DT, 64>(a, s);
+  else if (value == 128) launch<DT, 128>(a, s);
+  else launch<DT, 512>(a, s);
+}
+
+}  // namespace
+
+void launch_attend_join(const AttendArgs& a, bool f16, uint32_t value, hipStream_t s) {
+  if (f16) launch<F16>(a, value, s);
+  else launch<BF16>(a, value, s);
+}
+
+}  // namespace mori

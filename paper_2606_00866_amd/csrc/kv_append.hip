@@ -18,12 +18,6 @@ namespace {
 
 constexpr uint32_t NT = 256;
 
-struct Rows {
-  uint8_t* data;
-  uint64_t token, head;  // strides in bytes
-};
-Rows rows_of(const mori_rows& r) { return {static_cast<uint8_t*>(r.data), 2 * r.token_stride, 2 * r.head_stride}; }
-
 struct AppendArgs {
   Batch b;
   Rows k, v, q, q_out;

@@ -7,31 +7,15 @@
 // the scores, the value's elements over the lanes for the sum.
 #include <cmath>
 
-#include "float16.h"
-#include "tokens.h"
+#include "attend.h"
 
 namespace mori {
 namespace {
 
 constexpr uint32_t NT = 256;
 
-struct Rows {
-  uint8_t* data;
-  uint64_t token, head;  // strides in bytes
-};
-Rows rows_of(const mori_rows& r) { return {static_cast<uint8_t*>(r.data), 2 * r.token_stride, 2 * r.head_stride}; }
-
-struct AttendArgs {
-  Batch b;
-  Rows q, out;
-  uint32_t heads, group;
-  float scale;
-  float* lse;
-  uint64_t v_off;  // from a key to its value
-};
-
 template <typename DT, int DK, int DV>
-__global__ __launch_bounds__(NT) void attend_rows_kernel(AttendArgs a) {
+__global__ __launch_bounds__(NT) void attend_rows_kernel(AttendArgs a, float scale, uint64_t v_off) {
   __shared__ float s_q[NT / 64][DK];
   const uint32_t lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   const uint64_t row = (uint64_t)blockIdx.x * (NT / 64) + wv;
@@ -47,7 +31,7 @@ __global__ __launch_bounds__(NT) void attend_rows_kernel(AttendArgs a) {
   }
   const int32_t pos = sq.error ? -1 : sq.position(t - sq.t0);
   const typename DT::scalar* q = reinterpret_cast<const typename DT::scalar*>(a.q.data + t * a.q.token + h * a.q.head);
-  for (int d = lane; d < DK; d += 64) s_q[wv][d] = (float)q[d] * a.scale;
+  for (int d = lane; d < DK; d += 64) s_q[wv][d] = (float)q[d] * scale;
   float o[DV / 64] = {}, m = -INFINITY, l = 0;
   for (int32_t k0 = 0; k0 <= pos; k0 += 64) {
     const int32_t key = k0 + (int32_t)lane;
@@ -72,7 +56,7 @@ __global__ __launch_bounds__(NT) void attend_rows_kernel(AttendArgs a) {
     l = l * keep + sum;
     m = m2;
     for (int i = 0; i < DV / 64; ++i) o[i] *= keep;
-    const uint64_t v_at = (uint64_t)at + a.v_off;
+    const uint64_t v_at = (uint64_t)at + v_off;
     for (int j = 0; j < 64 && k0 + j <= pos; ++j) {
       const typename DT::scalar* v = reinterpret_cast<const typename DT::scalar*>(wave::lane_of(v_at, j));
       const float pj = __shfl(p, j);
@@ -86,10 +70,20 @@ __global__ __launch_bounds__(NT) void attend_rows_kernel(AttendArgs a) {
   report(a.b, err);
 }
 
-// Host check of what the call and its workspace size take.
-bool attend_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, const mori_attend* at, uint32_t* error,
-               AttendArgs* out) {
-  AttendArgs& a = *out;
+// How a batch is run.
+struct Plan {
+  AttendArgs a;
+  uint32_t dim, value, blocks;
+  float scale;
+  bool f16, step, tile;
+  uint64_t ml_at, bytes;  // workspace
+};
+
+// Host check of what the call and its workspace size take, and the schedule.
+bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, const mori_attend* at, uint32_t* error,
+             Plan* out) {
+  Plan& p = *out;
+  AttendArgs& a = p.a;
   if (!at || !batch_of(pool, layer, tokens, error, &a.b)) return false;
   if (at->dtype > MORI_DT_BF16 || !at->kv_heads || !at->q_heads || at->q_heads > 1024) return false;
   if (at->q_heads % at->kv_heads || !std::isfinite(at->scale)) return false;
@@ -100,19 +94,46 @@ bool attend_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens,
     return false;
   }
   if ((uint64_t)a.b.T * at->q_heads >= (1u << 31)) return false;
+  if ((uint64_t)pool->num_blocks * pool->block_tokens >= (1ull << 32)) return false;
+  p.dim = at->head_dim;
+  p.value = at->value_dim;
+  p.scale = at->scale;
+  p.f16 = at->dtype == MORI_DT_F16;
   a.heads = at->q_heads;
+  a.kv_heads = at->kv_heads;
   a.group = at->q_heads / at->kv_heads;
-  a.scale = at->scale;
-  a.v_off = pool->planes == 2 ? a.b.plane_bytes : 0;
+  a.by_group = fast_div(a.group);
+  a.by_kv = fast_div(a.kv_heads);
+  a.c = at->scale == 0 ? 1.f : std::fabs(at->scale) * 1.4426950408889634f;
+  a.q_keep = at->scale == 0 ? 0u : 0xFFFFFFFFu;
+  a.q_flip = at->scale < 0 ? 0x80008000u : 0u;
+  const uint64_t rows = (uint64_t)a.b.max_new * a.group;
+  p.step = pool->planes == 2 && rows <= 32;
+  p.tile = pool->planes == 2 && !p.step;
+  p.blocks = rows <= 16 ? 1 : 2;
+  a.tile_rows = p.step ? 16 * p.blocks : 128;
+  a.unit = p.step ? 128 : 64;
+  const uint64_t tiles = (uint64_t)a.b.T * a.group / a.tile_rows + a.b.B;  // no batch has more
+  a.slots = ((p.step ? 1536 : 1024) + a.kv_heads - 1) / a.kv_heads;
+  a.least = (p.step ? 2 : 4);
+  a.splits = a.b.max_kv > a.least * a.unit && (p.step || tiles * a.kv_heads < 2048);
+  const uint64_t items = tiles + (a.splits ? a.slots : 0);
+  if (items * a.kv_heads >= (1ull << 31)) return false;
+  a.items = (uint32_t)items;
+  const uint64_t n = (p.step || p.tile) && a.splits ? items * a.kv_heads * a.tile_rows : 0;
+  p.ml_at = n * p.value * sizeof(float);
+  p.bytes = p.ml_at + n * sizeof(float2);
   return true;
 }
 
 template <typename DT>
-void launch(const AttendArgs& a, uint32_t dk, hipStream_t s) {
+void launch(const Plan& p, hipStream_t s) {
+  const AttendArgs& a = p.a;
+  const uint64_t v_off = p.value == p.dim ? a.b.plane_bytes : 0;
   const dim3 grid((uint32_t)(((uint64_t)a.b.T * a.heads + NT / 64 - 1) / (NT / 64)));
-  if (dk == 64) hipLaunchKernelGGL((attend_rows_kernel<DT, 64, 64>), grid, dim3(NT), 0, s, a);
-  else if (dk == 128) hipLaunchKernelGGL((attend_rows_kernel<DT, 128, 128>), grid, dim3(NT), 0, s, a);
-  else hipLaunchKernelGGL((attend_rows_kernel<DT, 576, 512>), grid, dim3(NT), 0, s, a);
+  if (p.dim == 64) hipLaunchKernelGGL((attend_rows_kernel<DT, 64, 64>), grid, dim3(NT), 0, s, a, p.scale, v_off);
+  else if (p.dim == 128) hipLaunchKernelGGL((attend_rows_kernel<DT, 128, 128>), grid, dim3(NT), 0, s, a, p.scale, v_off);
+  else hipLaunchKernelGGL((attend_rows_kernel<DT, 576, 512>), grid, dim3(NT), 0, s, a, p.scale, v_off);
 }
 
 }  // namespace
@@ -121,9 +142,9 @@ void launch(const AttendArgs& a, uint32_t dk, hipStream_t s) {
 extern "C" int mori_kv_attend_workspace(const mori_pool* pool, const mori_tokens* tokens, const mori_attend* attend,
                                         uint64_t* bytes) {
   using namespace mori;
-  AttendArgs a{};
-  if (!bytes || !attend_of(pool, 0, tokens, attend, nullptr, &a)) return MORI_EINVAL;
-  *bytes = 0;
+  Plan p{};
+  if (!bytes || !plan_of(pool, 0, tokens, attend, nullptr, &p)) return MORI_EINVAL;
+  *bytes = p.bytes;
   return MORI_OK;
 }
 
@@ -131,16 +152,30 @@ extern "C" int mori_kv_attend(const mori_pool* pool, uint32_t layer, const mori_
                               const mori_attend* attend, void* workspace, uint64_t workspace_bytes, uint32_t* error,
                               void* stream) {
   using namespace mori;
-  AttendArgs a{};
-  if (!attend_of(pool, layer, tokens, attend, error, &a)) return MORI_EINVAL;
+  Plan p{};
+  if (!plan_of(pool, layer, tokens, attend, error, &p)) return MORI_EINVAL;
+  AttendArgs& a = p.a;
   if (a.b.T == 0) return MORI_OK;
   if (!rows_valid(attend->q) || !rows_valid(attend->out)) return MORI_EINVAL;
+  if (p.bytes && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < p.bytes))
+    return MORI_EINVAL;
   a.q = rows_of(attend->q);
   a.out = rows_of(attend->out);
   a.lse = attend->lse;
+  a.part = static_cast<float*>(workspace);
+  a.part_ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + p.ml_at);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (attend->dtype == MORI_DT_F16) launch<F16>(a, attend->head_dim, s);
-  else launch<BF16>(a, attend->head_dim, s);
+  if (p.step) {
+    launch_attend_step(a, p.f16, p.dim, p.blocks, s);
+    if (a.splits) launch_attend_join(a, p.f16, p.value, s);
+  } else if (p.tile) {
+    launch_attend_tile(a, p.f16, p.dim, s);
+    if (a.splits) launch_attend_join(a, p.f16, p.value, s);
+  } else if (p.f16) {
+    launch<F16>(p, s);
+  } else {
+    launch<BF16>(p, s);
+  }
   if (hipGetLastError() != hipSuccess) return MORI_EHIP;
   return MORI_OK;
 }

@@ -76,6 +76,14 @@ inline bool rows_valid(const mori_rows& r) {
   return r.data && !(reinterpret_cast<uintptr_t>(r.data) & 15u) && !(r.token_stride & 7u) && !(r.head_stride & 7u);
 }
 
+struct Rows {
+  uint8_t* data;
+  uint64_t token, head;  // strides in bytes
+};
+inline Rows rows_of(const mori_rows& r) {
+  return {static_cast<uint8_t*>(r.data), 2 * r.token_stride, 2 * r.head_stride};
+}
+
 // One sequence of the batch.
 struct Seq {
   uint32_t t0, n;     // its tokens
