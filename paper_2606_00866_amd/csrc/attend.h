@@ -232,6 +232,24 @@ __device__ inline uint32_t pair_of(float lo, float hi) {
   return bits<uint32_t>(h);
 }
 
+// 16 B per lane from global memory straight into LDS: lane l's to dst + 16 l (dst
+// the same for the wavefront).  Nothing orders a read of dst after it but the
+// wait below, and across wavefronts a barrier behind that.
+__device__ inline void to_lds(const uint8_t* src, uint8_t* dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                   (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+}
+// All loads of the wavefront have arrived, those into LDS among them, and no
+// read of LDS is still under way.
+__device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+
+// Transposing read: 16 lanes take 4 rows of 16 elements, lane l's address being
+// that of elements 4 (l % 4) .. of row (l % 16) / 4; a lane gets one element of each row.
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+__device__ inline u32x2 read_tr(const uint8_t* p) {
+  return bits<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
+}
+
 // Whether a pair of 16-bit values holds an infinity or a NaN.
 __device__ inline bool odd_pair(BF16, uint32_t x) {
   return (x & 0x7F80u) == 0x7F80u || (x & 0x7F800000u) == 0x7F800000u;
@@ -240,9 +258,10 @@ __device__ inline bool odd_pair(F16, uint32_t x) {
   return (x & 0x7C00u) == 0x7C00u || (x & 0x7C000000u) == 0x7C000000u;
 }
 
-// Launchers, by kernel.  `tile` fills a.tile_rows and a.unit.
-void launch_attend_step(const AttendArgs& a, bool f16, uint32_t dim, uint32_t blocks, hipStream_t s);
+// Launchers, by kernel.
+void launch_attend_step(const AttendArgs& a, bool f16, uint32_t dim, hipStream_t s);
 void launch_attend_tile(const AttendArgs& a, bool f16, uint32_t dim, hipStream_t s);
+void launch_attend_latent(const AttendArgs& a, bool f16, hipStream_t s);
 void launch_attend_join(const AttendArgs& a, bool f16, uint32_t value, hipStream_t s);
 
 }  // namespace mori

@@ -246,21 +246,21 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(AttendArgs a) {
 }
 
 template <typename DT, int D>
-void launch(const AttendArgs& a, uint32_t blocks, hipStream_t s) {
+void launch(const AttendArgs& a, hipStream_t s) {
   const dim3 grid(a.items * a.kv_heads);
-  if (blocks == 1) hipLaunchKernelGGL((attend_step_kernel<DT, D, 1>), grid, dim3(64 * NW), 0, s, a);
+  if (a.tile_rows == 16) hipLaunchKernelGGL((attend_step_kernel<DT, D, 1>), grid, dim3(64 * NW), 0, s, a);
   else hipLaunchKernelGGL((attend_step_kernel<DT, D, 2>), grid, dim3(64 * NW), 0, s, a);
 }
 
 }  // namespace
 
-void launch_attend_step(const AttendArgs& a, bool f16, uint32_t dim, uint32_t blocks, hipStream_t s) {
+void launch_attend_step(const AttendArgs& a, bool f16, uint32_t dim, hipStream_t s) {
   if (dim == 64) {
-    if (f16) launch<F16, 64>(a, blocks, s);
-    else launch<BF16, 64>(a, blocks, s);
+    if (f16) launch<F16, 64>(a, s);
+    else launch<BF16, 64>(a, s);
   } else {
-    if (f16) launch<F16, 128>(a, blocks, s);
-    else launch<BF16, 128>(a, blocks, s);
+    if (f16) launch<F16, 128>(a, s);
+    else launch<BF16, 128>(a, s);
   }
 }
 

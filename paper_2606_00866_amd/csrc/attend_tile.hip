@@ -20,18 +20,6 @@ namespace mori {
 namespace {
 
 constexpr uint32_t STEP = 64;
-typedef __attribute__((address_space(3))) uint8_t lds8;
-typedef __attribute__((address_space(1))) const uint8_t glb8;
-
-__device__ inline void to_lds(const uint8_t* src, uint8_t* dst) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                   (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
-}
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-__device__ inline u32x2 read_tr(const uint8_t* p) {
-  return bits<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
-}
-
 template <typename DT, int D, int NW, int QB>
 __global__ __launch_bounds__(64 * NW, QB == 1 && NW == 4 ? 2 : 1) void attend_tile_kernel(AttendArgs a) {
   constexpr uint32_t NT = 64 * NW, ROW = 2 * D, CH = D / 8;  // bytes and chunks of a row
@@ -105,6 +93,7 @@ __global__ __launch_bounds__(64 * NW, QB == 1 && NW == 4 ? 2 : 1) void attend_ti
     find(w.lo);
     fetch(w.lo, 0);
     find(min(w.lo + STEP, last));
+    wait_loads();
     __syncthreads();
     uint32_t buf = 0;
     for (uint32_t k0 = w.lo; k0 < w.hi; k0 += STEP, buf ^= 1) {
@@ -211,6 +200,7 @@ __global__ __launch_bounds__(64 * NW, QB == 1 && NW == 4 ? 2 : 1) void attend_ti
             }
         }
       }
+      wait_loads();
       __syncthreads();
     }
   }
