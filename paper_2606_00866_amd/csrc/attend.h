@@ -250,12 +250,80 @@ __device__ inline u32x2 read_tr(const uint8_t* p) {
   return bits<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
 }
 
+// The wavefront's index in its workgroup, as the scalar it is.
+__device__ inline uint32_t wave_index() { return (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+
 // Whether a pair of 16-bit values holds an infinity or a NaN.
 __device__ inline bool odd_pair(BF16, uint32_t x) {
   return (x & 0x7F80u) == 0x7F80u || (x & 0x7F800000u) == 0x7F800000u;
 }
 __device__ inline bool odd_pair(F16, uint32_t x) {
   return (x & 0x7C00u) == 0x7C00u || (x & 0x7C000000u) == 0x7C000000u;
+}
+
+// A tile whose rows see different numbers of keys, among them one with an
+// infinity or a NaN: in the matrix products it would reach the rows before it
+// (weight 0 times NaN).  Such a run of keys is taken again row by row, a wavefront
+// a row with plain arithmetic over the keys it may see, and that result counts.
+// Nothing of the matrix kernels' state is needed, so this costs them no registers.
+template <typename DT, int DK, int DV>
+__device__ inline void rows_one_by_one(const AttendArgs& a, const Work& w, uint32_t first_row, uint32_t row_step,
+                                       uint32_t lane) {
+  constexpr int W = DV / 64;
+  typedef typename DT::scalar scalar;
+  const uint64_t v_off = DK == DV ? a.b.plane_bytes : 0;
+  uint32_t err = 0;  // reported by the pass before
+  for (uint32_t r = first_row; r < w.rows; r += row_step) {
+    const RowAt at = row_at(a, w, r);
+    const uint32_t allowed = row_limit(a, w, r), hi = min(allowed, w.hi);
+    const u32x4* const q = reinterpret_cast<const u32x4*>(q_row(a, at));
+    float top = NO_TOP, sum = 0, o[W] = {};
+    for (uint32_t k0 = w.lo; k0 < hi; k0 += 64) {
+      const uint32_t key = k0 + lane;
+      const uint8_t* row = a.b.plane;
+      float s = -INFINITY;
+      if (key < hi) {
+        row += (uint64_t)pool_row(a.b, key, table_entry(a.b, w.s, key), &err) * a.b.row + (uint64_t)w.kv * DK * 2;
+        s = 0;
+        for (int c = 0; c < DK / 8; ++c) {
+          float x[8], y[8];
+          widen<DT>(reinterpret_cast<const u32x4*>(row)[c], x);
+          widen<DT>(q_signed(a, q[c]), y);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s += x[i] * y[i];
+        }
+        s *= a.c;
+      }
+      float m = s;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+      const float t = fmaxf(top, m), keep = __builtin_amdgcn_exp2f(top - t), f = __builtin_amdgcn_exp2f(s - t);
+      top = t;
+      sum = sum * keep + f;
+#pragma unroll
+      for (int i = 0; i < W; ++i) o[i] *= keep;
+      const uint64_t v_at = reinterpret_cast<uint64_t>(row) + v_off;
+      for (uint32_t j = 0; j < 64 && k0 + j < hi; ++j) {
+        const scalar* v = reinterpret_cast<const scalar*>(wave::lane_of(v_at, (int)j));
+        const float fj = __shfl(f, (int)j);
+#pragma unroll
+        for (int i = 0; i < W; ++i) o[i] += fj * (float)v[64 * i + lane];
+      }
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+    if (w.per_tile > 1) {
+      const uint64_t p = ((uint64_t)w.item * a.kv_heads + w.kv) * a.tile_rows + r;
+#pragma unroll
+      for (int i = 0; i < W; ++i) a.part[p * DV + 64 * i + lane] = o[i];
+      if (lane == 0) a.part_ml[p] = float2{top, sum};
+    } else {
+      scalar* const out = reinterpret_cast<scalar*>(a.out.data + at.t * a.out.token + at.h * a.out.head);
+#pragma unroll
+      for (int i = 0; i < W; ++i) out[64 * i + lane] = (scalar)(allowed ? o[i] / sum : 0.f);
+      if (lane == 0) store_lse(a, at, top, sum, allowed == 0);
+    }
+  }
 }
 
 // Launchers, by kernel.

@@ -14,7 +14,7 @@ template <typename DT, int DV, int WPH>
 __global__ __launch_bounds__(64 * NW) void attend_join_kernel(AttendArgs a) {
   constexpr int W = DV / 64;  // elements of a lane
   __shared__ float s_y[WPH > 1 ? NW : 1][DV], s_l[NW];
-  const uint32_t lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const uint32_t lane = threadIdx.x & 63, wv = wave_index();
   constexpr uint32_t heads_wg = NW / WPH;
   const uint32_t per_token = (a.heads + heads_wg - 1) / heads_wg;
   const uint32_t t = blockIdx.x / per_token, h = (blockIdx.x - t * per_token) * heads_wg + (WPH > 1 ? 0 : wv);

@@ -38,6 +38,7 @@ __device__ inline uint32_t swizzle(uint32_t row) {
 struct Acc {
   f32x4 o[DB];
   float top, sum;
+  bool odd;  // a score was not finite where it could reach rows that must not see it
 };
 
 // One step of 32 keys at `at` (LDS): scores, weights, values.  Keys of the step
@@ -56,15 +57,11 @@ __device__ __forceinline__ void take(const AttendArgs& a, const Work& w, const u
     for (int i = 0; i < 2; ++i)
       s[i] = mfma_16x16x32(DT(), *reinterpret_cast<const u32x4*>(c + 16 * i * ROW), q[k], s[i]);
   }
-  bool odd = false;
   if (base + STEP > w.open || base + STEP > w.hi) {
     if (w.open < w.hi) {
-      // A key that is not finite shows in the scores of all rows.  Its products
-      // must not reach the rows before it (weight 0), so such a step goes key by
-      // key.
+      // a key that is not finite shows in the scores of every row
 #pragma unroll
-      for (int i = 0; i < 8; ++i) odd |= !__builtin_isfinite(s[i / 4][i % 4]);
-      odd = __any(odd);
+      for (int i = 0; i < 8; ++i) acc.odd |= !__builtin_isfinite(s[i / 4][i % 4]);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -89,43 +86,33 @@ __device__ __forceinline__ void take(const AttendArgs& a, const Work& w, const u
     acc.sum += f0 + f1;
     p[i] = pair_of<DT>(f0, f1);
   }
-  if (!odd) {
-    // transposing reads: key rows 4 g .. 4 g + 3 of each 16, 16 elements per 16 lanes
-    const uint32_t vrow = 4 * g + (lane >> 2 & 3);
-    const uint32_t vx = swizzle(vrow), vc = lane >> 1 & 1;
-    const uint8_t* const vs = at + vrow * ROW + 8 * (lane & 1);
-    const u32x4 pt = {p[0], p[1], p[2], p[3]};
+  // transposing reads: key rows 4 g .. 4 g + 3 of each 16, 16 elements per 16 lanes
+  const uint32_t vrow = 4 * g + (lane >> 2 & 3);
+  const uint32_t vx = swizzle(vrow), vc = lane >> 1 & 1;
+  const uint8_t* const vs = at + vrow * ROW + 8 * (lane & 1);
+  const u32x4 pt = {p[0], p[1], p[2], p[3]};
 #pragma unroll
-    for (int d = 0; d < DB; ++d) {
-      const uint8_t* c = vs + ((((2 * (d & 3) + vc) ^ vx) + 8 * (d >> 2)) << 4);
-      const u32x2 lo = read_tr(c), hi = read_tr(c + 16 * ROW);
-      acc.o[d] = mfma_16x16x32(DT(), u32x4{lo[0], lo[1], hi[0], hi[1]}, pt, acc.o[d]);
-    }
-  } else {
-    for (uint32_t j = 0; j < STEP && base + j < w.hi; ++j) {
-      // weight of key j: element j % 4 of block j / 16, lanes of group (j % 16) / 4
-      const uint32_t word0 = j < 16 ? p[0] : p[2], word1 = j < 16 ? p[1] : p[3];
-      const uint32_t word = (uint32_t)__shfl((int)(j & 2 ? word1 : word0), (int)(16 * (j % 16 / 4) + n));
-      const float f = (float)bits<typename DT::x2>(word)[j % 2];
-      if (base + j < limit) {
-        const uint32_t x = swizzle(j);
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          const uint32_t chunk = 2 * d + (g >> 1);
-          const typename DT::x4 v = *reinterpret_cast<const typename DT::x4*>(at + j * ROW + ((chunk ^ x) << 4) + 8 * (g & 1));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc.o[d][i] += f * (float)v[i];
-        }
-      }
-    }
+  for (int d = 0; d < DB; ++d) {
+    const uint8_t* c = vs + ((((2 * (d & 3) + vc) ^ vx) + 8 * (d >> 2)) << 4);
+    const u32x2 lo = read_tr(c), hi = read_tr(c + 16 * ROW);
+    acc.o[d] = mfma_16x16x32(DT(), u32x4{lo[0], lo[1], hi[0], hi[1]}, pt, acc.o[d]);
   }
 }
 
 // This group's loads of SUB steps into `to`: whole pool rows, chunks permuted.
+// Load i of a thread is chunk (i * RG + rg) * 64 + lane.
 template <int RG, int SUB>
 __device__ __forceinline__ void fetch(const AttendArgs& a, uint8_t* __restrict__ to, uint32_t row, uint32_t rg,
-                                      const uint32_t (&place)[9]) {
+                                      uint32_t lane) {
   constexpr uint32_t LOADS = 36 * SUB / RG;
+  // recomputed at every step: nine places kept over the products cost more registers than there are
+  asm volatile("" : "+v"(lane));
+  uint32_t place[9];
+#pragma unroll
+  for (uint32_t i = 0; i < 9; ++i) {
+    const uint32_t c = (i * RG + rg) * 64 + lane, r = c / CH, at = c - r * CH;
+    place[i] = r << 16 | (at ^ swizzle(r)) * 16;
+  }
 #pragma unroll
   for (uint32_t i = 0; i < LOADS; ++i) {
     // nine loads of the group cover 8 * RG rows (8 rows on, bit 3 of the row flips the chunk's lowest)
@@ -142,7 +129,7 @@ __global__ __launch_bounds__(RG == 8 ? 512 : 256, RG == 4 ? 2 : 1) void attend_l
   constexpr uint32_t AREA = KEYS * ROW;
   __shared__ __align__(256) uint8_t s_a[KG * AREA], s_b[RG == 1 ? 16 : KG * AREA];
   __shared__ float s_top[KG][RG * 16], s_sum[KG][RG * 16];
-  const uint32_t tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wv = wave_index();
   const uint32_t n = lane & 15, g = lane >> 4;
   const uint32_t rg = wv % RG, kg = wv / RG;
   const Work w = work_of(a, blockIdx.x, lane);
@@ -161,17 +148,11 @@ __global__ __launch_bounds__(RG == 8 ? 512 : 256, RG == 4 ? 2 : 1) void attend_l
   Acc acc;
   acc.top = NO_TOP;
   acc.sum = 0;
+  acc.odd = false;
 #pragma unroll
   for (int d = 0; d < DB; ++d) acc.o[d] = f32x4{0, 0, 0, 0};
 
   if (w.lo < w.hi) {
-    // load i of the group's thread is chunk i * 64 RG + 64 rg + lane: row and permuted byte of the first nine
-    uint32_t place[9];
-#pragma unroll
-    for (uint32_t i = 0; i < 9; ++i) {
-      const uint32_t c = (i * RG + rg) * 64 + lane, row = c / CH, at = c - row * CH;
-      place[i] = row << 16 | (at ^ swizzle(row)) * 16;
-    }
     constexpr uint32_t WG_KEYS = KEYS * KG;
     const auto key_of = [&](uint32_t base) { return min(base + (lane & (KEYS - 1)), last); };
     const auto pool_at = [&](uint32_t base, uint32_t entry) { return pool_row(a.b, key_of(base), entry, &err); };
@@ -181,7 +162,7 @@ __global__ __launch_bounds__(RG == 8 ? 512 : 256, RG == 4 ? 2 : 1) void attend_l
     uint32_t entry = table_entry(a.b, w.s, key_of(base));
     if constexpr (RG == 1) {
       if (base < w.hi) {
-        fetch<RG, SUB>(a, mine_a, pool_at(base, entry), rg, place);
+        fetch<RG, SUB>(a, mine_a, pool_at(base, entry), rg, lane);
         entry = table_entry(a.b, w.s, key_of(base + WG_KEYS));
         for (;;) {
           wait_loads();
@@ -189,19 +170,19 @@ __global__ __launch_bounds__(RG == 8 ? 512 : 256, RG == 4 ? 2 : 1) void attend_l
           base += WG_KEYS;
           if (base >= w.hi) break;
           wait_loads();  // the area has been read
-          fetch<RG, SUB>(a, mine_a, pool_at(base, entry), rg, place);
+          fetch<RG, SUB>(a, mine_a, pool_at(base, entry), rg, lane);
           entry = table_entry(a.b, w.s, key_of(base + WG_KEYS));
         }
       }
     } else {
       // every group takes the workgroup's number of steps (its keys past the end are masked)
-      fetch<RG, SUB>(a, mine_a, pool_at(base, entry), rg, place);
+      fetch<RG, SUB>(a, mine_a, pool_at(base, entry), rg, lane);
       entry = table_entry(a.b, w.s, key_of(base + WG_KEYS));
       wait_loads();
       __syncthreads();
       const auto step = [&](const uint8_t* __restrict__ now, uint8_t* __restrict__ then, uint32_t first) {
         if (first + WG_KEYS < w.hi) {
-          fetch<RG, SUB>(a, then, pool_at(base + WG_KEYS, entry), rg, place);
+          fetch<RG, SUB>(a, then, pool_at(base + WG_KEYS, entry), rg, lane);
           entry = table_entry(a.b, w.s, key_of(base + 2 * WG_KEYS));
         }
 #pragma unroll
@@ -220,6 +201,10 @@ __global__ __launch_bounds__(RG == 8 ? 512 : 256, RG == 4 ? 2 : 1) void attend_l
     }
   }
   if (__any(err != 0)) report(a.b, err);
+  if (w.open < w.hi && __syncthreads_or(acc.odd)) {
+    rows_one_by_one<DT, DK, DV>(a, w, wv, NW, lane);
+    return;
+  }
 
   // join the key groups: group 0 takes the others' rows in their order, through LDS
   acc.sum = sum_over_16(sum_over_32(acc.sum));
@@ -228,6 +213,7 @@ __global__ __launch_bounds__(RG == 8 ? 512 : 256, RG == 4 ? 2 : 1) void attend_l
       s_top[kg][r] = acc.top;
       s_sum[kg][r] = acc.sum;
     }
+    wait_loads();
     __syncthreads();  // also: the staging areas have been read
     float t = NO_TOP;
 #pragma unroll

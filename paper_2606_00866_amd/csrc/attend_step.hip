@@ -29,7 +29,7 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(AttendArgs a) {
   constexpr int VW = E / 2;        // their 32-bit words
   __shared__ float s_o[NW][16][D + 4];
   __shared__ float s_top[NW][16 * NB], s_sum[NW][16 * NB];
-  const uint32_t tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wv = wave_index();
   const uint32_t n = lane & 15, g = lane >> 4;
   const Work w = work_of(a, blockIdx.x, lane);
   if (!w.some) return;
@@ -58,6 +58,7 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(AttendArgs a) {
     for (int e = 0; e < E; ++e) o[nb][e] = f32x4{0, 0, 0, 0};
   }
 
+  bool odd = false;  // a value that rows see in part is infinite or NaN
   uint32_t k0 = w.lo + wv * STEP;
   if (k0 < w.hi) {
     u32x4 kr[2][KS];
@@ -141,54 +142,31 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(AttendArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) p[nb][i] = pair_of<DT>(f[2 * i], f[2 * i + 1]);
       }
-      // A step that some rows see only in part multiplies their weights of 0 with
-      // the values of later keys, which must not be infinite or NaN: such a step
-      // goes key by key, without the others' products.
-      bool odd = false;
       if (k0 + STEP > w.open && w.open < w.hi) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
           for (int i = 0; i < VW; ++i) odd |= odd_pair(DT(), vr[j][i]);
       }
-      if (__any(odd)) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        u32x4 v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          v[j] = __builtin_amdgcn_perm(vr[2 * j + 1][e / 2], vr[2 * j][e / 2], e % 2 ? 0x07060302u : 0x05040100u);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
-          for (uint32_t j = 0; j < STEP && k0 + j < w.hi; ++j) {
-            const uint32_t key = k0 + j;
-            // weights of key j: words 2 (j / 16) + (j % 4) / 2 of the lanes of group (j % 16) / 4
-            uint32_t word = 0;
-#pragma unroll
-            for (uint32_t i = 0; i < 4; ++i)
-              if (2 * (j / 16) + (j % 4) / 2 == i) word = p[nb][i];
-            word = (uint32_t)__shfl((int)word, (int)(16 * ((j % 16) / 4) + n));
-            const float f = (float)bits<typename DT::x2>(word)[j % 2];
-            if (key >= limit[nb]) continue;
-            const uint32_t at = pool_row(a.b, key, table_entry(a.b, w.s, key), &err);
-            const typename DT::scalar* v = reinterpret_cast<const typename DT::scalar*>(
-                a.b.plane + a.b.plane_bytes + (uint64_t)w.kv * (2 * D) + (uint64_t)at * a.b.row) + 4 * g * E;
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) o[nb][e][i] += f * (float)v[i * E + e];
-          }
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          u32x4 v;
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            v[j] = __builtin_amdgcn_perm(vr[2 * j + 1][e / 2], vr[2 * j][e / 2], e % 2 ? 0x07060302u : 0x05040100u);
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-            o[nb][e] = mfma_16x16x32(DT(), v, u32x4{p[nb][0], p[nb][1], p[nb][2], p[nb][3]}, o[nb][e]);
-        }
+          o[nb][e] = mfma_16x16x32(DT(), v, u32x4{p[nb][0], p[nb][1], p[nb][2], p[nb][3]}, o[nb][e]);
       }
       if (!more) break;
       k0 = next;
     }
   }
   if (__any(err != 0)) report(a.b, err);
+  if (w.open < w.hi && __syncthreads_or(odd)) {
+    rows_one_by_one<DT, D, D>(a, w, wv, NW, lane);
+    return;
+  }
 
   // join the wavefronts, in their order
 #pragma unroll

@@ -29,7 +29,7 @@ __global__ __launch_bounds__(64 * NW, QB == 1 && NW == 4 ? 2 : 1) void attend_ti
   constexpr int KS = D / 16, DB = D / 32;
   __shared__ __align__(256) uint8_t s_k[2][TILE];
   __shared__ __align__(256) uint8_t s_v[2][TILE];
-  const uint32_t tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wv = wave_index();
   const uint32_t n = lane & 31, h = lane >> 5;
   const Work w = work_of(a, blockIdx.x, lane);
   if (!w.some) return;
@@ -63,6 +63,7 @@ __global__ __launch_bounds__(64 * NW, QB == 1 && NW == 4 ? 2 : 1) void attend_ti
       for (int i = 0; i < 16; ++i) o[qb][d][i] = 0;
   }
 
+  bool odd = false;  // a value that rows see in part is infinite or NaN
   if (w.lo < w.hi) {
     // this thread's part of a load: row and permuted chunk
     const uint32_t lr = tid / CH, lc = tid % CH;
@@ -102,14 +103,11 @@ __global__ __launch_bounds__(64 * NW, QB == 1 && NW == 4 ? 2 : 1) void attend_ti
         find(min(k0 + 2 * STEP, last));
       }
       const bool mixed = k0 + STEP > w.open || k0 + STEP > w.hi;
-      bool odd = false;
       if (k0 + STEP > w.open && w.open < w.hi) {
-        // a later key's infinity or NaN must not reach the rows before it (see below)
         for (uint32_t i = 0; i < LD; ++i) {
           const u32x4 x = *reinterpret_cast<const u32x4*>(&s_v[buf][(i * NT + tid) * 16]);
           for (int j = 0; j < 4; ++j) odd |= odd_pair(DT(), x[j]);
         }
-        odd = __syncthreads_or(odd);
       }
       if (k0 < wave_hi) {
         const uint8_t* const ks = s_k[buf] + n * ROW;
@@ -159,45 +157,18 @@ __global__ __launch_bounds__(64 * NW, QB == 1 && NW == 4 ? 2 : 1) void attend_ti
             p[qb][i] = pair_of<DT>(f0, f1);
           }
         }
-        if (!odd) {
 #pragma unroll
-          for (int t = 0; t < 4; ++t) {
+        for (int t = 0; t < 4; ++t) {
 #pragma unroll
-            for (int d = 0; d < DB; ++d) {
-              const uint8_t* at = vs + 16 * t * ROW + (((4 * d + vc) ^ vx) << 4);
-              const u32x2 lo = read_tr(at), hi = read_tr(at + 8 * ROW);
-              const u32x4 v = {lo[0], lo[1], hi[0], hi[1]};
+          for (int d = 0; d < DB; ++d) {
+            const uint8_t* at = vs + 16 * t * ROW + (((4 * d + vc) ^ vx) << 4);
+            const u32x2 lo = read_tr(at), hi = read_tr(at + 8 * ROW);
+            const u32x4 v = {lo[0], lo[1], hi[0], hi[1]};
 #pragma unroll
-              for (int qb = 0; qb < QB; ++qb)
-                o[qb][d] = mfma_32x32x16(DT(), v, u32x4{p[qb][4 * t], p[qb][4 * t + 1], p[qb][4 * t + 2], p[qb][4 * t + 3]},
-                                         o[qb][d]);
-            }
+            for (int qb = 0; qb < QB; ++qb)
+              o[qb][d] = mfma_32x32x16(DT(), v, u32x4{p[qb][4 * t], p[qb][4 * t + 1], p[qb][4 * t + 2], p[qb][4 * t + 3]},
+                                       o[qb][d]);
           }
-        } else {
-          // key by key, without the products of masked rows
-#pragma unroll
-          for (int qb = 0; qb < QB; ++qb)
-            for (uint32_t j = 0; j < STEP && k0 + j < w.hi; ++j) {
-              // weight of key j: element (j % 32) / 8 * 4 + j % 4 of block j / 32, lanes of half (j % 8) / 4
-              const uint32_t e = 16 * (j / 32) + (j % 32) / 8 * 4 + j % 4;
-              uint32_t word = 0;
-#pragma unroll
-              for (uint32_t i = 0; i < 16; ++i)
-                if (e / 2 == i) word = p[qb][i];
-              word = (uint32_t)__shfl((int)word, (int)(32 * (j % 8 / 4) + n));
-              const float f = (float)bits<typename DT::x2>(word)[e % 2];
-              if (k0 + j < limit[qb]) {
-                const uint32_t x = D == 128 ? (j & 3) << 2 : ((j >> 1) & 1) << 2;
-#pragma unroll
-                for (int d = 0; d < DB; ++d)
-#pragma unroll
-                  for (int i = 0; i < 16; ++i) {
-                    const uint32_t el = 32 * d + 8 * (i / 4) + 4 * h + i % 4;
-                    o[qb][d][i] += f * (float)*reinterpret_cast<const typename DT::scalar*>(
-                                           &s_v[buf][j * ROW + (((el / 8) ^ x) << 4) + 2 * (el % 8)]);
-                  }
-              }
-            }
         }
       }
       wait_loads();
@@ -205,6 +176,10 @@ __global__ __launch_bounds__(64 * NW, QB == 1 && NW == 4 ? 2 : 1) void attend_ti
     }
   }
   if (__any(err != 0)) report(a.b, err);
+  if (w.open < w.hi && __syncthreads_or(odd)) {
+    rows_one_by_one<DT, D, D>(a, w, wv, NW, lane);
+    return;
+  }
 
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
