@@ -128,6 +128,9 @@ struct Work {
   bool first_run, some;
 };
 
+// A value that is the same in every lane, in a scalar register.
+__device__ inline uint32_t same(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+
 __device__ inline Work work_of(const AttendArgs& a, uint32_t block, uint32_t lane) {
   Work w{};
   w.item = divide(block, a.by_kv);
@@ -138,20 +141,25 @@ __device__ inline Work work_of(const AttendArgs& a, uint32_t block, uint32_t lan
   if (block == 0 && it.bad) report(a.b, MORI_DEV_BAD_TOKENS);
   if (!w.some) return w;
   w.s = sequence(a.b, it.b);
+  w.s.t0 = same(w.s.t0);
+  w.s.n = same(w.s.n);
+  w.s.len = same(w.s.len);
+  w.s.tbl = same(w.s.tbl);
+  w.s.error = same(w.s.error);
   const uint32_t tiles = (w.s.n * a.group + a.tile_rows - 1) / a.tile_rows;
   const uint32_t k = w.item - it.first, back = k / it.per_tile, run = k - back * it.per_tile;
   w.per_tile = it.per_tile;
   w.first_run = run == 0;
   // the last tile first: with a causal mask it has the most keys
-  w.row0 = (tiles - 1 - back) * a.tile_rows;
+  w.row0 = same((tiles - 1 - back) * a.tile_rows);
   w.rows = min(a.tile_rows, w.s.n * a.group - w.row0);
   // keys of the tile's first and last row: up to and with their own positions
   const int32_t at0 = w.s.position(divide(w.row0, a.by_group)) + 1;
   const int32_t at1 = w.s.position(divide(w.row0 + w.rows - 1, a.by_group)) + 1;
-  w.open = (uint32_t)max(at0, 0);
+  w.open = same((uint32_t)max(at0, 0));
   const uint64_t lo = (uint64_t)run * it.run_units * a.unit, hi = lo + (uint64_t)it.run_units * a.unit;
-  w.lo = (uint32_t)min(lo, (uint64_t)0x7FFFFFFFu);
-  w.hi = (uint32_t)min(hi, (uint64_t)(uint32_t)max(at1, 0));
+  w.lo = same((uint32_t)min(lo, (uint64_t)0x7FFFFFFFu));
+  w.hi = same((uint32_t)min(hi, (uint64_t)(uint32_t)max(at1, 0)));
   return w;
 }
 
@@ -248,6 +256,23 @@ __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 __device__ inline u32x2 read_tr(const uint8_t* p) {
   return bits<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
+}
+
+// N products whose first operand is read from LDS by read(i), AHEAD reads in
+// flight.  The order is fixed: left to itself the compiler keeps one operand and
+// waits for every read where registers are scarce.
+template <int N, int AHEAD, typename R, typename P>
+__device__ __forceinline__ void products(R read, P product) {
+  u32x4 f[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) f[i] = read(i);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    product(i, f[i % AHEAD]);
+    if (i + AHEAD < N) f[i % AHEAD] = read(i + AHEAD);
+    __builtin_amdgcn_sched_barrier(0);
+  }
 }
 
 // The wavefront's index in its workgroup, as the scalar it is.

@@ -29,6 +29,7 @@ namespace {
 constexpr uint32_t STEP = 32, ROW = 1152, CH = 72;
 constexpr int DK = 576, DV = 512;
 constexpr int KS = DK / 32, DB = DV / 16;
+constexpr int AHEAD = 5;  // operands read ahead of the products
 
 __device__ inline uint32_t swizzle(uint32_t row) {
   return (row >> 1 & 1) << 2 | (row >> 2 & 1) << 1 | (row >> 3 & 1);
@@ -50,13 +51,12 @@ __device__ __forceinline__ void take(const AttendArgs& a, const Work& w, const u
   f32x4 s[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
   const uint32_t kx = swizzle(n);  // the same for key n + 16
   const uint8_t* const ks = at + n * ROW;
-#pragma unroll
-  for (int k = 0; k < KS; ++k) {
-    const uint8_t* const c = ks + ((((4 * (k & 1) + g) ^ kx) + 8 * (k >> 1)) << 4);
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      s[i] = mfma_16x16x32(DT(), *reinterpret_cast<const u32x4*>(c + 16 * i * ROW), q[k], s[i]);
-  }
+  products<2 * KS, AHEAD>(
+      [&](int x) {
+        const int k = x >> 1;
+        return *reinterpret_cast<const u32x4*>(ks + ((((4 * (k & 1) + g) ^ kx) + 8 * (k >> 1)) << 4) + 16 * (x & 1) * ROW);
+      },
+      [&](int x, u32x4 f) { s[x & 1] = mfma_16x16x32(DT(), f, q[x >> 1], s[x & 1]); });
   if (base + STEP > w.open || base + STEP > w.hi) {
     if (w.open < w.hi) {
       // a key that is not finite shows in the scores of every row
@@ -91,12 +91,13 @@ __device__ __forceinline__ void take(const AttendArgs& a, const Work& w, const u
   const uint32_t vx = swizzle(vrow), vc = lane >> 1 & 1;
   const uint8_t* const vs = at + vrow * ROW + 8 * (lane & 1);
   const u32x4 pt = {p[0], p[1], p[2], p[3]};
-#pragma unroll
-  for (int d = 0; d < DB; ++d) {
-    const uint8_t* c = vs + ((((2 * (d & 3) + vc) ^ vx) + 8 * (d >> 2)) << 4);
-    const u32x2 lo = read_tr(c), hi = read_tr(c + 16 * ROW);
-    acc.o[d] = mfma_16x16x32(DT(), u32x4{lo[0], lo[1], hi[0], hi[1]}, pt, acc.o[d]);
-  }
+  products<DB, AHEAD>(
+      [&](int d) {
+        const uint8_t* c = vs + ((((2 * (d & 3) + vc) ^ vx) + 8 * (d >> 2)) << 4);
+        const u32x2 lo = read_tr(c), hi = read_tr(c + 16 * ROW);
+        return u32x4{lo[0], lo[1], hi[0], hi[1]};
+      },
+      [&](int d, u32x4 f) { acc.o[d] = mfma_16x16x32(DT(), f, pt, acc.o[d]); });
 }
 
 // This group's loads of SUB steps into `to`: whole pool rows, chunks permuted.
@@ -122,12 +123,25 @@ __device__ __forceinline__ void fetch(const AttendArgs& a, uint8_t* __restrict__
   }
 }
 
+// A group's step: the next keys set out for one area, these taken from the other.
+// (The areas' being apart is what lets the reads run beside the loads.)
+template <typename DT, int RG, int SUB>
+__device__ __forceinline__ void step(const AttendArgs& a, const Work& w, const uint8_t* __restrict__ now,
+                                     uint8_t* __restrict__ then, bool more, uint32_t row, uint32_t rg,
+                                     const u32x4 (&q)[KS], Acc& acc, uint32_t base, uint32_t limit, uint32_t lane) {
+  if (more) fetch<RG, SUB>(a, then, row, rg, lane);
+#pragma unroll 1
+  for (uint32_t i = 0; i < SUB; ++i)
+    if (base + STEP * i < w.hi) take<DT>(a, w, now + i * STEP * ROW, q, acc, base + STEP * i, limit, lane);
+}
+
 template <typename DT, int RG>
 __global__ __launch_bounds__(RG == 8 ? 512 : 256, RG == 4 ? 2 : 1) void attend_latent_kernel(AttendArgs a) {
   constexpr int NW = RG == 8 ? 8 : 4, KG = NW / RG, SUB = RG == 8 ? 2 : 1;
   constexpr uint32_t KEYS = STEP * SUB;  // a group's keys at a time
   constexpr uint32_t AREA = KEYS * ROW;
-  __shared__ __align__(256) uint8_t s_a[KG * AREA], s_b[RG == 1 ? 16 : KG * AREA];
+  constexpr uint32_t AREAS = RG == 1 ? 1 : 2;  // of each group
+  __shared__ __align__(256) uint8_t s_a[AREAS * KG * AREA];
   __shared__ float s_top[KG][RG * 16], s_sum[KG][RG * 16];
   const uint32_t tid = threadIdx.x, lane = tid & 63, wv = wave_index();
   const uint32_t n = lane & 15, g = lane >> 4;
@@ -157,46 +171,37 @@ __global__ __launch_bounds__(RG == 8 ? 512 : 256, RG == 4 ? 2 : 1) void attend_l
     const auto key_of = [&](uint32_t base) { return min(base + (lane & (KEYS - 1)), last); };
     const auto pool_at = [&](uint32_t base, uint32_t entry) { return pool_row(a.b, key_of(base), entry, &err); };
     uint32_t base = w.lo + kg * KEYS;
-    uint8_t* const mine_a = s_a + kg * AREA;
-    uint8_t* const mine_b = RG == 1 ? mine_a : s_b + kg * AREA;
+    uint8_t* const mine = s_a + kg * (AREAS * AREA);
     uint32_t entry = table_entry(a.b, w.s, key_of(base));
     if constexpr (RG == 1) {
       if (base < w.hi) {
-        fetch<RG, SUB>(a, mine_a, pool_at(base, entry), rg, lane);
+        fetch<RG, SUB>(a, mine, pool_at(base, entry), rg, lane);
         entry = table_entry(a.b, w.s, key_of(base + WG_KEYS));
         for (;;) {
           wait_loads();
-          take<DT>(a, w, mine_a, q, acc, base, limit, lane);
+          take<DT>(a, w, mine, q, acc, base, limit, lane);
           base += WG_KEYS;
           if (base >= w.hi) break;
           wait_loads();  // the area has been read
-          fetch<RG, SUB>(a, mine_a, pool_at(base, entry), rg, lane);
+          fetch<RG, SUB>(a, mine, pool_at(base, entry), rg, lane);
           entry = table_entry(a.b, w.s, key_of(base + WG_KEYS));
         }
       }
     } else {
       // every group takes the workgroup's number of steps (its keys past the end are masked)
-      fetch<RG, SUB>(a, mine_a, pool_at(base, entry), rg, lane);
+      fetch<RG, SUB>(a, mine, pool_at(base, entry), rg, lane);
       entry = table_entry(a.b, w.s, key_of(base + WG_KEYS));
       wait_loads();
       __syncthreads();
-      const auto step = [&](const uint8_t* __restrict__ now, uint8_t* __restrict__ then, uint32_t first) {
-        if (first + WG_KEYS < w.hi) {
-          fetch<RG, SUB>(a, then, pool_at(base + WG_KEYS, entry), rg, lane);
-          entry = table_entry(a.b, w.s, key_of(base + 2 * WG_KEYS));
-        }
-#pragma unroll
-        for (int i = 0; i < SUB; ++i)
-          if (base + STEP * i < w.hi) take<DT>(a, w, now + i * STEP * ROW, q, acc, base + STEP * i, limit, lane);
+      uint32_t now = 0;
+      for (uint32_t first = w.lo; first < w.hi; first += WG_KEYS, now ^= AREA) {
+        const bool more = first + WG_KEYS < w.hi;
+        const uint32_t row = more ? pool_at(base + WG_KEYS, entry) : 0;
+        step<DT, RG, SUB>(a, w, mine + now, mine + (now ^ AREA), more, row, rg, q, acc, base, limit, lane);
+        if (more) entry = table_entry(a.b, w.s, key_of(base + 2 * WG_KEYS));
         base += WG_KEYS;
         wait_loads();
         __syncthreads();
-      };
-      for (uint32_t first = w.lo;;) {
-        step(mine_a, mine_b, first);
-        if ((first += WG_KEYS) >= w.hi) break;
-        step(mine_b, mine_a, first);
-        if ((first += WG_KEYS) >= w.hi) break;
       }
     }
   }
