@@ -17,7 +17,7 @@ import numpy as np
 import torch
 
 from . import mori as M
-from .tiering import MoriError, PoolGeometry, _stream, check
+from .tiering import MoriError, PoolGeometry, check
 
 DTYPES = {torch.float16: M.MORI_DT_F16, torch.bfloat16: M.MORI_DT_BF16}
 STYLES = {"half": M.MORI_ROPE_HALF, "pairs": M.MORI_ROPE_PAIRS}
@@ -36,6 +36,11 @@ def rope_table(positions: int, rot_dim: int, theta: float = 10000.0, device="cud
     angle = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * \
         theta ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64, device=device) / rot_dim)
     return torch.cat([angle.cos(), angle.sin()], 1).float()
+
+
+def _stream_of(batch, stream) -> int:
+    """The stream's handle; by default the current one of the batch's device."""
+    return torch._C._cuda_getCurrentRawStream(batch.index) if stream is None else stream.cuda_stream
 
 
 def _on(stream):
@@ -73,6 +78,7 @@ class TokenBatch:
         _need(num_tokens >= 0 and max_new >= 0 and 0 < max_kv < 1 << 31, "TokenBatch: bounds out of range")
         _need(tbl_off.numel() >= 2, "TokenBatch: tbl_off is empty")
         self.device = kv_len.device
+        self.index = kv_len.device.index
         self.error = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._keep = (tbl_off, tbl, seq_off, kv_len, program)
         self.desc = M.mori_tokens(self.num_seqs, self.num_tokens, int(max_new), int(max_kv), seq_off.data_ptr(),
@@ -114,16 +120,18 @@ def _rows(name: str, x: torch.Tensor, batch: TokenBatch, dtype: torch.dtype, hea
           dim: int | None = None, written: bool = False) -> M.mori_rows:
     """A [tokens][heads][elements] view with its strides; elements are adjacent.
     Views to write have a place for every element (no broadcast)."""
-    _need(x.dim() == 3 and x.shape[0] == batch.num_tokens and x.dtype == dtype and x.device == batch.device,
-          f"{name}: [{batch.num_tokens}][heads][elements] of {dtype} on {batch.device}")
-    _need((heads is None or x.shape[1] == heads) and (dim is None or x.shape[2] == dim),
-          f"{name}: shape {tuple(x.shape)}, not [tokens][{heads}][{dim}]")
-    _need(x.shape[2] == 0 or x.stride(2) == 1, f"{name}: elements are not adjacent")
+    shape, strides = x.shape, x.stride()
+    if len(shape) != 3 or shape[0] != batch.num_tokens or x.dtype != dtype or x.device != batch.device:
+        raise MoriError(f"{name}: [{batch.num_tokens}][heads][elements] of {dtype} on {batch.device}", M.MORI_EINVAL)
+    tokens, h, d = shape
+    if (heads is not None and h != heads) or (dim is not None and d != dim):
+        raise MoriError(f"{name}: shape {tuple(shape)}, not [tokens][{heads}][{dim}]", M.MORI_EINVAL)
     # a stride over one token or one head is never used; views may carry any value there
-    token = x.stride(0) if x.shape[0] > 1 else 0
-    head = x.stride(1) if x.shape[1] > 1 else 0
-    _need(token >= 0 and head >= 0, f"{name}: strides")
-    _need(not written or ((token > 0 or x.shape[0] < 2) and (head > 0 or x.shape[1] < 2)), f"{name}: broadcast")
+    token = strides[0] if tokens > 1 else 0
+    head = strides[1] if h > 1 else 0
+    if (d and strides[2] != 1) or (written and ((tokens > 1 and not token) or (h > 1 and not head))):
+        raise MoriError(f"{name}: strides {strides}: elements are adjacent, and views to write have a place for each",
+                        M.MORI_EINVAL)
     return M.mori_rows(x.data_ptr() or None, token, head)
 
 
@@ -159,7 +167,7 @@ def kv_append(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, k: torch.
                 q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         a.q_out = _rows("q_out", q_out, heads=q.shape[1], dim=q.shape[2], written=True, **kw)
         a.q_heads = q.shape[1]
-    check(M.mori_kv_append(_pool(pool, geom), int(layer), batch.desc, a, batch.error.data_ptr(), _stream(stream)),
+    check(M.mori_kv_append(_pool(pool, geom), int(layer), batch.desc, a, batch.error.data_ptr(), _stream_of(batch, stream)),
           "mori_kv_append")
     return q_out
 
@@ -213,5 +221,5 @@ def kv_attend(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, q: torch.
         with _on(stream):
             workspace = torch.empty(n, dtype=torch.uint8, device=batch.device)
     check(M.mori_kv_attend(desc, int(layer), batch.desc, a, workspace.data_ptr(), workspace.numel(),
-                           batch.error.data_ptr(), _stream(stream)), "mori_kv_attend")
+                           batch.error.data_ptr(), _stream_of(batch, stream)), "mori_kv_attend")
     return out

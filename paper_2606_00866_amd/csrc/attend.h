@@ -136,16 +136,22 @@ __device__ inline Work work_of(const AttendArgs& a, uint32_t block, uint32_t lan
   w.item = divide(block, a.by_kv);
   w.kv = block - w.item * a.kv_heads;
   const uint32_t item = w.item;
+  // batches of up to 64: every lane has its sequence's numbers on the way while the item is found
+  const bool few = a.b.B <= 64;
+  SeqNumbers x{};
+  if (few && lane < a.b.B) x = read_sequence(a.b, lane);
   const Item it = find_item(a, lane, [&](uint32_t first, uint32_t n, uint32_t) { return item - first < n; });
   w.some = it.found;
   if (block == 0 && it.bad) report(a.b, MORI_DEV_BAD_TOKENS);
   if (!w.some) return w;
-  w.s = sequence(a.b, it.b);
-  w.s.t0 = same(w.s.t0);
-  w.s.n = same(w.s.n);
-  w.s.len = same(w.s.len);
-  w.s.tbl = same(w.s.tbl);
-  w.s.error = same(w.s.error);
+  if (few) {
+    const auto of = [&](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, (int)it.b); };
+    x = SeqNumbers{of(x.lo), of(x.hi), of(x.len), of(x.p), of(x.first), of(x.last)};
+  } else {
+    x = read_sequence(a.b, it.b);
+    x = SeqNumbers{same(x.lo), same(x.hi), same(x.len), same(x.p), same(x.first), same(x.last)};
+  }
+  w.s = checked_sequence(a.b, x);
   const uint32_t tiles = (w.s.n * a.group + a.tile_rows - 1) / a.tile_rows;
   const uint32_t k = w.item - it.first, back = k / it.per_tile, run = k - back * it.per_tile;
   w.per_tile = it.per_tile;
@@ -295,6 +301,8 @@ template <typename DT, int DK, int DV>
 __device__ inline void rows_one_by_one(const AttendArgs& a, const Work& w, uint32_t first_row, uint32_t row_step,
                                        uint32_t lane) {
   constexpr int W = DV / 64;
+  typedef float vec __attribute__((ext_vector_type(W)));  // vectors, not arrays: those would end up in LDS
+  typedef float f32x8 __attribute__((ext_vector_type(8)));
   typedef typename DT::scalar scalar;
   const uint64_t v_off = DK == DV ? a.b.plane_bytes : 0;
   uint32_t err = 0;  // reported by the pass before
@@ -302,7 +310,8 @@ __device__ inline void rows_one_by_one(const AttendArgs& a, const Work& w, uint3
     const RowAt at = row_at(a, w, r);
     const uint32_t allowed = row_limit(a, w, r), hi = min(allowed, w.hi);
     const u32x4* const q = reinterpret_cast<const u32x4*>(q_row(a, at));
-    float top = NO_TOP, sum = 0, o[W] = {};
+    float top = NO_TOP, sum = 0;
+    vec o = 0;
     for (uint32_t k0 = w.lo; k0 < hi; k0 += 64) {
       const uint32_t key = k0 + lane;
       const uint8_t* row = a.b.plane;
@@ -311,11 +320,9 @@ __device__ inline void rows_one_by_one(const AttendArgs& a, const Work& w, uint3
         row += (uint64_t)pool_row(a.b, key, table_entry(a.b, w.s, key), &err) * a.b.row + (uint64_t)w.kv * DK * 2;
         s = 0;
         for (int c = 0; c < DK / 8; ++c) {
-          float x[8], y[8];
-          widen<DT>(reinterpret_cast<const u32x4*>(row)[c], x);
-          widen<DT>(q_signed(a, q[c]), y);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) s += x[i] * y[i];
+          const f32x8 x = __builtin_convertvector(bits<typename DT::x8>(reinterpret_cast<const u32x4*>(row)[c]), f32x8) *
+                          __builtin_convertvector(bits<typename DT::x8>(q_signed(a, q[c])), f32x8);
+          s += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
         }
         s *= a.c;
       }
@@ -325,8 +332,7 @@ __device__ inline void rows_one_by_one(const AttendArgs& a, const Work& w, uint3
       const float t = fmaxf(top, m), keep = __builtin_amdgcn_exp2f(top - t), f = __builtin_amdgcn_exp2f(s - t);
       top = t;
       sum = sum * keep + f;
-#pragma unroll
-      for (int i = 0; i < W; ++i) o[i] *= keep;
+      o *= keep;
       const uint64_t v_at = reinterpret_cast<uint64_t>(row) + v_off;
       for (uint32_t j = 0; j < 64 && k0 + j < hi; ++j) {
         const scalar* v = reinterpret_cast<const scalar*>(wave::lane_of(v_at, (int)j));

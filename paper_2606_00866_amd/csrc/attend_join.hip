@@ -6,13 +6,13 @@
 namespace mori {
 namespace {
 
-constexpr uint32_t NW = 4;
-
-// WPH wavefronts share a head's runs (4 when there are few rows), else a
-// wavefront takes a head of the token each.
-template <typename DT, int DV, int WPH>
+// WPH wavefronts share a head's runs (8 when there are few rows, so that all runs
+// are on the way at once), else a wavefront takes a head of the token each.
+template <typename DT, int DV, int NW, int WPH>
 __global__ __launch_bounds__(64 * NW) void attend_join_kernel(AttendArgs a) {
-  constexpr int W = DV / 64;  // elements of a lane
+  constexpr int W = DV / 64;                // elements of a lane
+  constexpr uint32_t U = W > 2 ? 8 : 16;    // runs on the way at a time
+  typedef float vec __attribute__((ext_vector_type(W)));
   __shared__ float s_y[WPH > 1 ? NW : 1][DV], s_l[NW];
   const uint32_t lane = threadIdx.x & 63, wv = wave_index();
   constexpr uint32_t heads_wg = NW / WPH;
@@ -23,22 +23,23 @@ __global__ __launch_bounds__(64 * NW) void attend_join_kernel(AttendArgs a) {
   });
   if (!it.found || it.per_tile < 2) return;
   if (h >= a.heads) return;  // only with a head per wavefront: no barrier follows
-  const Seq s = sequence(a.b, it.b);
-  const uint32_t kv = h / a.group, x = (t - s.t0) * a.group + (h - kv * a.group);
-  const uint32_t tiles = (s.n * a.group + a.tile_rows - 1) / a.tile_rows, tile = x / a.tile_rows;
+  const uint32_t t0 = same(a.b.seq_off[it.b]), n = same(a.b.seq_off[it.b + 1]) - t0;
+  const uint32_t kv = h / a.group, x = (t - t0) * a.group + (h - kv * a.group);
+  const uint32_t tiles = (n * a.group + a.tile_rows - 1) / a.tile_rows, tile = x / a.tile_rows;
   const uint64_t item = it.first + (uint64_t)(tiles - 1 - tile) * it.per_tile;
   const uint64_t at0 = (item * a.kv_heads + kv) * a.tile_rows + (x - tile * a.tile_rows);
   const uint64_t step = (uint64_t)a.kv_heads * a.tile_rows;
   const uint32_t runs = it.per_tile;
+  const uint32_t r0 = WPH > 1 ? (uint32_t)((uint64_t)runs * wv / NW) : 0;
+  const uint32_t r1 = WPH > 1 ? (uint32_t)((uint64_t)runs * (wv + 1) / NW) : runs;
 
   float top = NO_TOP;
   for (uint32_t i = lane; i < runs; i += 64) top = fmaxf(top, a.part_ml[at0 + i * step].x);
   top = max_over_16(max_over_32(top));
 #pragma unroll
   for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-  float l = 0, y[W] = {};
-  const uint32_t r0 = WPH > 1 ? (uint32_t)((uint64_t)runs * wv / NW) : 0;
-  const uint32_t r1 = WPH > 1 ? (uint32_t)((uint64_t)runs * (wv + 1) / NW) : runs;
+  float l = 0;
+  vec y = 0;
   for (uint32_t i0 = r0; i0 < r1; i0 += 64) {
     const uint32_t m = min(64u, r1 - i0);
     float2 ml{NO_TOP, 0};
@@ -46,20 +47,15 @@ __global__ __launch_bounds__(64 * NW) void attend_join_kernel(AttendArgs a) {
     const float f = ml.x == NO_TOP ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
     l += f * ml.y;
     const uint64_t skip = __ballot(ml.x == NO_TOP);
-    for (uint32_t i = 0; i < m; i += 8) {
-      float v[8][W];
+    for (uint32_t i = 0; i < m; i += U) {
+      vec v[U];
 #pragma unroll
-      for (uint32_t u = 0; u < 8; ++u) {
-        const float* src = a.part + (at0 + (i0 + min(i + u, m - 1)) * step) * DV + W * lane;
+      for (uint32_t u = 0; u < U; ++u)
+        v[u] = *reinterpret_cast<const vec*>(a.part + (at0 + (i0 + min(i + u, m - 1)) * step) * DV + W * lane);
 #pragma unroll
-        for (int d = 0; d < W; ++d) v[u][d] = src[d];
-      }
-#pragma unroll
-      for (uint32_t u = 0; u < 8; ++u) {
+      for (uint32_t u = 0; u < U; ++u) {
         if (i + u >= m || (skip >> (i + u) & 1)) continue;  // a run without keys wrote no rows
-        const float fu = bits<float>((uint32_t)__builtin_amdgcn_readlane((int)bits<uint32_t>(f), (int)(i + u)));
-#pragma unroll
-        for (int d = 0; d < W; ++d) y[d] += fu * v[u][d];
+        y += v[u] * bits<float>((uint32_t)__builtin_amdgcn_readlane((int)bits<uint32_t>(f), (int)(i + u)));
       }
     }
   }
@@ -82,6 +78,7 @@ __global__ __launch_bounds__(64 * NW) void attend_join_kernel(AttendArgs a) {
       for (uint32_t i = 0; i < NW; ++i) y[d] += s_y[i][W * lane + d];
     }
   }
+  const Seq s = sequence(a.b, it.b);
   const bool none = s.position(t - s.t0) < 0;
   const float inv = 1.f / l;
   typename DT::scalar* out =
@@ -93,11 +90,11 @@ __global__ __launch_bounds__(64 * NW) void attend_join_kernel(AttendArgs a) {
 
 template <typename DT, int DV>
 void launch(const AttendArgs& a, hipStream_t s) {
-  // Few rows: a workgroup each, so that their runs are read by four wavefronts
+  // Few rows: a workgroup each, so that all of their runs are read at once
   if ((uint64_t)a.b.T * a.heads <= 1024)
-    hipLaunchKernelGGL((attend_join_kernel<DT, DV, NW>), dim3(a.b.T * a.heads), dim3(64 * NW), 0, s, a);
+    hipLaunchKernelGGL((attend_join_kernel<DT, DV, 8, 8>), dim3(a.b.T * a.heads), dim3(512), 0, s, a);
   else
-    hipLaunchKernelGGL((attend_join_kernel<DT, DV, 1>), dim3(a.b.T * ((a.heads + NW - 1) / NW)), dim3(64 * NW), 0, s, a);
+    hipLaunchKernelGGL((attend_join_kernel<DT, DV, 4, 1>), dim3(a.b.T * ((a.heads + 3) / 4)), dim3(256), 0, s, a);
 }
 template <typename DT>
 void launch(const AttendArgs& a, uint32_t value, hipStream_t s) {

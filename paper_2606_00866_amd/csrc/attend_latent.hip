@@ -267,6 +267,254 @@ __global__ __launch_bounds__(RG == 8 ? 512 : 256, RG == 4 ? 2 : 1) void attend_l
   }
 }
 
+// ---- up to 128 rows --------------------------------------------------------
+// Eight wavefronts of 16 rows would each read every key from LDS: 544 KiB for 32
+// keys, and what a wavefront waits for is those reads.  Here two wavefronts share
+// 32 rows, so that a read serves two products: of the scores each takes half of the
+// elements for all 32 rows (the halves are added through LDS), of the values half
+// of the 512.  A wavefront's own 16 rows are its block 0, its partner's block 1; it
+// finishes the scores of its own and hands over their weights.
+//   barrier - scores of half the elements - other block's half to LDS - barrier -
+//   add, weights, to LDS - barrier - values
+// Keys are staged in three areas: two steps' loads are under way.
+namespace wide {
+
+constexpr int NW = 8, AREAS = 3, LOADS = 5;
+constexpr uint32_t AREA = LOADS * NW * 1024;  // 32 rows and a tail that is loaded but not read
+constexpr int KS = DK / 64, DB = DV / 32;  // steps and value blocks of a half
+
+// Barrier for data in LDS that wavefronts wrote themselves (loads into LDS may be
+// under way; those are waited for by count).
+__device__ inline void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// All but the newest step's loads have arrived.
+__device__ inline void wait_step() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(LOADS) : "memory"); }
+
+// Stores to LDS that the compiler does not set behind the loads into LDS under way
+// (it orders any store after all of them); barrier() waits for these.
+template <typename T>
+__device__ inline uint32_t lds_address(T* p) {
+  return (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) T*)p);
+}
+__device__ inline void put(f32x4* p, f32x4 v) {
+  asm volatile("ds_write_b128 %0, %1" ::"v"(lds_address(p)), "v"(v) : "memory");
+}
+__device__ inline void put(u32x4* p, u32x4 v) {
+  asm volatile("ds_write_b128 %0, %1" ::"v"(lds_address(p)), "v"(v) : "memory");
+}
+__device__ inline void put(float* p, float v) {
+  asm volatile("ds_write_b32 %0, %1" ::"v"(lds_address(p)), "v"(v) : "memory");
+}
+
+// 16-B chunk of a key that lane group g reads for step k of half h: the groups'
+// chunks are 128 B apart, so that only the rows decide the banks (but in the last
+// step, which takes the row's last 128 B).
+__device__ inline uint32_t chunk_of(uint32_t k, uint32_t h, uint32_t g) {
+  return k < 8 ? 8 * (4 * (k >> 2) + g) + 4 * h + (k & 3) : 64 + 4 * h + g;
+}
+
+// A step's loads: five by every wavefront, so that they can be waited for by count
+// (36 would do: the last four bring rows 0 to 3 again).
+__device__ __forceinline__ void fetch(const AttendArgs& a, uint8_t* __restrict__ to, uint32_t row, uint32_t wv,
+                                      uint32_t lane) {
+  asm volatile("" : "+v"(lane));  // the places are recomputed at every step: there is no room to keep them
+#pragma unroll
+  for (uint32_t i = 0; i < LOADS; ++i) {
+    const uint32_t c = (i * NW + wv) * 64 + lane, r = c / CH, at = c - r * CH;
+    const uint32_t p = (uint32_t)__shfl((int)row, (int)r);
+    to_lds(a.b.plane + (uint64_t)p * ROW + ((at ^ swizzle(r)) << 4), to + (i * NW + wv) * 1024);
+  }
+}
+
+struct Shared {
+  alignas(16) f32x4 part[NW][2][64];  // scores of the partner's rows over this wavefront's elements
+  alignas(16) u32x4 weight[NW][64];
+  float keep[NW][16], top[NW][16], sum[NW][16];
+};
+
+struct Acc {
+  f32x4 o[DB][2];  // this wavefront's elements: its own rows, its partner's
+  float top, sum;  // of its own rows
+  bool odd;
+};
+
+template <typename DT>
+__device__ __forceinline__ void step(const AttendArgs& a, const Work& w, const uint8_t* __restrict__ now,
+                                     uint8_t* __restrict__ then, uint32_t row, Shared& x,
+                                     const u32x4 (&q)[KS][2], Acc& acc, uint32_t base, uint32_t limit, uint32_t wv,
+                                     uint32_t lane) {
+  fetch(a, then, row, wv, lane);
+  asm volatile("" : "+v"(lane));  // as in fetch
+  const uint32_t n = lane & 15, g = lane >> 4, h = wv & 1;
+  f32x4 s[2][2];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) s[b][0] = s[b][1] = f32x4{0, 0, 0, 0};
+  const uint32_t kx = swizzle(n);  // the same for key n + 16
+  const uint8_t* const ks = now + n * ROW;
+  products<2 * KS, 4>(
+      [&](int i) {
+        return *reinterpret_cast<const u32x4*>(ks + ((chunk_of(i >> 1, h, g) ^ kx) << 4) + 16 * (i & 1) * ROW);
+      },
+      [&](int i, u32x4 f) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) s[b][i & 1] = mfma_16x16x32(DT(), f, q[i >> 1][b], s[b][i & 1]);
+      });
+  // the compiler sees no store here: the products' delay before their results may be read is kept by hand
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15\n\ts_nop 3" ::: "memory");
+  put(&x.part[wv][0][lane], s[1][0]);
+  put(&x.part[wv][1][lane], s[1][1]);
+  barrier();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) s[0][i] += x.part[wv ^ 1][i][lane];
+  if (base + STEP > w.open || base + STEP > w.hi) {
+    if (w.open < w.hi) {
+      // a key that is not finite shows in the scores of every row
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc.odd |= !__builtin_isfinite(s[0][i / 4][i % 4]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (base + 16 * (i / 4) + 4 * g + i % 4 >= limit) s[0][i / 4][i % 4] = -INFINITY;
+  }
+  float m = s[0][0][0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) m = fmaxf(m, s[0][i / 4][i % 4]);
+  m = a.c * max_over_16(max_over_32(m));
+  float keep = 1.f;
+  if (__any(m > acc.top + RISE)) {
+    const float t = fmaxf(acc.top, m);
+    keep = __builtin_amdgcn_exp2f(acc.top - t);
+    acc.top = t;
+    acc.sum *= keep;
+  }
+  u32x4 p[2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float f0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][i / 2][2 * i % 4], a.c, -acc.top));
+    const float f1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][i / 2][2 * i % 4 + 1], a.c, -acc.top));
+    acc.sum += f0 + f1;
+    p[0][i] = pair_of<DT>(f0, f1);
+  }
+  put(&x.weight[wv][lane], p[0]);
+  put(&x.keep[wv][n], keep);
+  wait_step();
+  barrier();
+  p[1] = x.weight[wv ^ 1][lane];
+  const float keep1 = x.keep[wv ^ 1][n];
+  if (__any(keep != 1.f || keep1 != 1.f)) {
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+      acc.o[d][0] *= keep;
+      acc.o[d][1] *= keep1;
+    }
+  }
+  // transposing reads: key rows 4 g .. 4 g + 3 of each 16, 16 elements per 16 lanes
+  const uint32_t vrow = 4 * g + (lane >> 2 & 3);
+  const uint32_t vx = swizzle(vrow), vc = lane >> 1 & 1;
+  const uint8_t* const vs = now + vrow * ROW + 8 * (lane & 1) + h * DV;
+  products<DB, 4>(
+      [&](int d) {
+        const uint8_t* c = vs + ((((2 * (d & 3) + vc) ^ vx) + 8 * (d >> 2)) << 4);
+        const u32x2 lo = read_tr(c), hi = read_tr(c + 16 * ROW);
+        return u32x4{lo[0], lo[1], hi[0], hi[1]};
+      },
+      [&](int d, u32x4 f) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) acc.o[d][b] = mfma_16x16x32(DT(), f, p[b], acc.o[d][b]);
+      });
+}
+
+template <typename DT>
+__global__ __launch_bounds__(64 * NW, 1) void attend_latent_wide_kernel(AttendArgs a) {
+  __shared__ __align__(256) uint8_t key[AREAS * AREA];  // apart from the rest: loads into it run beside reads of that
+  __shared__ Shared x;
+  const uint32_t lane = threadIdx.x & 63, wv = wave_index();
+  const uint32_t n = lane & 15, g = lane >> 4, h = wv & 1;
+  const Work w = work_of(a, blockIdx.x, lane);
+  if (!w.some) return;
+  uint32_t err = w.s.error;
+  const uint32_t last = w.hi - 1;
+  const uint32_t limit = min(row_limit(a, w, 16 * wv + n), w.hi);
+
+  u32x4 q[KS][2];
+  Acc acc;
+  acc.odd = false;
+  acc.top = NO_TOP;
+  acc.sum = 0;
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const uint32_t r = 16 * (wv ^ b) + n;
+    const u32x4* src = reinterpret_cast<const u32x4*>(q_row(a, row_at(a, w, min(r, w.rows - 1))));
+#pragma unroll
+    for (int k = 0; k < KS; ++k) q[k][b] = q_signed(a, src[chunk_of(k, h, g)]);
+#pragma unroll
+    for (int d = 0; d < DB; ++d) acc.o[d][b] = f32x4{0, 0, 0, 0};
+  }
+
+  if (w.lo < w.hi) {
+    const auto key_of = [&](uint32_t base) { return min(base + (lane & (STEP - 1)), last); };
+    const auto pool_at = [&](uint32_t base, uint32_t entry) { return pool_row(a.b, key_of(base), entry, &err); };
+    // loads past the end take the last key again: every step counts the same loads
+    fetch(a, key, pool_at(w.lo, table_entry(a.b, w.s, key_of(w.lo))), wv, lane);
+    const uint32_t second = min(w.lo + STEP, last);
+    const uint32_t row1 = pool_at(second, table_entry(a.b, w.s, key_of(second)));
+    uint32_t entry = table_entry(a.b, w.s, key_of(min(w.lo + 2 * STEP, last)));
+    fetch(a, key + AREA, row1, wv, lane);
+    wait_step();
+    barrier();
+    uint32_t now = 0, then = 2 * AREA;
+    for (uint32_t base = w.lo; base < w.hi; base += STEP) {
+      const uint32_t ahead = min(base + 2 * STEP, last);
+      const uint32_t row = pool_at(ahead, entry);
+      entry = table_entry(a.b, w.s, key_of(min(base + 3 * STEP, last)));
+      step<DT>(a, w, key + now, key + then, row, x, q, acc, base, limit, wv, lane);
+      now = now == 2 * AREA ? 0 : now + AREA;
+      then = then == 2 * AREA ? 0 : then + AREA;
+      barrier();
+    }
+    wait_loads();
+  }
+  if (__any(err != 0)) report(a.b, err);
+  if (w.open < w.hi && __syncthreads_or(acc.odd)) {
+    rows_one_by_one<DT, DK, DV>(a, w, wv, NW, lane);
+    return;
+  }
+
+  acc.sum = sum_over_16(sum_over_32(acc.sum));
+  if (g == 0) {
+    x.top[wv][n] = acc.top;
+    x.sum[wv][n] = acc.sum;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const uint32_t r = 16 * (wv ^ b) + n;
+    const float top = x.top[wv ^ b][n], sum = x.sum[wv ^ b][n];
+    if (r >= w.rows) continue;
+    if (w.per_tile > 1) {
+      const uint64_t at = (uint64_t)w.item * a.tile_rows + r;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+        *reinterpret_cast<f32x4*>(a.part + at * DV + h * (DV / 2) + 16 * d + 4 * g) = acc.o[d][b];
+      if (g == 0 && b == 0) a.part_ml[at] = float2{top, sum};
+    } else {
+      const RowAt at = row_at(a, w, r);
+      const bool none = row_limit(a, w, r) == 0;
+      const float inv = 1.f / sum;
+      uint8_t* out = a.out.data + at.t * a.out.token + at.h * a.out.head + h * DV;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        const f32x4 y = acc.o[d][b] * inv;
+        const u32x2 z = {pair_of<DT>(y[0], y[1]), pair_of<DT>(y[2], y[3])};
+        *reinterpret_cast<u32x2*>(out + 2 * (16 * d + 4 * g)) = none ? u32x2{0, 0} : z;
+      }
+      if (g == 0 && b == 0) store_lse(a, at, top, sum, none);
+    }
+  }
+}
+
+}  // namespace wide
+
 template <typename DT>
 void launch(const AttendArgs& a, hipStream_t s) {
   const dim3 grid(a.items);
@@ -274,7 +522,7 @@ void launch(const AttendArgs& a, hipStream_t s) {
     case 16: hipLaunchKernelGGL((attend_latent_kernel<DT, 1>), grid, dim3(256), 0, s, a); break;
     case 32: hipLaunchKernelGGL((attend_latent_kernel<DT, 2>), grid, dim3(256), 0, s, a); break;
     case 64: hipLaunchKernelGGL((attend_latent_kernel<DT, 4>), grid, dim3(256), 0, s, a); break;
-    default: hipLaunchKernelGGL((attend_latent_kernel<DT, 8>), grid, dim3(512), 0, s, a); break;
+    default: hipLaunchKernelGGL((wide::attend_latent_wide_kernel<DT>), grid, dim3(64 * wide::NW), 0, s, a); break;
   }
 }
 

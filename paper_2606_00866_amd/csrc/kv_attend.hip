@@ -5,6 +5,7 @@
 //
 // Three kernels by what bounds them (few rows per key head, many, latent rows),
 // and one that joins the runs of split contexts; see attend.h for what they share.
+#include <algorithm>
 #include <cmath>
 
 #include "attend.h"
@@ -64,7 +65,9 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
   a.slots = ((p.step ? 1536 : p.latent && a.tile_rows == 128 ? 512 : 1024) + a.kv_heads - 1) / a.kv_heads;
   a.least = (p.step ? 2 : 4);
   a.splits = a.b.max_kv > a.least * a.unit && tiles * a.kv_heads < 2048;
-  const uint64_t items = tiles + (a.splits ? a.slots : 0);
+  // runs have `least` units or more, so short contexts give fewer items than slots
+  const uint64_t runs = tiles * (((uint64_t)a.b.max_kv + a.unit - 1) / a.unit) / a.least;
+  const uint64_t items = tiles + (a.splits ? std::min<uint64_t>(a.slots, runs + 1) : 0);
   if (items * a.kv_heads >= (1ull << 31)) return false;
   a.items = (uint32_t)items;
   const uint64_t n = a.splits ? items * a.kv_heads * a.tile_rows : 0;

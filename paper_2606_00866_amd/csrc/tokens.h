@@ -94,32 +94,40 @@ struct Seq {
   __device__ int32_t position(uint32_t i) const { return (int32_t)(len + i) - (int32_t)n; }
 };
 
-// Sequence b < B, checked.  Every bound that later indexing relies on holds
+// What the batch and the tables say of a sequence.
+struct SeqNumbers {
+  uint32_t lo, hi, len, p, first, last;
+};
+__device__ inline SeqNumbers read_sequence(const Batch& a, uint32_t b) {
+  SeqNumbers x{a.seq_off[b], a.seq_off[b + 1], a.kv_len[b], a.program ? a.program[b] : b, 1, 0};
+  if (x.p < a.P) {
+    x.first = a.tbl_off[x.p];
+    x.last = a.tbl_off[x.p + 1];
+  }
+  return x;
+}
+
+// A sequence, checked.  Every bound that later indexing relies on holds
 // afterwards: t0 + n <= T, and len <= blocks * bt with tbl + blocks <= tbl_len.
-__device__ inline Seq sequence(const Batch& a, uint32_t b) {
+__device__ inline Seq checked_sequence(const Batch& a, const SeqNumbers& x) {
   Seq s{};
-  const uint32_t lo = a.seq_off[b], hi = a.seq_off[b + 1], len = a.kv_len[b];
-  const uint32_t p = a.program ? a.program[b] : b;
-  if (lo > hi || hi > a.T) {
+  if (x.lo > x.hi || x.hi > a.T) {
     s.error = MORI_DEV_BAD_TOKENS;
     return s;
   }
   s.named = true;
-  s.t0 = lo;
-  s.n = hi - lo;
-  if (s.n > a.max_new || len > a.max_kv || p >= a.P) {
+  s.t0 = x.lo;
+  s.n = x.hi - x.lo;
+  if (s.n > a.max_new || x.len > a.max_kv || x.p >= a.P || x.first > x.last || x.last > a.tbl_len ||
+      (uint64_t)(x.last - x.first) * a.bt < x.len) {
     s.error = MORI_DEV_BAD_TOKENS;
     return s;
   }
-  const uint32_t first = a.tbl_off[p], last = a.tbl_off[p + 1];
-  if (first > last || last > a.tbl_len || (uint64_t)(last - first) * a.bt < len) {
-    s.error = MORI_DEV_BAD_TOKENS;
-    return s;
-  }
-  s.tbl = first;
-  s.len = len;
+  s.tbl = x.first;
+  s.len = x.len;
   return s;
 }
+__device__ inline Seq sequence(const Batch& a, uint32_t b) { return checked_sequence(a, read_sequence(a, b)); }
 
 // The page of a block as the table has it: its id, or 0 and the error bit.
 __device__ inline uint32_t checked_page(const Batch& a, uint32_t id, uint32_t* err) {
