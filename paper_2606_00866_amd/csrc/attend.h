@@ -201,6 +201,12 @@ __device__ inline uint32_t table_entry(const Batch& b, const Seq& s, uint32_t ke
   return b.tbl[s.tbl + divide(key, b.by_bt)];
 }
 
+// Byte offset in a plane of a key's row, all of it in scalar registers; `entry` is its block's.
+__device__ inline uint64_t row_bytes_at(const Batch& b, uint32_t key, uint32_t entry, uint32_t* err) {
+  const uint32_t block = divide(key, b.by_bt);
+  return checked_page(b, entry, err) * b.run + (uint64_t)(key - block * b.bt) * b.row;
+}
+
 // Where the logarithm of a row's sum goes; top and sum in the kernels' units.
 __device__ inline void store_lse(const AttendArgs& a, RowAt p, float top, float sum, bool none) {
   if (a.lse) a.lse[(uint64_t)p.t * a.heads + p.h] = none ? -INFINITY : (top + __log2f(sum)) * 0.69314718055994531f;

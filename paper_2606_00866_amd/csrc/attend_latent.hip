@@ -316,7 +316,6 @@ __device__ inline uint32_t chunk_of(uint32_t k, uint32_t h, uint32_t g) {
 // (36 would do: the last four bring rows 0 to 3 again).
 __device__ __forceinline__ void fetch(const AttendArgs& a, uint8_t* __restrict__ to, uint32_t row, uint32_t wv,
                                       uint32_t lane) {
-  asm volatile("" : "+v"(lane));  // the places are recomputed at every step: there is no room to keep them
 #pragma unroll
   for (uint32_t i = 0; i < LOADS; ++i) {
     const uint32_t c = (i * NW + wv) * 64 + lane, r = c / CH, at = c - r * CH;
@@ -342,8 +341,8 @@ __device__ __forceinline__ void step(const AttendArgs& a, const Work& w, const u
                                      uint8_t* __restrict__ then, uint32_t row, Shared& x,
                                      const u32x4 (&q)[KS][2], Acc& acc, uint32_t base, uint32_t limit, uint32_t wv,
                                      uint32_t lane) {
+  asm volatile("" : "+v"(lane));  // what follows from it is computed at every step: there is no room to keep it
   fetch(a, then, row, wv, lane);
-  asm volatile("" : "+v"(lane));  // as in fetch
   const uint32_t n = lane & 15, g = lane >> 4, h = wv & 1;
   f32x4 s[2][2];
 #pragma unroll
@@ -436,6 +435,17 @@ __global__ __launch_bounds__(64 * NW, 1) void attend_latent_wide_kernel(AttendAr
   const uint32_t last = w.hi - 1;
   const uint32_t limit = min(row_limit(a, w, 16 * wv + n), w.hi);
 
+  const auto key_of = [&](uint32_t base) { return min(base + (lane & (STEP - 1)), last); };
+  const auto pool_at = [&](uint32_t base, uint32_t entry) { return pool_row(a.b, key_of(base), entry, &err); };
+  uint32_t entry = 0;
+  if (w.lo < w.hi) {  // the first keys on the way, then the queries
+    // loads past the end take the last key again: every step counts the same loads
+    fetch(a, key, pool_at(w.lo, table_entry(a.b, w.s, key_of(w.lo))), wv, lane);
+    const uint32_t second = min(w.lo + STEP, last);
+    const uint32_t row1 = pool_at(second, table_entry(a.b, w.s, key_of(second)));
+    entry = table_entry(a.b, w.s, key_of(min(w.lo + 2 * STEP, last)));
+    fetch(a, key + AREA, row1, wv, lane);
+  }
   u32x4 q[KS][2];
   Acc acc;
   acc.odd = false;
@@ -452,14 +462,6 @@ __global__ __launch_bounds__(64 * NW, 1) void attend_latent_wide_kernel(AttendAr
   }
 
   if (w.lo < w.hi) {
-    const auto key_of = [&](uint32_t base) { return min(base + (lane & (STEP - 1)), last); };
-    const auto pool_at = [&](uint32_t base, uint32_t entry) { return pool_row(a.b, key_of(base), entry, &err); };
-    // loads past the end take the last key again: every step counts the same loads
-    fetch(a, key, pool_at(w.lo, table_entry(a.b, w.s, key_of(w.lo))), wv, lane);
-    const uint32_t second = min(w.lo + STEP, last);
-    const uint32_t row1 = pool_at(second, table_entry(a.b, w.s, key_of(second)));
-    uint32_t entry = table_entry(a.b, w.s, key_of(min(w.lo + 2 * STEP, last)));
-    fetch(a, key + AREA, row1, wv, lane);
     wait_step();
     barrier();
     uint32_t now = 0, then = 2 * AREA;

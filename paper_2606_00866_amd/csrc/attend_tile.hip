@@ -1,6 +1,6 @@
 // Attention of many rows per key head (chunks, prompts), bound by the matrix rate.
 //
-// A workgroup takes NW * 32 * QB rows and walks the keys in steps of 64; keys and
+// A workgroup takes 128 rows, 32 a wavefront, and walks the keys in steps of 64; keys and
 // values of a step are staged in LDS, two steps' worth, so that the next step's
 // loads run behind this one's products.
 //   scores   S^T = K Q^T, 32x32x16: a wavefront's rows are the columns, so a row's
@@ -19,203 +19,253 @@
 namespace mori {
 namespace {
 
-constexpr uint32_t STEP = 64;
-template <typename DT, int D, int NW, int QB>
-__global__ __launch_bounds__(64 * NW, QB == 1 && NW == 4 ? 2 : 1) void attend_tile_kernel(AttendArgs a) {
-  constexpr uint32_t NT = 64 * NW, ROW = 2 * D, CH = D / 8;  // bytes and chunks of a row
-  constexpr uint32_t TILE = STEP * ROW;
-  constexpr uint32_t LD = STEP * CH / NT;  // chunks a thread loads of each
-  constexpr uint32_t RPL = NT / CH;        // rows of one load of the workgroup
-  constexpr int KS = D / 16, DB = D / 32;
-  __shared__ __align__(256) uint8_t s_k[2][TILE];
-  __shared__ __align__(256) uint8_t s_v[2][TILE];
+constexpr uint32_t STEP = 64, NW = 4;
+// A wavefront's rows and its place in the loads.
+template <int D, bool PAGED>
+struct Tile {
+  static constexpr uint32_t NT = 64 * NW, ROW = 2 * D, CH = D / 8;  // bytes and chunks of a row
+  static constexpr uint32_t AREA = STEP * ROW;
+  static constexpr uint32_t LD = STEP * CH / NT;  // chunks a thread loads of each
+  static constexpr uint32_t RPL = NT / CH;        // rows of one load of the workgroup
+  static constexpr uint32_t RPW = 64 / CH;        // and of a wavefront
+  static constexpr int KS = D / 16, DB = D / 32;
+  static constexpr int BETWEEN = KS / LD;         // steps of the scores from one load to the next
+
+  u32x4 q[KS];
+  f32x16 o[DB];
+  float top, sum;
+  uint32_t limit, wave_hi;  // keys of a row, most of any row
+  bool odd;                     // a value that rows see in part is infinite or NaN
+  uint32_t entry[LD], err;
+  // Byte offsets of this thread's chunks from the first row of a load.  They stay
+  // where they are: a register that held a load's address counts as busy until the
+  // load is done, and these are never anything else.
+  uint32_t k_off, v_off;
+
+  __device__ __forceinline__ void place(const AttendArgs& a, uint32_t tid) {
+    const uint32_t lr = tid / CH, lc = tid % CH, in_load = PAGED ? lr % RPW * a.b.row : 0;
+    k_off = 16 * (lc ^ (D == 128 ? lr & 15 : (lr >> 1) & 7)) + in_load;
+    v_off = 16 * (lc ^ (D == 128 ? (lr & 3) << 2 : ((lr >> 1) & 1) << 2)) + in_load;
+  }
+
+  // Table entries of the next loads' keys.
+  __device__ __forceinline__ void find(const AttendArgs& a, const Work& w, uint32_t base, uint32_t tid) {
+#pragma unroll
+    for (uint32_t i = 0; i < LD; ++i) entry[i] = table_entry(a.b, w.s, min(base + i * RPL + tid / CH, w.hi - 1));
+  }
+
+  // Load i of the keys from `base` on.  A wavefront's rows lie in one page where RPW
+  // divides the block (PAGED): their place is a scalar then.  Behind the end a load
+  // takes rows that are not the sequence's (drop_tail) or the last group's again.
+  __device__ __forceinline__ void fetch(const AttendArgs& a, const Work& w, uint32_t base, uint8_t* __restrict__ to_k,
+                                        uint8_t* __restrict__ to_v, uint32_t tid, uint32_t wv, uint32_t i) {
+    const uint32_t last = w.hi - 1;
+    const uint8_t* const plane = a.b.plane + (uint64_t)w.kv * ROW;
+    const uint8_t* at;
+    if constexpr (PAGED)
+      at = plane + row_bytes_at(a.b, min(base + i * RPL + wv * RPW, last / RPW * RPW), same(entry[i]), &err);
+    else
+      at = plane + (uint64_t)pool_row(a.b, min(base + i * RPL + tid / CH, last), entry[i], &err) * a.b.row;
+    const uint8_t* bt = at + a.b.plane_bytes;
+    if constexpr (PAGED) {  // a scalar and a 32-bit offset, not an address per lane
+      at = reinterpret_cast<const uint8_t*>(wave::uniform(reinterpret_cast<uint64_t>(at)));
+      bt = reinterpret_cast<const uint8_t*>(wave::uniform(reinterpret_cast<uint64_t>(bt)));
+    }
+    asm("" : "+v"(k_off), "+v"(v_off));  // 32-bit offsets as they are: not widened ahead of the loop
+    const uint8_t *const ka = at + k_off, *const va = bt + v_off;
+    to_lds(ka, to_k + (i * NT + wv * 64) * 16);
+    to_lds(va, to_v + (i * NT + wv * 64) * 16);
+  }
+};
+
+// The rows behind the end of the last step's values: zeros, so that weights of 0
+// meet no infinity or NaN there.
+template <typename T>
+__device__ inline void drop_tail(const Work& w, uint8_t* area, uint32_t k0, uint32_t tid) {
+  for (uint32_t i = 0; i < T::LD; ++i)
+    if (k0 + i * T::RPL + tid / T::CH >= w.hi)
+      *reinterpret_cast<u32x4*>(area + (i * T::NT + tid) * 16) = u32x4{0, 0, 0, 0};
+  __syncthreads();
+}
+
+// One step of 64 keys: these taken from the one area, the next ones' loads set out for the other.
+template <typename DT, int D, bool PAGED>
+__device__ __forceinline__ void step(const AttendArgs& a, const Work& w, Tile<D, PAGED>& x,
+                                     const uint8_t* __restrict__ now_k, const uint8_t* __restrict__ now_v,
+                                     uint8_t* __restrict__ then_k, uint8_t* __restrict__ then_v, uint32_t k0,
+                                     uint32_t tid, uint32_t wv) {
+  typedef Tile<D, PAGED> T;
+  constexpr uint32_t NT = T::NT, ROW = T::ROW, LD = T::LD;
+  constexpr int KS = T::KS, DB = T::DB;
+  const uint32_t lane = tid & 63, n = lane & 31, h = lane >> 5;
+  // LDS addresses of a lane's reads
+  const uint32_t kx = D == 128 ? n & 15 : (n >> 1) & 7;
+  const uint32_t vrow = 4 * h + ((lane >> 2) & 3);
+  const uint32_t vx = D == 128 ? (vrow & 3) << 2 : ((vrow >> 1) & 1) << 2;
+  const uint32_t vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), vsub = 8 * (lane & 1);
+  const uint32_t next = min(k0 + STEP, w.hi - 1);  // behind the last step the last key again, for nothing
+  const bool mixed = k0 + STEP > w.open || k0 + STEP > w.hi;
+  if (k0 + STEP > w.open && w.open < w.hi) {
+    for (uint32_t i = 0; i < LD; ++i) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(now_v + (i * NT + tid) * 16);
+      for (int j = 0; j < 4; ++j) x.odd |= odd_pair(DT(), v[j]);
+    }
+  }
+  if (k0 < x.wave_hi) {
+    const uint8_t* const ks = now_k + n * ROW;
+    const uint8_t* const vs = now_v + vrow * ROW + vsub;
+    f32x16 s[2];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const u32x4 kr = *reinterpret_cast<const u32x4*>(ks + kb * 32 * ROW + (((2 * k + h) ^ kx) << 4));
+        s[kb] = mfma_32x32x16(DT(), kr, x.q[k], s[kb]);
+      }
+      // the next step's loads, a few at a time: issued at once they hold the wavefront up
+      if (k % T::BETWEEN == 0) x.fetch(a, w, next, then_k, then_v, tid, wv, k / T::BETWEEN);
+    }
+    uint32_t p[16];
+    if (mixed) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (k0 + 32 * kb + 8 * (i / 4) + 4 * h + i % 4 >= x.limit) s[kb][i] = -INFINITY;
+    }
+    float m = s[0][0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) m = fmaxf(m, s[i / 16][i % 16]);
+    m = a.c * max_over_32(m);
+    if (__any(m > x.top + RISE)) {
+      const float t = fmaxf(x.top, m), keep = __builtin_amdgcn_exp2f(x.top - t);
+      x.top = t;
+      x.sum *= keep;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) x.o[d] *= keep;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float f0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 8][2 * i % 16], a.c, -x.top));
+      const float f1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 8][2 * i % 16 + 1], a.c, -x.top));
+      x.sum += f0 + f1;
+      p[i] = pair_of<DT>(f0, f1);
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        const uint8_t* at = vs + 16 * t * ROW + (((4 * d + vc) ^ vx) << 4);
+        const u32x2 lo = read_tr(at), hi = read_tr(at + 8 * ROW);
+        const u32x4 v = {lo[0], lo[1], hi[0], hi[1]};
+        x.o[d] = mfma_32x32x16(DT(), v, u32x4{p[4 * t], p[4 * t + 1], p[4 * t + 2], p[4 * t + 3]}, x.o[d]);
+      }
+    }
+  }
+  if (k0 >= x.wave_hi) {
+#pragma unroll
+    for (uint32_t i = 0; i < LD; ++i) x.fetch(a, w, next, then_k, then_v, tid, wv, i);
+  }
+}
+
+template <typename DT, int D, bool PAGED>
+__global__ __launch_bounds__(64 * NW, 2) void attend_tile_kernel(AttendArgs a) {
+  typedef Tile<D, PAGED> T;
+  constexpr int KS = T::KS, DB = T::DB;
+  // Arrays of their own, and the loop written out for both: a read of the one area
+  // does not wait for loads into another only where the compiler can tell them apart.
+  __shared__ __align__(256) uint8_t s_k0[T::AREA], s_k1[T::AREA];
+  __shared__ __align__(256) uint8_t s_v0[T::AREA], s_v1[T::AREA];
   const uint32_t tid = threadIdx.x, lane = tid & 63, wv = wave_index();
   const uint32_t n = lane & 31, h = lane >> 5;
   const Work w = work_of(a, blockIdx.x, lane);
   if (!w.some) return;
-  uint32_t err = w.s.error;
-  const uint32_t last = w.hi - 1;
+  T x;
+  x.err = w.s.error;
+  x.odd = false;
+  x.place(a, tid);
 
-  // rows: block qb of the wavefront is rows 32 * (wv * QB + qb) + n
-  u32x4 q[QB][KS];
-  uint32_t limit[QB], wave_hi = 0;
+  if (w.lo < w.hi) {  // the first keys on the way, then the queries
+    x.find(a, w, w.lo, tid);
 #pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    const uint32_t r = 32 * (wv * QB + qb) + n;
-    limit[qb] = min(row_limit(a, w, r), w.hi);
-    const u32x4* src = reinterpret_cast<const u32x4*>(q_row(a, row_at(a, w, min(r, w.rows - 1))) + 16 * h);
-#pragma unroll
-    for (int k = 0; k < KS; ++k) q[qb][k] = q_signed(a, src[2 * k]);
-    wave_hi = max(wave_hi, limit[qb]);
+    for (uint32_t i = 0; i < T::LD; ++i) x.fetch(a, w, w.lo, s_k0, s_v0, tid, wv, i);
+    x.find(a, w, w.lo + STEP, tid);
   }
+  // rows: the wavefront's are 32 * wv + n
+  const uint32_t r = 32 * wv + n;
+  x.limit = min(row_limit(a, w, r), w.hi);
+  const u32x4* src = reinterpret_cast<const u32x4*>(q_row(a, row_at(a, w, min(r, w.rows - 1))) + 16 * h);
 #pragma unroll
-  for (int d = 1; d < 32; d <<= 1) wave_hi = max(wave_hi, (uint32_t)__shfl_xor((int)wave_hi, d));
-  wave_hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)wave_hi);
-  f32x16 o[QB][DB];
-  float top[QB], sum[QB];
+  for (int k = 0; k < KS; ++k) x.q[k] = q_signed(a, src[2 * k]);
+  x.top = NO_TOP;
+  x.sum = 0;
 #pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    top[qb] = NO_TOP;
-    sum[qb] = 0;
+  for (int d = 0; d < DB; ++d)
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+    for (int i = 0; i < 16; ++i) x.o[d][i] = 0;
+  x.wave_hi = x.limit;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[qb][d][i] = 0;
-  }
+  for (int d = 1; d < 32; d <<= 1) x.wave_hi = max(x.wave_hi, (uint32_t)__shfl_xor((int)x.wave_hi, d));
+  x.wave_hi = same(x.wave_hi);
 
-  bool odd = false;  // a value that rows see in part is infinite or NaN
   if (w.lo < w.hi) {
-    // this thread's part of a load: row and permuted chunk
-    const uint32_t lr = tid / CH, lc = tid % CH;
-    const uint32_t swk = D == 128 ? lr & 15 : (lr >> 1) & 7;
-    const uint32_t swv = D == 128 ? (lr & 3) << 2 : ((lr >> 1) & 1) << 2;
-    const uint8_t* const kp = a.b.plane + (uint64_t)w.kv * ROW + 16 * (lc ^ swk);
-    const uint8_t* const vp = a.b.plane + a.b.plane_bytes + (uint64_t)w.kv * ROW + 16 * (lc ^ swv);
-    const auto key_of = [&](uint32_t base, uint32_t i) { return min(base + i * RPL + lr, last); };
-    uint32_t entry[LD];
-    const auto find = [&](uint32_t base) {
-#pragma unroll
-      for (uint32_t i = 0; i < LD; ++i) entry[i] = table_entry(a.b, w.s, key_of(base, i));
-    };
-    const auto fetch = [&](uint32_t base, uint32_t buf) {
-#pragma unroll
-      for (uint32_t i = 0; i < LD; ++i) {
-        const uint64_t at = (uint64_t)pool_row(a.b, key_of(base, i), entry[i], &err) * a.b.row;
-        to_lds(kp + at, &s_k[buf][(i * NT + wv * 64) * 16]);
-        to_lds(vp + at, &s_v[buf][(i * NT + wv * 64) * 16]);
-      }
-    };
-    // LDS addresses of a lane's reads
-    const uint32_t kx = D == 128 ? n & 15 : (n >> 1) & 7;
-    const uint32_t vrow = 4 * h + ((lane >> 2) & 3);
-    const uint32_t vx = D == 128 ? (vrow & 3) << 2 : ((vrow >> 1) & 1) << 2;
-    const uint32_t vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), vsub = 8 * (lane & 1);
-
-    find(w.lo);
-    fetch(w.lo, 0);
-    find(min(w.lo + STEP, last));
     wait_loads();
     __syncthreads();
-    uint32_t buf = 0;
-    for (uint32_t k0 = w.lo; k0 < w.hi; k0 += STEP, buf ^= 1) {
-      if (k0 + STEP < w.hi) {
-        fetch(k0 + STEP, buf ^ 1);
-        find(min(k0 + 2 * STEP, last));
-      }
-      const bool mixed = k0 + STEP > w.open || k0 + STEP > w.hi;
-      if (k0 + STEP > w.open && w.open < w.hi) {
-        for (uint32_t i = 0; i < LD; ++i) {
-          const u32x4 x = *reinterpret_cast<const u32x4*>(&s_v[buf][(i * NT + tid) * 16]);
-          for (int j = 0; j < 4; ++j) odd |= odd_pair(DT(), x[j]);
-        }
-      }
-      if (k0 < wave_hi) {
-        const uint8_t* const ks = s_k[buf] + n * ROW;
-        const uint8_t* const vs = s_v[buf] + vrow * ROW + vsub;
-        f32x16 s[QB][2];
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[qb][kb][i] = 0;
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb) {
-            const u32x4 kr = *reinterpret_cast<const u32x4*>(ks + kb * 32 * ROW + (((2 * k + h) ^ kx) << 4));
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb) s[qb][kb] = mfma_32x32x16(DT(), kr, q[qb][k], s[qb][kb]);
-          }
-        }
-        uint32_t p[QB][16];
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-          if (mixed) {
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-              for (int i = 0; i < 16; ++i)
-                if (k0 + 32 * kb + 8 * (i / 4) + 4 * h + i % 4 >= limit[qb]) s[qb][kb][i] = -INFINITY;
-          }
-          float m = s[qb][0][0];
-#pragma unroll
-          for (int i = 1; i < 32; ++i) m = fmaxf(m, s[qb][i / 16][i % 16]);
-          m = a.c * max_over_32(m);
-          if (__any(m > top[qb] + RISE)) {
-            const float t = fmaxf(top[qb], m), keep = __builtin_amdgcn_exp2f(top[qb] - t);
-            top[qb] = t;
-            sum[qb] *= keep;
-#pragma unroll
-            for (int d = 0; d < DB; ++d) o[qb][d] *= keep;
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float f0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qb][i / 8][2 * i % 16], a.c, -top[qb]));
-            const float f1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qb][i / 8][2 * i % 16 + 1], a.c, -top[qb]));
-            sum[qb] += f0 + f1;
-            p[qb][i] = pair_of<DT>(f0, f1);
-          }
-        }
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-#pragma unroll
-          for (int d = 0; d < DB; ++d) {
-            const uint8_t* at = vs + 16 * t * ROW + (((4 * d + vc) ^ vx) << 4);
-            const u32x2 lo = read_tr(at), hi = read_tr(at + 8 * ROW);
-            const u32x4 v = {lo[0], lo[1], hi[0], hi[1]};
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb)
-              o[qb][d] = mfma_32x32x16(DT(), v, u32x4{p[qb][4 * t], p[qb][4 * t + 1], p[qb][4 * t + 2], p[qb][4 * t + 3]},
-                                       o[qb][d]);
-          }
-        }
-      }
+    const auto turn = [&](uint8_t* now_k, uint8_t* now_v, uint8_t* then_k, uint8_t* then_v, uint32_t k0) {
+      if (PAGED && k0 + STEP > w.hi) drop_tail<T>(w, now_v, k0, tid);
+      step<DT>(a, w, x, now_k, now_v, then_k, then_v, k0, tid, wv);
+      x.find(a, w, k0 + 2 * STEP, tid);
       wait_loads();
       __syncthreads();
+    };
+    for (uint32_t k0 = w.lo;;) {
+      turn(s_k0, s_v0, s_k1, s_v1, k0);
+      if ((k0 += STEP) >= w.hi) break;
+      turn(s_k1, s_v1, s_k0, s_v0, k0);
+      if ((k0 += STEP) >= w.hi) break;
     }
   }
-  if (__any(err != 0)) report(a.b, err);
-  if (w.open < w.hi && __syncthreads_or(odd)) {
+  if (__any(x.err != 0)) report(a.b, x.err);
+  if (w.open < w.hi && __syncthreads_or(x.odd)) {
     rows_one_by_one<DT, D, D>(a, w, wv, NW, lane);
     return;
   }
 
+  const float l = sum_over_32(x.sum);
+  if (r >= w.rows) return;
+  if (w.per_tile > 1) {
+    const uint64_t at = ((uint64_t)w.item * a.kv_heads + w.kv) * a.tile_rows + r;
 #pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    const float l = sum_over_32(sum[qb]);
-    const uint32_t r = 32 * (wv * QB + qb) + n;
-    if (r >= w.rows) continue;
-    if (w.per_tile > 1) {
-      const uint64_t at = ((uint64_t)w.item * a.kv_heads + w.kv) * a.tile_rows + r;
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int d = 0; d < DB; ++d)
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(a.part + at * D + 32 * d + 8 * i + 4 * h) =
+            f32x4{x.o[d][4 * i], x.o[d][4 * i + 1], x.o[d][4 * i + 2], x.o[d][4 * i + 3]};
+    if (h == 0) a.part_ml[at] = float2{x.top, l};
+  } else {
+    const RowAt at = row_at(a, w, r);
+    const bool none = row_limit(a, w, r) == 0;
+    const float inv = 1.f / l;
+    uint8_t* out = a.out.data + at.t * a.out.token + at.h * a.out.head;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<f32x4*>(a.part + at * D + 32 * d + 8 * i + 4 * h) =
-              f32x4{o[qb][d][4 * i], o[qb][d][4 * i + 1], o[qb][d][4 * i + 2], o[qb][d][4 * i + 3]};
-      if (h == 0) a.part_ml[at] = float2{top[qb], l};
-    } else {
-      const RowAt at = row_at(a, w, r);
-      const bool none = row_limit(a, w, r) == 0;
-      const float inv = 1.f / l;
-      uint8_t* out = a.out.data + at.t * a.out.token + at.h * a.out.head;
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const u32x2 y = {pair_of<DT>(o[qb][d][4 * i] * inv, o[qb][d][4 * i + 1] * inv),
-                           pair_of<DT>(o[qb][d][4 * i + 2] * inv, o[qb][d][4 * i + 3] * inv)};
-          *reinterpret_cast<u32x2*>(out + 2 * (32 * d + 8 * i + 4 * h)) = none ? u32x2{0, 0} : y;
-        }
-      if (h == 0) store_lse(a, at, top[qb], l, none);
-    }
+      for (int i = 0; i < 4; ++i) {
+        const u32x2 y = {pair_of<DT>(x.o[d][4 * i] * inv, x.o[d][4 * i + 1] * inv),
+                         pair_of<DT>(x.o[d][4 * i + 2] * inv, x.o[d][4 * i + 3] * inv)};
+        *reinterpret_cast<u32x2*>(out + 2 * (32 * d + 8 * i + 4 * h)) = none ? u32x2{0, 0} : y;
+      }
+    if (h == 0) store_lse(a, at, x.top, l, none);
   }
 }
 
 template <typename DT, int D>
 void launch(const AttendArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((attend_tile_kernel<DT, D, 4, 1>), dim3(a.items * a.kv_heads), dim3(256), 0, s, a);
+  const dim3 grid(a.items * a.kv_heads), block(64 * NW);
+  if (a.b.bt % Tile<D, true>::RPW == 0) hipLaunchKernelGGL((attend_tile_kernel<DT, D, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((attend_tile_kernel<DT, D, false>), grid, block, 0, s, a);
 }
 
 }  // namespace
