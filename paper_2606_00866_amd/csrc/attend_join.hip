@@ -27,6 +27,7 @@ __global__ __launch_bounds__(64 * NW) void attend_join_kernel(AttendArgs a) {
   const uint32_t kv = h / a.group, x = (t - t0) * a.group + (h - kv * a.group);
   const uint32_t tiles = (n * a.group + a.tile_rows - 1) / a.tile_rows, tile = x / a.tile_rows;
   const uint64_t item = it.first + (uint64_t)(tiles - 1 - tile) * it.per_tile;
+  if (item + it.per_tile > a.items) return;  // sequences that overlap: more items than tokens give, which were not run
   const uint64_t at0 = (item * a.kv_heads + kv) * a.tile_rows + (x - tile * a.tile_rows);
   const uint64_t step = (uint64_t)a.kv_heads * a.tile_rows;
   const uint32_t runs = it.per_tile;

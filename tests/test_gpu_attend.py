@@ -314,3 +314,21 @@ def test_device_refusals(n, planes):
     inst.seq_off = np.array([0, 3 * n, 2 * n])  # decreasing
     e, out, _ = bits(inst)
     assert e == M.MORI_DEV_BAD_TOKENS
+
+
+@pytest.mark.parametrize("planes", [1, 2])
+def test_overlapping_sequences_stay_inside_the_workspace(planes):
+    """Offsets that name tokens twice give more items than the workspace is for:
+    the fault is reported, what is written stays in bounds."""
+    from paper_2606_00866_amd import attention as A
+    dim, H = (576, 16) if planes == 1 else (128, 8)
+    inst = R.instance(25, [40] * 9, [3000] * 9, kv=1, dim=dim, planes=planes)
+    inst.seq_off = np.array([0, 40, 0, 40, 0, 40, 0, 40, 0, 40])
+    b = R.batch(inst, tokens=40)
+    q = torch.randn(40, H, dim).to(BF16).cuda()
+    ws = A.kv_attend_workspace(inst.geom, b, q)
+    guarded = torch.full((ws.numel() + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    A.kv_attend(inst.pool.cuda(), inst.geom, 1, b, q, workspace=guarded[:ws.numel()])
+    torch.cuda.synchronize()
+    assert int(b.error.item()) == M.MORI_DEV_BAD_TOKENS
+    assert (guarded[ws.numel():] == 0x5A).all()
