@@ -11,7 +11,8 @@
 // batch on the device:
 //     c = max(least, ceil(sum over tiles of their units / slots)),
 // so that a batch gives about `slots` items however its lengths are spread, and
-// at most slots + tiles.  No scheduling pass precedes the kernel: every
+// at most slots + tiles.  A kernel whose workgroup takes a whole CU runs them in
+// rounds of `round` items, and there a c is taken that fills one or two rounds.  No scheduling pass precedes the kernel: every
 // wavefront finds its item from the lengths by a scan over the sequences.
 // Tiles of one run write their rows; the others leave partial sums (unnormalised
 // rows, their maxima and sums) that a second kernel joins in a fixed order.
@@ -41,6 +42,7 @@ struct AttendArgs {
   uint32_t tile_rows;  // rows of a tile
   uint32_t unit;       // keys of a unit
   uint32_t slots, least;
+  uint32_t round;      // items that run at a time, where that decides the run length; else 0
   uint32_t splits;     // 0: every tile is one run
   uint32_t items;      // bound on the number of items (grid and workspace)
   float* part;         // [items * kv_heads][tile_rows][value]
@@ -72,6 +74,33 @@ struct Item {
   bool bad;            // a sequence of this lane has no usable token range
 };
 
+// Among c and the least run lengths (within a sixteenth) whose items fit one round
+// and two, the one that takes the least time.  In units: each round its run and an
+// item's fixed cost (queries, first keys), about 3, and for every 64 items of split
+// tiles one more to write and join 256 KiB of partial sums each.  No choice is below
+// c, so the bound on the items stands.
+__device__ inline uint32_t run_of_rounds(const AttendArgs& a, const Share& own, uint64_t total, uint32_t c) {
+  const uint32_t tiles = wave::sum(own.tiles);
+  const auto items = [&](uint32_t run) { return wave::sum(own.tiles * ((own.units + run - 1) / run)); };
+  const auto cost = [&](uint32_t run) {
+    const uint32_t n = items(run);
+    return (uint64_t)((n + a.round - 1) / a.round) * (run + 3) + (n > tiles ? n / 64 : 0);
+  };
+  uint32_t best = c;
+  uint64_t least = cost(c);
+  for (uint32_t fit = a.round; fit <= 2 * a.round; fit += a.round) {
+    if (tiles > fit) continue;
+    uint32_t run = max(c, (uint32_t)((total + fit - 1) / fit));
+    while (items(run) > fit) run += 1 + run / 16;  // ends: `tiles` items are left where run passes the longest
+    const uint64_t x = cost(run);
+    if (x < least) {
+      least = x;
+      best = run;
+    }
+  }
+  return best;
+}
+
 // The sequence that `want(first item, number of items, b)` picks, the same for
 // the whole wavefront (all of whose lanes are active).
 template <typename F>
@@ -89,6 +118,7 @@ __device__ inline Item find_item(const AttendArgs& a, uint32_t lane, F want) {
     }
     total = wave::sum(total);
     it.run_units = (uint32_t)max((uint64_t)a.least, (total + a.slots - 1) / a.slots);
+    if (a.round && k == 1) it.run_units = run_of_rounds(a, own, total, it.run_units);
   }
   const auto count = [&](const Share& s) { return s.tiles * ((s.units + it.run_units - 1) / it.run_units); };
   uint32_t mine = count(own);

@@ -274,9 +274,11 @@ __global__ __launch_bounds__(RG == 8 ? 512 : 256, RG == 4 ? 2 : 1) void attend_l
 // elements for all 32 rows (the halves are added through LDS), of the values half
 // of the 512.  A wavefront's own 16 rows are its block 0, its partner's block 1; it
 // finishes the scores of its own and hands over their weights.
-//   barrier - scores of half the elements - other block's half to LDS - barrier -
-//   add, weights, to LDS - barrier - values
-// Keys are staged in three areas: two steps' loads are under way.
+//   scores of half the elements - other block's half to LDS - barrier 1 - earlier loads
+//   have arrived, new ones set out - add, weights, to LDS - barrier 2 - values
+// Two barriers a step are enough: what is overwritten behind a barrier was last read
+// before it (halves before barrier 2, weights and keys before barrier 1 of the next
+// step).  Keys are staged in three areas: two steps' loads are under way.
 namespace wide {
 
 constexpr int NW = 8, AREAS = 3, LOADS = 5;
@@ -286,9 +288,6 @@ constexpr int KS = DK / 64, DB = DV / 32;  // steps and value blocks of a half
 // Barrier for data in LDS that wavefronts wrote themselves (loads into LDS may be
 // under way; those are waited for by count).
 __device__ inline void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-// All but the newest step's loads have arrived.
-__device__ inline void wait_step() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(LOADS) : "memory"); }
-
 // Stores to LDS that the compiler does not set behind the loads into LDS under way
 // (it orders any store after all of them); barrier() waits for these.
 template <typename T>
@@ -312,15 +311,19 @@ __device__ inline uint32_t chunk_of(uint32_t k, uint32_t h, uint32_t g) {
   return k < 8 ? 8 * (4 * (k >> 2) + g) + 4 * h + (k & 3) : 64 + 4 * h + g;
 }
 
-// A step's loads: five by every wavefront, so that they can be waited for by count
-// (36 would do: the last four bring rows 0 to 3 again).
-__device__ __forceinline__ void fetch(const AttendArgs& a, uint8_t* __restrict__ to, uint32_t row, uint32_t wv,
-                                      uint32_t lane) {
+// A step's loads (the last four of the 40 bring rows 0 to 3 again).  They have no
+// result in registers.  Written out, because the compiler keeps the registers of such
+// a load's address until it is done, and here they are wanted at once; wait_loads()
+// waits for them.
+__device__ __forceinline__ void fetch(const AttendArgs& a, uint8_t* to, uint32_t row, uint32_t wv, uint32_t lane) {
 #pragma unroll
   for (uint32_t i = 0; i < LOADS; ++i) {
     const uint32_t c = (i * NW + wv) * 64 + lane, r = c / CH, at = c - r * CH;
     const uint32_t p = (uint32_t)__shfl((int)row, (int)r);
-    to_lds(a.b.plane + (uint64_t)p * ROW + ((at ^ swizzle(r)) << 4), to + (i * NW + wv) * 1024);
+    const uint8_t* const src = a.b.plane + (uint64_t)p * ROW + ((at ^ swizzle(r)) << 4);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src),
+                 "s"(same(lds_address(to + (i * NW + wv) * 1024)))
+                 : "memory");  // m0 is set before each use, here as by the compiler
   }
 }
 
@@ -338,18 +341,20 @@ struct Acc {
 
 template <typename DT>
 __device__ __forceinline__ void step(const AttendArgs& a, const Work& w, const uint8_t* __restrict__ now,
-                                     uint8_t* __restrict__ then, uint32_t row, Shared& x,
+                                     uint8_t* __restrict__ then, Shared& x,
                                      const u32x4 (&q)[KS][2], Acc& acc, uint32_t base, uint32_t limit, uint32_t wv,
-                                     uint32_t lane) {
+                                     uint32_t lane, uint32_t* err) {
   asm volatile("" : "+v"(lane));  // what follows from it is computed at every step: there is no room to keep it
-  fetch(a, then, row, wv, lane);
+  // the keys after next: their table entry is here when the scores are
+  const uint32_t ahead = min(base + 2 * STEP + (lane & (STEP - 1)), w.hi - 1);
+  const uint32_t entry = table_entry(a.b, w.s, ahead);
   const uint32_t n = lane & 15, g = lane >> 4, h = wv & 1;
   f32x4 s[2][2];
 #pragma unroll
   for (int b = 0; b < 2; ++b) s[b][0] = s[b][1] = f32x4{0, 0, 0, 0};
   const uint32_t kx = swizzle(n);  // the same for key n + 16
   const uint8_t* const ks = now + n * ROW;
-  products<2 * KS, 4>(
+  products<2 * KS, 3>(
       [&](int i) {
         return *reinterpret_cast<const u32x4*>(ks + ((chunk_of(i >> 1, h, g) ^ kx) << 4) + 16 * (i & 1) * ROW);
       },
@@ -362,7 +367,9 @@ __device__ __forceinline__ void step(const AttendArgs& a, const Work& w, const u
   asm volatile("s_nop 15\n\ts_nop 3" ::: "memory");
   put(&x.part[wv][0][lane], s[1][0]);
   put(&x.part[wv][1][lane], s[1][1]);
-  barrier();
+  barrier();  // every wavefront is through with the step before: its area is free
+  wait_loads();
+  fetch(a, then, pool_row(a.b, ahead, entry, err), wv, lane);
 #pragma unroll
   for (int i = 0; i < 2; ++i) s[0][i] += x.part[wv ^ 1][i][lane];
   if (base + STEP > w.open || base + STEP > w.hi) {
@@ -396,7 +403,6 @@ __device__ __forceinline__ void step(const AttendArgs& a, const Work& w, const u
   }
   put(&x.weight[wv][lane], p[0]);
   put(&x.keep[wv][n], keep);
-  wait_step();
   barrier();
   p[1] = x.weight[wv ^ 1][lane];
   const float keep1 = x.keep[wv ^ 1][n];
@@ -427,8 +433,10 @@ template <typename DT>
 __global__ __launch_bounds__(64 * NW, 1) void attend_latent_wide_kernel(AttendArgs a) {
   __shared__ __align__(256) uint8_t key[AREAS * AREA];  // apart from the rest: loads into it run beside reads of that
   __shared__ Shared x;
-  const uint32_t lane = threadIdx.x & 63, wv = wave_index();
-  const uint32_t n = lane & 15, g = lane >> 4, h = wv & 1;
+  uint32_t lane = threadIdx.x & 63;
+  const uint32_t wv = wave_index();
+  uint32_t n = lane & 15, g = lane >> 4;
+  const uint32_t h = wv & 1;
   const Work w = work_of(a, blockIdx.x, lane);
   if (!w.some) return;
   uint32_t err = w.s.error;
@@ -437,14 +445,11 @@ __global__ __launch_bounds__(64 * NW, 1) void attend_latent_wide_kernel(AttendAr
 
   const auto key_of = [&](uint32_t base) { return min(base + (lane & (STEP - 1)), last); };
   const auto pool_at = [&](uint32_t base, uint32_t entry) { return pool_row(a.b, key_of(base), entry, &err); };
-  uint32_t entry = 0;
   if (w.lo < w.hi) {  // the first keys on the way, then the queries
-    // loads past the end take the last key again: every step counts the same loads
+    // (past the end: the last key again)
     fetch(a, key, pool_at(w.lo, table_entry(a.b, w.s, key_of(w.lo))), wv, lane);
     const uint32_t second = min(w.lo + STEP, last);
-    const uint32_t row1 = pool_at(second, table_entry(a.b, w.s, key_of(second)));
-    entry = table_entry(a.b, w.s, key_of(min(w.lo + 2 * STEP, last)));
-    fetch(a, key + AREA, row1, wv, lane);
+    fetch(a, key + AREA, pool_at(second, table_entry(a.b, w.s, key_of(second))), wv, lane);
   }
   u32x4 q[KS][2];
   Acc acc;
@@ -462,17 +467,13 @@ __global__ __launch_bounds__(64 * NW, 1) void attend_latent_wide_kernel(AttendAr
   }
 
   if (w.lo < w.hi) {
-    wait_step();
+    wait_loads();
     barrier();
     uint32_t now = 0, then = 2 * AREA;
     for (uint32_t base = w.lo; base < w.hi; base += STEP) {
-      const uint32_t ahead = min(base + 2 * STEP, last);
-      const uint32_t row = pool_at(ahead, entry);
-      entry = table_entry(a.b, w.s, key_of(min(base + 3 * STEP, last)));
-      step<DT>(a, w, key + now, key + then, row, x, q, acc, base, limit, wv, lane);
+      step<DT>(a, w, key + now, key + then, x, q, acc, base, limit, wv, lane, &err);
       now = now == 2 * AREA ? 0 : now + AREA;
       then = then == 2 * AREA ? 0 : then + AREA;
-      barrier();
     }
     wait_loads();
   }
@@ -482,6 +483,10 @@ __global__ __launch_bounds__(64 * NW, 1) void attend_latent_wide_kernel(AttendAr
     return;
   }
 
+  // the rows' places are computed again: there was no room to keep them over the steps
+  asm volatile("" : "+v"(lane));
+  n = lane & 15;
+  g = lane >> 4;
   acc.sum = sum_over_16(sum_over_32(acc.sum));
   if (g == 0) {
     x.top[wv][n] = acc.top;
