@@ -20,6 +20,9 @@
  *                        allocated for them (CPU -> GPU, Sec. 4.1: a CPU-tier
  *                        program resumes over PCIe).
  *
+ * Beside them the two calls a model makes on the pool's pages in every layer:
+ * mori_kv_append writes new tokens' keys and values, mori_kv_attend reads them.
+ *
  * Conventions
  *   - Every call returns an int: MORI_OK (0) or a negative MORI_E* code.
  *     Nothing throws across the ABI.  Errors found on the host are reported
@@ -36,7 +39,8 @@
  *     direction has read its address table.
  *   - Threads: a context is driven by one host thread at a time (its calls
  *     are not synchronised against each other); distinct contexts share no
- *     state, and mori_evict_order and mori_replica_admit keep none.
+ *     state, and mori_evict_order, mori_replica_admit, mori_kv_append and
+ *     mori_kv_attend keep none.
  *   - Ownership: the caller owns the pool, the program arrays, the host
  *     buffers and the streams.  The context owns its device scratch, a small
  *     pinned mirror of the plan and, for copy-engine swaps, device staging

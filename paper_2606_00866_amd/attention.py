@@ -21,7 +21,7 @@ from .tiering import MoriError, PoolGeometry, check
 
 DTYPES = {torch.float16: M.MORI_DT_F16, torch.bfloat16: M.MORI_DT_BF16}
 STYLES = {"half": M.MORI_ROPE_HALF, "pairs": M.MORI_ROPE_PAIRS}
-LATENT_DIM, LATENT_ROPE = 512, 64  # the latent rows kv_attend reads
+LATENT_ROPE = 64  # rotated elements behind the latent part of a latent row
 
 
 def _need(ok: bool, what: str) -> None:

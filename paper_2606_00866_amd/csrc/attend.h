@@ -155,7 +155,7 @@ struct Work {
   uint32_t lo, hi;         // keys; lo >= hi: none
   uint32_t open;           // keys below this are allowed to every row of the tile
   uint32_t per_tile;
-  bool first_run, some;
+  bool some;
 };
 
 // A value that is the same in every lane, in a scalar register.
@@ -185,7 +185,6 @@ __device__ inline Work work_of(const AttendArgs& a, uint32_t block, uint32_t lan
   const uint32_t tiles = (w.s.n * a.group + a.tile_rows - 1) / a.tile_rows;
   const uint32_t k = w.item - it.first, back = k / it.per_tile, run = k - back * it.per_tile;
   w.per_tile = it.per_tile;
-  w.first_run = run == 0;
   // the last tile first: with a causal mask it has the most keys
   w.row0 = same((tiles - 1 - back) * a.tile_rows);
   w.rows = min(a.tile_rows, w.s.n * a.group - w.row0);

@@ -5,16 +5,16 @@
 // byte at H = 128: bytes bound a few heads, the matrix rate many.  So a key is
 // staged in LDS once, as key and value, for as many rows as there are.
 //
-// A wavefront has 16 rows: 128 registers hold their sums (16 x 512), 72 their
-// queries.  RG wavefronts share their keys and KG groups take different keys, 32
-// (RG 8: 64) at a time, joined through LDS at the end:
+// Up to 64 rows a wavefront has 16: 128 registers hold their sums (16 x 512), 72
+// their queries.  RG of the four wavefronts share their keys and the KG groups take
+// different keys, 32 at a time, joined through LDS at the end:
 //   RG 1  up to 16 rows, four groups: each wavefront stages and reads its own
 //         keys without barriers; four staging areas of 36 KiB, filled while the
 //         other wavefronts compute, keep enough loads in flight;
 //   RG 2  up to 32 rows, two groups with two areas each: the next keys load behind
 //         this step's products;
-//   RG 4  up to 64 rows, one group, two workgroups a CU;
-//   RG 8  up to 128 rows, one group of eight wavefronts.
+//   RG 4  up to 64 rows, one group, two workgroups a CU.
+// More rows than that have a kernel of their own, below.
 //   scores   S^T = K Q^T, 16x16x32;  values  O^T += V^T P^T, the weights in the
 //            order in which they leave the score product (see attend_step.hip).
 // A row is 72 chunks of 16 B, permuted within each 8 by a function f of the row:
@@ -100,12 +100,12 @@ __device__ __forceinline__ void take(const AttendArgs& a, const Work& w, const u
       [&](int d, u32x4 f) { acc.o[d] = mfma_16x16x32(DT(), f, pt, acc.o[d]); });
 }
 
-// This group's loads of SUB steps into `to`: whole pool rows, chunks permuted.
+// This group's loads of a step into `to`: whole pool rows, chunks permuted.
 // Load i of a thread is chunk (i * RG + rg) * 64 + lane.
-template <int RG, int SUB>
+template <int RG>
 __device__ __forceinline__ void fetch(const AttendArgs& a, uint8_t* __restrict__ to, uint32_t row, uint32_t rg,
                                       uint32_t lane) {
-  constexpr uint32_t LOADS = 36 * SUB / RG;
+  constexpr uint32_t LOADS = 36 / RG;
   // recomputed at every step: nine places kept over the products cost more registers than there are
   asm volatile("" : "+v"(lane));
   uint32_t place[9];
@@ -125,21 +125,18 @@ __device__ __forceinline__ void fetch(const AttendArgs& a, uint8_t* __restrict__
 
 // A group's step: the next keys set out for one area, these taken from the other.
 // (The areas' being apart is what lets the reads run beside the loads.)
-template <typename DT, int RG, int SUB>
+template <typename DT, int RG>
 __device__ __forceinline__ void step(const AttendArgs& a, const Work& w, const uint8_t* __restrict__ now,
                                      uint8_t* __restrict__ then, bool more, uint32_t row, uint32_t rg,
                                      const u32x4 (&q)[KS], Acc& acc, uint32_t base, uint32_t limit, uint32_t lane) {
-  if (more) fetch<RG, SUB>(a, then, row, rg, lane);
-#pragma unroll 1
-  for (uint32_t i = 0; i < SUB; ++i)
-    if (base + STEP * i < w.hi) take<DT>(a, w, now + i * STEP * ROW, q, acc, base + STEP * i, limit, lane);
+  if (more) fetch<RG>(a, then, row, rg, lane);
+  if (base < w.hi) take<DT>(a, w, now, q, acc, base, limit, lane);
 }
 
 template <typename DT, int RG>
-__global__ __launch_bounds__(RG == 8 ? 512 : 256, RG == 4 ? 2 : 1) void attend_latent_kernel(AttendArgs a) {
-  constexpr int NW = RG == 8 ? 8 : 4, KG = NW / RG, SUB = RG == 8 ? 2 : 1;
-  constexpr uint32_t KEYS = STEP * SUB;  // a group's keys at a time
-  constexpr uint32_t AREA = KEYS * ROW;
+__global__ __launch_bounds__(256, RG == 4 ? 2 : 1) void attend_latent_kernel(AttendArgs a) {
+  constexpr int NW = 4, KG = NW / RG;
+  constexpr uint32_t AREA = STEP * ROW;
   constexpr uint32_t AREAS = RG == 1 ? 1 : 2;  // of each group
   __shared__ __align__(256) uint8_t s_a[AREAS * KG * AREA];
   __shared__ float s_top[KG][RG * 16], s_sum[KG][RG * 16];
@@ -167,15 +164,15 @@ __global__ __launch_bounds__(RG == 8 ? 512 : 256, RG == 4 ? 2 : 1) void attend_l
   for (int d = 0; d < DB; ++d) acc.o[d] = f32x4{0, 0, 0, 0};
 
   if (w.lo < w.hi) {
-    constexpr uint32_t WG_KEYS = KEYS * KG;
-    const auto key_of = [&](uint32_t base) { return min(base + (lane & (KEYS - 1)), last); };
+    constexpr uint32_t WG_KEYS = STEP * KG;
+    const auto key_of = [&](uint32_t base) { return min(base + (lane & (STEP - 1)), last); };
     const auto pool_at = [&](uint32_t base, uint32_t entry) { return pool_row(a.b, key_of(base), entry, &err); };
-    uint32_t base = w.lo + kg * KEYS;
+    uint32_t base = w.lo + kg * STEP;
     uint8_t* const mine = s_a + kg * (AREAS * AREA);
     uint32_t entry = table_entry(a.b, w.s, key_of(base));
     if constexpr (RG == 1) {
       if (base < w.hi) {
-        fetch<RG, SUB>(a, mine, pool_at(base, entry), rg, lane);
+        fetch<RG>(a, mine, pool_at(base, entry), rg, lane);
         entry = table_entry(a.b, w.s, key_of(base + WG_KEYS));
         for (;;) {
           wait_loads();
@@ -183,13 +180,13 @@ __global__ __launch_bounds__(RG == 8 ? 512 : 256, RG == 4 ? 2 : 1) void attend_l
           base += WG_KEYS;
           if (base >= w.hi) break;
           wait_loads();  // the area has been read
-          fetch<RG, SUB>(a, mine, pool_at(base, entry), rg, lane);
+          fetch<RG>(a, mine, pool_at(base, entry), rg, lane);
           entry = table_entry(a.b, w.s, key_of(base + WG_KEYS));
         }
       }
     } else {
       // every group takes the workgroup's number of steps (its keys past the end are masked)
-      fetch<RG, SUB>(a, mine, pool_at(base, entry), rg, lane);
+      fetch<RG>(a, mine, pool_at(base, entry), rg, lane);
       entry = table_entry(a.b, w.s, key_of(base + WG_KEYS));
       wait_loads();
       __syncthreads();
@@ -197,7 +194,7 @@ __global__ __launch_bounds__(RG == 8 ? 512 : 256, RG == 4 ? 2 : 1) void attend_l
       for (uint32_t first = w.lo; first < w.hi; first += WG_KEYS, now ^= AREA) {
         const bool more = first + WG_KEYS < w.hi;
         const uint32_t row = more ? pool_at(base + WG_KEYS, entry) : 0;
-        step<DT, RG, SUB>(a, w, mine + now, mine + (now ^ AREA), more, row, rg, q, acc, base, limit, lane);
+        step<DT, RG>(a, w, mine + now, mine + (now ^ AREA), more, row, rg, q, acc, base, limit, lane);
         if (more) entry = table_entry(a.b, w.s, key_of(base + 2 * WG_KEYS));
         base += WG_KEYS;
         wait_loads();

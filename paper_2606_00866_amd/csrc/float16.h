@@ -13,13 +13,11 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 struct F16 {
   typedef _Float16 scalar;
   typedef _Float16 x8 __attribute__((ext_vector_type(8)));
-  typedef _Float16 x4 __attribute__((ext_vector_type(4)));
   typedef _Float16 x2 __attribute__((ext_vector_type(2)));
 };
 struct BF16 {
   typedef __bf16 scalar;
   typedef __bf16 x8 __attribute__((ext_vector_type(8)));
-  typedef __bf16 x4 __attribute__((ext_vector_type(4)));
   typedef __bf16 x2 __attribute__((ext_vector_type(2)));
 };
 
