@@ -1,6 +1,8 @@
 // Joins the partial sums of tiles whose keys were split into runs:
 //   out = sum_i 2^(top_i - top) part_i / sum_i 2^(top_i - top) sum_i, in run order.
-// A token whose tile was one run has nothing to join.
+// A token whose tile was one run has nothing to join.  Bound by reading the partial
+// sums (2 KiB a row and run where rows are latent): 27-50 us where 480 items of 128
+// latent rows are joined, 4 us for a decode step of one long sequence.
 #include "attend.h"
 
 namespace mori {
