@@ -12,8 +12,9 @@
 //     c = max(least, ceil(sum over tiles of their units / slots)),
 // so that a batch gives about `slots` items however its lengths are spread, and
 // at most slots + tiles.  A kernel whose workgroup takes a whole CU runs them in
-// rounds of `round` items, and there a c is taken that fills one or two rounds.  No scheduling pass precedes the kernel: every
-// wavefront finds its item from the lengths by a scan over the sequences.
+// rounds of `round` items; there a c is taken that fills one or two rounds.  No
+// scheduling pass precedes the kernel: every wavefront finds its item from the
+// lengths by a scan over the sequences.
 // Tiles of one run write their rows; the others leave partial sums (unnormalised
 // rows, their maxima and sums) that a second kernel joins in a fixed order.
 //

@@ -65,10 +65,11 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
   // Items that fill the chip a few times over (measured on decode steps, chunks and mixed
   // batches: half of these leave 2-10% to uneven items, twice as many cost that in
   // partial sums and joins); 128 latent rows are 256 KiB of partial sums an item.
-  const uint32_t full = (p.latent ? (a.tile_rows == 128 ? 512 : 1024) : 1536);
+  const uint32_t full = p.latent ? (a.tile_rows == 128 ? 512 : 1024) : 1536;
   a.slots = (full + a.kv_heads - 1) / a.kv_heads;
-  a.least = (p.step ? 2 : 4);
+  a.least = p.step ? 2 : 4;
   a.round = p.latent && a.tile_rows == 128 ? 256 : 0;  // one workgroup a CU
+  // nothing to split in short contexts, no need where the tiles alone are that many items
   a.splits = a.b.max_kv > a.least * a.unit && tiles * a.kv_heads < 2048;
   // runs have `least` units or more, so short contexts give fewer items than slots
   const uint64_t runs = tiles * (((uint64_t)a.b.max_kv + a.unit - 1) / a.unit) / a.least;
