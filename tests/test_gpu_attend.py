@@ -28,11 +28,12 @@ def run(inst, H, seed=0, q=None, value_dim=None, scale=None, b=None, **kw):
     return q, scale, value_dim, out, lse, b
 
 
-def check(inst, H, rows=None, **kw):
+def check(inst, H, rows=None, heads=slice(None), **kw):
+    """heads: those that are compared (only where inst has one key head)."""
     q, scale, vd, out, lse, b = run(inst, H, **kw)
     b.check()
-    want, want_lse, mean, delta, count, top = R.attend(inst, q, scale, vd)
-    got, got_lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    want, want_lse, mean, delta, count, top = R.attend(inst, q[:, heads], scale, vd)
+    got, got_lse = out[:, heads].double().cpu().numpy(), lse[:, heads].double().cpu().numpy()
     bound = R.attend_bound(inst.dtype, want, mean, delta, count, top)
     rows = slice(None) if rows is None else rows
     assert np.isfinite(got[rows]).all()
@@ -106,6 +107,18 @@ def test_latent_chunks(H):
 
 def test_latent_long_split():
     check(R.instance(10, [1, 2], [6007, 31], kv=1, dim=576, planes=1, bt=64), 16)
+
+
+def test_latent_many_heads_split():
+    """More runs of keys than the chip takes at a time unless they are made longer."""
+    length = [15000, 9001, 17777, 12345, 16000, 14999, 11111, 13000, 18000, 8192]
+    check(R.instance(24, [1] * len(length), length, kv=1, dim=576, planes=1, bt=64), 65, heads=slice(0, 65, 16))
+
+
+def test_latent_many_sequences():
+    """More sequences than a wavefront has lanes, a few of them split."""
+    length = [1 + 5 * i for i in range(69)] + [2500, 1]
+    check(R.instance(25, [1] * 70 + [0], length, kv=1, dim=576, planes=1, bt=16), 100, heads=slice(3, 100, 24))
 
 
 def test_padding_and_empty_sequences():
