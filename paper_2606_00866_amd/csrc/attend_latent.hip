@@ -283,7 +283,7 @@ __global__ __launch_bounds__(256, RG == 4 ? 2 : 1) void attend_latent_kernel(Att
 // step).  Keys are staged in three areas: two steps' loads are under way.
 //
 // 48 sequences of 0.41 M keys in all, 128 heads (0.49 GB, 0.115 TFLOP): 169 us, 677
-// TFLOP/s; two chunks of 754 tokens in all, 32 heads (0.177 TFLOP): 311 us, 569
+// TFLOP/s; two chunks of 754 tokens in all, 32 heads (0.177 TFLOP): 298 us, 593
 // TFLOP/s on 189 of 256 CUs.  Of a step's cycles about 1300 are the score products,
 // 1160 the values, 575 setting out the loads and 575 the weights; the rest waits at
 // the barriers for the slowest wavefront: with one workgroup a CU nothing else runs

@@ -22,8 +22,8 @@
 // TFLOP): 1091 us, 961 TFLOP/s of the 1330 that a large product reaches; the matrix
 // units are busy 42% of the cycles, and the rest are the weights: 32 exponentials, a
 // maximum and roundings a lane for 32 products, which run beside the other
-// workgroup's products in part only.  Chunks of four sequences (0.2 TFLOP): 302 us,
-// 654 TFLOP/s, with uneven last items and the join; decode steps and chunks mixed
+// workgroup's products in part only.  Chunks of four sequences (0.2 TFLOP): 287 us,
+// 687 TFLOP/s, with uneven last items and the join; decode steps and chunks mixed
 // (32 sequences, 0.51 GB, 0.12 TFLOP): 270 us.
 #include "attend.h"
 
