@@ -20,7 +20,7 @@
 //
 // Three prompts of 19215 tokens in all (32 heads over 8 key heads of 128; 1.05
 // TFLOP): 1091 us, 961 TFLOP/s of the 1330 that a large product reaches; the matrix
-// units are busy 42% of the cycles, and the rest are the weights: 32 exponentials, a
+// units are busy 48% of the cycles, and the rest are the weights: 32 exponentials, a
 // maximum and roundings a lane for 32 products, which run beside the other
 // workgroup's products in part only.  Chunks of four sequences (0.2 TFLOP): 287 us,
 // 687 TFLOP/s, with uneven last items and the join; decode steps and chunks mixed
