@@ -282,8 +282,8 @@ __global__ __launch_bounds__(256, RG == 4 ? 2 : 1) void attend_latent_kernel(Att
 // before it (halves before barrier 2, weights and keys before barrier 1 of the next
 // step).  Keys are staged in three areas: two steps' loads are under way.
 //
-// 48 sequences of 0.41 M keys in all, 128 heads (0.49 GB, 0.115 TFLOP): 169 us, 677
-// TFLOP/s; two chunks of 754 tokens in all, 32 heads (0.177 TFLOP): 298 us, 593
+// 48 sequences of 0.41 M keys in all, 128 heads (0.49 GB, 0.115 TFLOP): 182 us, 631
+// TFLOP/s; two chunks of 754 tokens in all, 32 heads (0.177 TFLOP): 294 us, 600
 // TFLOP/s on 189 of 256 CUs.  Of a step's cycles about 1300 are the score products,
 // 1160 the values, 575 setting out the loads and 575 the weights; the rest waits at
 // the barriers for the slowest wavefront: with one workgroup a CU nothing else runs
@@ -321,19 +321,14 @@ __device__ inline uint32_t chunk_of(uint32_t k, uint32_t h, uint32_t g) {
   return k < 8 ? 8 * (4 * (k >> 2) + g) + 4 * h + (k & 3) : 64 + 4 * h + g;
 }
 
-// A step's loads (the last four of the 40 bring rows 0 to 3 again).  They have no
-// result in registers.  Written out, because the compiler keeps the registers of such
-// a load's address until it is done, and here they are wanted at once; wait_loads()
-// waits for them.
+// A step's loads (the last four of the 40 bring rows 0 to 3 again).
 __device__ __forceinline__ void fetch(const AttendArgs& a, uint8_t* to, uint32_t row, uint32_t wv, uint32_t lane) {
 #pragma unroll
   for (uint32_t i = 0; i < LOADS; ++i) {
     const uint32_t c = (i * NW + wv) * 64 + lane, r = c / CH, at = c - r * CH;
     const uint32_t p = (uint32_t)__shfl((int)row, (int)r);
     const uint8_t* const src = a.b.plane + (uint64_t)p * ROW + ((at ^ swizzle(r)) << 4);
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src),
-                 "s"(same(lds_address(to + (i * NW + wv) * 1024)))
-                 : "memory");  // m0 is set before each use, here as by the compiler
+    to_lds(src, to + (i * NW + wv) * 1024);
   }
 }
 
@@ -378,6 +373,7 @@ __device__ __forceinline__ void step(const AttendArgs& a, const Work& w, const u
   put(&x.part[wv][0][lane], s[1][0]);
   put(&x.part[wv][1][lane], s[1][1]);
   barrier();  // every wavefront is through with the step before: its area is free
+  __builtin_amdgcn_sched_barrier(0);  // the wait for the earlier loads (and the entry) stays behind it
   wait_loads();
   fetch(a, then, pool_row(a.b, ahead, entry, err), wv, lane);
 #pragma unroll
