@@ -372,12 +372,14 @@ __device__ inline void rows_one_by_one(const AttendArgs& a, const Work& w, uint3
       sum = sum * keep + f;
       o *= keep;
       const uint64_t v_at = reinterpret_cast<uint64_t>(row) + v_off;
+      vec part = 0;
       for (uint32_t j = 0; j < 64 && k0 + j < hi; ++j) {
         const scalar* v = reinterpret_cast<const scalar*>(wave::lane_of(v_at, (int)j));
         const float fj = __shfl(f, (int)j);
 #pragma unroll
-        for (int i = 0; i < W; ++i) o[i] += fj * (float)v[64 * i + lane];
+        for (int i = 0; i < W; ++i) part[i] += fj * (float)v[64 * i + lane];
       }
+      o += part;
     }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);

@@ -83,14 +83,16 @@ __device__ __forceinline__ void take(const AttendArgs& a, const Work& w, const u
 #pragma unroll
     for (int d = 0; d < DB; ++d) acc.o[d] *= keep;
   }
+  float part = 0;  // of this step: one by one, small weights would be lost in a large sum
   uint32_t p[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float f0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 2][2 * i % 4], a.c, -acc.top));
     const float f1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 2][2 * i % 4 + 1], a.c, -acc.top));
-    acc.sum += f0 + f1;
+    part += f0 + f1;
     p[i] = pair_of<DT>(f0, f1);
   }
+  acc.sum += part;
   // transposing reads: key rows 4 g .. 4 g + 3 of each 16, 16 elements per 16 lanes
   const uint32_t vrow = 4 * g + (lane >> 2 & 3);
   const uint32_t vx = swizzle(vrow), vc = lane >> 1 & 1;
@@ -399,14 +401,16 @@ __device__ __forceinline__ void step(const AttendArgs& a, const Work& w, const u
     acc.top = t;
     acc.sum *= keep;
   }
+  float part = 0;  // of this step, as above
   u32x4 p[2];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float f0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][i / 2][2 * i % 4], a.c, -acc.top));
     const float f1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][i / 2][2 * i % 4 + 1], a.c, -acc.top));
-    acc.sum += f0 + f1;
+    part += f0 + f1;
     p[0][i] = pair_of<DT>(f0, f1);
   }
+  acc.sum += part;
   put(&x.weight[wv][lane], p[0]);
   put(&x.keep[wv][n], keep);
   barrier();

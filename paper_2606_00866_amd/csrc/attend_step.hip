@@ -142,12 +142,13 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(AttendArgs a) {
 #pragma unroll
           for (int e = 0; e < E; ++e) o[nb][e] *= keep;
         }
-        float f[8];
+        float f[8], part = 0;  // of this step: one by one, small weights would be lost in a large sum
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           f[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nb][i / 4][i % 4], a.c, -top[nb]));
-          sum[nb] += f[i];
+          part += f[i];
         }
+        sum[nb] += part;
 #pragma unroll
         for (int i = 0; i < 4; ++i) p[nb][i] = pair_of<DT>(f[2 * i], f[2 * i + 1]);
       }

@@ -157,13 +157,15 @@ __device__ __forceinline__ void step(const AttendArgs& a, const Work& w, Tile<D,
 #pragma unroll
       for (int d = 0; d < DB; ++d) x.o[d] *= keep;
     }
+    float part = 0;  // of this step: one by one, small weights would be lost in a large sum
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const float f0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 8][2 * i % 16], a.c, -x.top));
       const float f1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 8][2 * i % 16 + 1], a.c, -x.top));
-      x.sum += f0 + f1;
+      part += f0 + f1;
       p[i] = pair_of<DT>(f0, f1);
     }
+    x.sum += part;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
 #pragma unroll
