@@ -19,9 +19,11 @@
 // rows, their maxima and sums) that a second kernel joins in a fixed order.
 //
 // Softmax.  Scores are kept in units of log2(e) / scale: weights are
-// exp2(score * c - top).  `top` is at or below the running maximum and follows
-// it only when that has risen by more than RISE, so weights stay at most 2^RISE
-// and most steps leave the accumulators alone.
+// exp2(score * c - top).  When the running maximum has risen more than RISE over
+// where it was last followed, `top` is set LIFT below it, so weights stay at most
+// 2^(LIFT + RISE) and most steps leave the accumulators alone.  The weights of the
+// sums and of the products are the same numbers but for the rounding of the latter
+// to the pool's type, so LIFT takes part in no result; it is there for that rounding.
 #pragma once
 #include "float16.h"
 #include "tokens.h"
@@ -29,7 +31,20 @@
 namespace mori {
 
 constexpr float NO_TOP = -3.0e38f;  // below any score; finite, so that masked scores (-inf) give weight 0
-constexpr float RISE = 8.0f;
+// bfloat16 has the exponents of 32 bits: any place will do.  float16 has 2^15 down to
+// 2^-14 (2^-24 with fewer bits): the maximum is put at 2^12 to 2^15, so that weights
+// keep all bits down to 2^-26 of it and vanish below 2^-37 (at 2^0 to 2^8: 2^-14 and
+// 2^-25, where 40000 keys 17.5 nats below a first one were lost whole).
+template <typename DT>
+struct Weight;
+template <>
+struct Weight<BF16> {
+  static constexpr float LIFT = 0.0f, RISE = 8.0f;
+};
+template <>
+struct Weight<F16> {
+  static constexpr float LIFT = 12.0f, RISE = 3.0f;
+};
 
 struct AttendArgs {
   Batch b;
@@ -260,6 +275,16 @@ __device__ inline float sum_over_32(float x) {
 __device__ inline float sum_over_16(float x) {
   const auto r = __builtin_amdgcn_permlane16_swap(bits<uint32_t>(x), bits<uint32_t>(x), false, false);
   return bits<float>(r[0]) + bits<float>(r[1]);
+}
+
+// Whether `top` has to follow the step's maximum m, and where to.
+template <typename DT>
+__device__ inline bool risen(float m, float top) {
+  return m > top + (Weight<DT>::LIFT + Weight<DT>::RISE);
+}
+template <typename DT>
+__device__ inline float follow(float m, float top) {
+  return fmaxf(top, m - Weight<DT>::LIFT);
 }
 
 __device__ inline f32x4 mfma_16x16x32(BF16, u32x4 a, u32x4 b, f32x4 c) {

@@ -76,8 +76,8 @@ __device__ __forceinline__ void take(const AttendArgs& a, const Work& w, const u
 #pragma unroll
   for (int i = 1; i < 8; ++i) m = fmaxf(m, s[i / 4][i % 4]);
   m = a.c * max_over_16(max_over_32(m));
-  if (__any(m > acc.top + RISE)) {
-    const float t = fmaxf(acc.top, m), keep = __builtin_amdgcn_exp2f(acc.top - t);
+  if (__any(risen<DT>(m, acc.top))) {
+    const float t = follow<DT>(m, acc.top), keep = __builtin_amdgcn_exp2f(acc.top - t);
     acc.top = t;
     acc.sum *= keep;
 #pragma unroll
@@ -395,8 +395,8 @@ __device__ __forceinline__ void step(const AttendArgs& a, const Work& w, const u
   for (int i = 1; i < 8; ++i) m = fmaxf(m, s[0][i / 4][i % 4]);
   m = a.c * max_over_16(max_over_32(m));
   float keep = 1.f;
-  if (__any(m > acc.top + RISE)) {
-    const float t = fmaxf(acc.top, m);
+  if (__any(risen<DT>(m, acc.top))) {
+    const float t = follow<DT>(m, acc.top);
     keep = __builtin_amdgcn_exp2f(acc.top - t);
     acc.top = t;
     acc.sum *= keep;

@@ -135,8 +135,8 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(AttendArgs a) {
 #pragma unroll
         for (int i = 1; i < 8; ++i) m = fmaxf(m, s[nb][i / 4][i % 4]);
         m = a.c * max_over_16(max_over_32(m));
-        if (__any(m > top[nb] + RISE)) {
-          const float t = fmaxf(top[nb], m), keep = __builtin_amdgcn_exp2f(top[nb] - t);
+        if (__any(risen<DT>(m, top[nb]))) {
+          const float t = follow<DT>(m, top[nb]), keep = __builtin_amdgcn_exp2f(top[nb] - t);
           top[nb] = t;
           sum[nb] *= keep;
 #pragma unroll

@@ -150,8 +150,8 @@ __device__ __forceinline__ void step(const AttendArgs& a, const Work& w, Tile<D,
 #pragma unroll
     for (int i = 1; i < 32; ++i) m = fmaxf(m, s[i / 16][i % 16]);
     m = a.c * max_over_32(m);
-    if (__any(m > x.top + RISE)) {
-      const float t = fmaxf(x.top, m), keep = __builtin_amdgcn_exp2f(x.top - t);
+    if (__any(risen<DT>(m, x.top))) {
+      const float t = follow<DT>(m, x.top), keep = __builtin_amdgcn_exp2f(x.top - t);
       x.top = t;
       x.sum *= keep;
 #pragma unroll

@@ -1,5 +1,5 @@
-"""kv_attend's weights over a wide range: many keys far below one that draws most of the
-weight."""
+"""kv_attend's weights over a wide range: keys far below one that draws most of the
+weight, scores that keep rising, in every form of the attention kernels."""
 import numpy as np
 import pytest
 import torch
@@ -69,3 +69,34 @@ def test_sum_of_small_weights_beside_a_large_one(form):
     each below half a step of the sum that holds it."""
     inst, q, H = sunk(form, 40000, [1] * 2200, BF16)
     compare(inst, q, 1.0, slice(0, H, max(1, H // 2)))
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("length", [250, 2000])
+def test_small_weights_beside_a_large_one(form, length):
+    inst, q, H = sunk(form, length)
+    compare(inst, q, 1.0, slice(0, H, max(1, H // 3)))
+
+
+@pytest.mark.parametrize("form", ["step16", "chunk", "latent16", "latent128"])
+def test_small_weights_in_one_run(form):
+    """A batch so large that no context is split: 40000 small weights meet the large one in
+    the same sum."""
+    inst, q, H = sunk(form, 40000, [1] * 2200)
+    compare(inst, q, 1.0, slice(0, H, max(1, H // 2)))
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("form", FORMS)
+def test_rising_scores(form, dtype):
+    """Every few keys a larger score than all before: the sums follow it each time."""
+    H, kv, n, latent = FORMS[form]
+    dim, rot = (576, 64) if latent else (64, 64)
+    inst = R.instance(32, [n], [400], kv=kv, dim=dim, planes=1 if latent else 2, dtype=dtype)
+    for j in range(400):
+        page, row = inst.slot(0, j)
+        inst.pool[1, 0, page, row, 0, dim - rot:] = 0.02 * j
+    g = torch.Generator().manual_seed(3)
+    q = torch.zeros(n, H, dim)
+    q[..., dim - rot:] = torch.rand(n, H, rot, generator=g) + 0.5  # some rows rise faster than others
+    compare(inst, q.to(dtype), 0.125, slice(0, H, max(1, H // 4)))
