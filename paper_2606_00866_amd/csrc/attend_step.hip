@@ -152,6 +152,16 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(AttendArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) p[nb][i] = pair_of<DT>(f[2 * i], f[2 * i + 1]);
       }
+      if (k0 + STEP > w.hi) {
+        // behind the end the last key's value is here again: its weight is 0, which an
+        // infinity there would turn into NaN
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (k0 + 16 * (j / 4) + 4 * g + j % 4 >= w.hi) {
+#pragma unroll
+            for (int i = 0; i < VW; ++i) vr[j][i] = 0;
+          }
+      }
       if (k0 + STEP > w.open && w.open < w.hi) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)

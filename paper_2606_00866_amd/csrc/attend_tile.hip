@@ -90,7 +90,8 @@ struct Tile {
 };
 
 // The rows behind the end of the last step's values: zeros, so that weights of 0
-// meet no infinity or NaN there.
+// meet no infinity or NaN there, be it of a row that is not the sequence's or of the
+// last one again.
 template <typename T>
 __device__ inline void drop_tail(const Work& w, uint8_t* area, uint32_t k0, uint32_t tid) {
   for (uint32_t i = 0; i < T::LD; ++i)
@@ -227,7 +228,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tile_kernel(AttendArgs a) {
     wait_loads();
     __syncthreads();
     const auto turn = [&](uint8_t* now_k, uint8_t* now_v, uint8_t* then_k, uint8_t* then_v, uint32_t k0) {
-      if (PAGED && k0 + STEP > w.hi) drop_tail<T>(w, now_v, k0, tid);
+      if (k0 + STEP > w.hi) drop_tail<T>(w, now_v, k0, tid);
       step<DT>(a, w, x, now_k, now_v, then_k, then_v, k0, tid, wv);
       x.find(a, w, k0 + 2 * STEP, tid);
       wait_loads();
