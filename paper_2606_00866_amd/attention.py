@@ -61,19 +61,23 @@ class TokenBatch:
     tensors may be rewritten between steps, also under a captured graph, as long
     as these bounds hold.
 
+    A batch is for pools of the geometry that it was made with.
+
     ``error`` collects the device's MORI_DEV_* bits; ``check`` waits, reads and
     clears it."""
 
     def __init__(self, geom, tbl_off: torch.Tensor, tbl: torch.Tensor, seq_off: torch.Tensor, kv_len: torch.Tensor,
                  program: torch.Tensor | None = None, *, num_tokens: int, max_new: int, max_kv: int):
-        self.geom = PoolGeometry(geom.layers, geom.planes, geom.block_tokens, geom.row_bytes, geom.num_blocks)
+        self.shape = tuple(int(x) for x in (geom.layers, geom.planes, geom.block_tokens, geom.row_bytes, geom.num_blocks))
+        self.geom = PoolGeometry(*self.shape)
+        self.pool_bytes = self.geom.pool_bytes
         self.num_seqs, self.num_tokens = int(kv_len.numel()), int(num_tokens)
         for name, x, n in (("tbl_off", tbl_off, None), ("tbl", tbl, None), ("seq_off", seq_off, self.num_seqs + 1),
                            ("kv_len", kv_len, self.num_seqs), ("program", program, self.num_seqs)):
             if x is None:
                 continue
-            _need(x.dtype == torch.int32 and x.is_contiguous() and x.dim() == 1 and x.device.type == "cuda",
-                  f"TokenBatch: {name} is a contiguous int32 vector on the device")
+            _need(x.dtype == torch.int32 and x.is_contiguous() and x.dim() == 1 and x.device.type == "cuda" and
+                  x.device == kv_len.device, f"TokenBatch: {name} is a contiguous int32 vector on the batch's device")
             _need(n is None or x.numel() == n, f"TokenBatch: {name} has {x.numel()} entries, not {n}")
         _need(num_tokens >= 0 and max_new >= 0 and 0 < max_kv < 1 << 31, "TokenBatch: bounds out of range")
         _need(tbl_off.numel() >= 2, "TokenBatch: tbl_off is empty")
@@ -109,11 +113,19 @@ class TokenBatch:
             raise MoriError("token batch", M.MORI_EDEVICE, bits)
 
 
-def _pool(pool: torch.Tensor, geom) -> M.mori_pool:
-    _need(pool.is_contiguous() and pool.device.type == "cuda" and
-          pool.numel() * pool.element_size() == geom.layers * geom.planes * geom.num_blocks * geom.block_tokens *
-          geom.row_bytes, "pool does not have its geometry's bytes")
-    return M.mori_pool(geom.layers, geom.planes, geom.block_tokens, geom.row_bytes, geom.num_blocks, pool.data_ptr())
+def _same_geometry(geom, batch: TokenBatch) -> None:
+    if (geom.layers, geom.planes, geom.block_tokens, geom.row_bytes, geom.num_blocks) != batch.shape:
+        raise MoriError("geom is not the batch's", M.MORI_EINVAL)
+
+
+def _pool(pool: torch.Tensor, geom, batch: TokenBatch, dtype: torch.dtype) -> M.mori_pool:
+    """The pool as bytes (any integer type) or as what its rows hold."""
+    _same_geometry(geom, batch)
+    if not pool.is_contiguous() or pool.device != batch.device or pool.nbytes != batch.pool_bytes:
+        raise MoriError("pool does not have its geometry's bytes on the batch's device", M.MORI_EINVAL)
+    if pool.dtype != dtype and pool.dtype.is_floating_point:
+        raise MoriError(f"the pool is of {pool.dtype}, the tokens of {dtype}", M.MORI_EINVAL)
+    return M.mori_pool(*batch.shape, pool.data_ptr())
 
 
 def _rows(name: str, x: torch.Tensor, batch: TokenBatch, dtype: torch.dtype, heads: int | None = None,
@@ -167,8 +179,8 @@ def kv_append(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, k: torch.
                 q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         a.q_out = _rows("q_out", q_out, heads=q.shape[1], dim=q.shape[2], written=True, **kw)
         a.q_heads = q.shape[1]
-    check(M.mori_kv_append(_pool(pool, geom), int(layer), batch.desc, a, batch.error.data_ptr(), _stream_of(batch, stream)),
-          "mori_kv_append")
+    check(M.mori_kv_append(_pool(pool, geom, batch, k.dtype), int(layer), batch.desc, a, batch.error.data_ptr(),
+                           _stream_of(batch, stream)), "mori_kv_append")
     return q_out
 
 
@@ -189,6 +201,7 @@ def _empty_pool(geom) -> M.mori_pool:
 def kv_attend_workspace(geom, batch: TokenBatch, q: torch.Tensor) -> torch.Tensor:
     """Device workspace for kv_attend of this batch, in every layer; calls that may
     overlap (on other streams) need one each."""
+    _same_geometry(geom, batch)
     a, _ = _attend_desc(geom, batch, q, None)
     rc, n = M.mori_kv_attend_workspace(_empty_pool(geom), batch.desc, a)
     check(rc, "mori_kv_attend_workspace")
@@ -214,12 +227,15 @@ def kv_attend(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, q: torch.
         _need(lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2] and
               lse.device == batch.device, "kv_attend: lse is a contiguous float32 [tokens][heads]")
         a.lse = lse.data_ptr()
-    desc = _pool(pool, geom)
-    if workspace is None:
+    desc = _pool(pool, geom, batch, q.dtype)
+    if workspace is not None:
+        if workspace.device != batch.device or not workspace.is_contiguous():
+            raise MoriError("kv_attend: workspace is contiguous and on the batch's device", M.MORI_EINVAL)
+    else:
         rc, n = M.mori_kv_attend_workspace(desc, batch.desc, a)
         check(rc, "mori_kv_attend_workspace")
         with _on(stream):
             workspace = torch.empty(n, dtype=torch.uint8, device=batch.device)
-    check(M.mori_kv_attend(desc, int(layer), batch.desc, a, workspace.data_ptr(), workspace.numel(),
+    check(M.mori_kv_attend(desc, int(layer), batch.desc, a, workspace.data_ptr(), workspace.nbytes,
                            batch.error.data_ptr(), _stream_of(batch, stream)), "mori_kv_attend")
     return out

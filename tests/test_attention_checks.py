@@ -1,0 +1,114 @@
+"""CPU-only checks of the Python entry points of the token operators: what does not
+fit raises before the library is called.  The batch is made without its device
+checks, on host tensors; the library's calls are replaced, so no address is used."""
+import dataclasses
+
+import pytest
+import torch
+
+from paper_2606_00866_amd import attention as A
+from paper_2606_00866_amd import mori as M
+from paper_2606_00866_amd.tiering import MoriError, PoolGeometry
+
+BF16, F16 = torch.bfloat16, torch.float16
+KV, DIM, H, T = 2, 64, 4, 3
+GEOM = dict(layers=2, planes=2, block_tokens=16, row_bytes=KV * DIM * 2, num_blocks=8)
+
+
+def geometry(**kw):
+    return PoolGeometry(**{**GEOM, **kw})
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """What reaches the library: a list of (name, arguments)."""
+    seen = []
+    monkeypatch.setattr(M, "mori_kv_append", lambda *a, **k: seen.append(("append", a)) or M.MORI_OK)
+    monkeypatch.setattr(M, "mori_kv_attend", lambda *a, **k: seen.append(("attend", a)) or M.MORI_OK)
+    monkeypatch.setattr(M, "mori_kv_attend_workspace", lambda *a, **k: (M.MORI_OK, 512))
+    monkeypatch.setattr(A, "_stream_of", lambda *a, **k: 0)
+    return seen
+
+
+def batch(**kw):
+    b = object.__new__(A.TokenBatch)
+    b.geom, b.num_seqs, b.num_tokens = geometry(**kw), 1, T
+    b.shape, b.pool_bytes = dataclasses.astuple(b.geom), b.geom.pool_bytes
+    b.device, b.index, b.error = torch.device("cpu"), 0, torch.zeros(1, dtype=torch.int32)
+    b.desc = M.mori_tokens(num_seqs=1, num_tokens=T, max_new=T, max_kv=40)
+    return b
+
+
+def pool(dtype=BF16, device="cpu"):
+    return torch.zeros(2, 2, 8, 16, KV, DIM, dtype=BF16, device=device).view(dtype)
+
+
+def append(p=None, geom=None, b=None, dtype=BF16, **kw):
+    k = torch.zeros(T, KV, DIM, dtype=dtype)
+    return A.kv_append(pool() if p is None else p, geom or geometry(), 0, b or batch(), k, k.clone(), **kw)
+
+
+def attend(p=None, geom=None, b=None, dtype=BF16, **kw):
+    q = torch.zeros(T, H, DIM, dtype=dtype)
+    return A.kv_attend(pool() if p is None else p, geom or geometry(), 0, b or batch(), q, **kw)
+
+
+def refused(call, calls, **kw):
+    with pytest.raises(MoriError) as e:
+        call(**kw)
+    assert e.value.code == M.MORI_EINVAL and not calls
+
+
+def test_what_fits_is_called(calls):
+    for p in (pool(), pool(torch.uint8), pool(torch.int16)):
+        append(p=p)
+        attend(p=p)
+        attend(p=p, workspace=torch.empty(512, dtype=torch.uint8))
+    assert [n for n, _ in calls] == ["append", "attend", "attend"] * 3
+    attend(workspace=torch.empty(128, dtype=torch.float32))
+    assert calls[-1][1][5] == 512  # bytes, whatever the type
+
+
+def test_workspace(calls):
+    """Somewhere else than the batch, or not one piece."""
+    for w in (torch.empty(512, dtype=torch.uint8, device="meta"), torch.empty(1024, dtype=torch.uint8)[::2],
+              torch.empty(16, 64, dtype=torch.uint8).t()):
+        refused(attend, calls, workspace=w)
+
+
+@pytest.mark.parametrize("call", [append, attend])
+def test_pool(calls, call):
+    """On another device than the batch, of the other 16-bit type, of another size."""
+    refused(call, calls, p=pool(device="meta"))
+    for dtype, other in ((F16, BF16), (BF16, F16)):
+        refused(call, calls, p=pool(other), dtype=dtype)
+    refused(call, calls, p=pool(torch.float32))
+    refused(call, calls, p=pool()[:1])
+
+
+@pytest.mark.parametrize("call", [append, attend])
+@pytest.mark.parametrize("change", [dict(block_tokens=32, num_blocks=4), dict(block_tokens=8, num_blocks=16),
+                                    dict(layers=1, num_blocks=16), dict(layers=4, planes=1)])
+def test_geometry_of_the_batch(calls, call, change):
+    """Another division of the same bytes: the batch's tables do not speak of it."""
+    assert geometry(**change).pool_bytes == geometry().pool_bytes
+    refused(call, calls, geom=geometry(**change))
+    refused(call, calls, b=batch(**change))
+
+
+def test_geometry_of_the_workspace(calls):
+    q = torch.zeros(T, H, DIM, dtype=BF16)
+    assert A.kv_attend_workspace(geometry(), batch(), q).numel() == 512
+    with pytest.raises(MoriError):
+        A.kv_attend_workspace(geometry(block_tokens=32, num_blocks=4), batch(), q)
+
+
+def test_inputs_elsewhere(calls):
+    k = torch.zeros(T, KV, DIM, dtype=BF16)
+    for kk, vv, kw in ((k.to("meta"), k, {}), (k, k.to("meta"), {}), (k, k, dict(q=k.to("meta"))),
+                       (k, k, dict(q=k, q_out=k.to("meta"))), (k, k, dict(rope=torch.zeros(40, 64, device="meta")))):
+        with pytest.raises(MoriError):
+            A.kv_append(pool(), geometry(), 0, batch(), kk, vv, **kw)
+    refused(attend, calls, out=torch.zeros(T, H, DIM, dtype=BF16, device="meta"))
+    refused(attend, calls, lse=torch.zeros(T, H, device="meta"))
+    assert not calls
