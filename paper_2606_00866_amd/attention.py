@@ -39,8 +39,12 @@ def rope_table(positions: int, rot_dim: int, theta: float = 10000.0, device="cud
 
 
 def _stream_of(batch, stream) -> int:
-    """The stream's handle; by default the current one of the batch's device."""
-    return torch._C._cuda_getCurrentRawStream(batch.index) if stream is None else stream.cuda_stream
+    """The handle of the stream that a call runs on, by default the current one of the
+    batch's device; the batch's error word is ready for it."""
+    handle = torch._C._cuda_getCurrentRawStream(batch.index) if stream is None else stream.cuda_stream
+    if handle != batch._last:
+        batch._enter(handle)
+    return handle
 
 
 def _on(stream):
@@ -64,7 +68,8 @@ class TokenBatch:
     A batch is for pools of the geometry that it was made with.
 
     ``error`` collects the device's MORI_DEV_* bits; ``check`` waits, reads and
-    clears it."""
+    clears it.  Calls may run on any streams; those stay alive until ``check`` or
+    the batch's end."""
 
     def __init__(self, geom, tbl_off: torch.Tensor, tbl: torch.Tensor, seq_off: torch.Tensor, kv_len: torch.Tensor,
                  program: torch.Tensor | None = None, *, num_tokens: int, max_new: int, max_kv: int):
@@ -84,6 +89,10 @@ class TokenBatch:
         self.device = kv_len.device
         self.index = kv_len.device.index
         self.error = torch.zeros(1, dtype=torch.int32, device=self.device)
+        # Streams other than the one that clears the word wait for that, and check waits for them.
+        made = torch.cuda.current_stream(self.device)
+        self._made, self._used, self._last = made.cuda_stream, set(), None
+        self._ready = None if torch.cuda.is_current_stream_capturing() else made.record_event()
         self._keep = (tbl_off, tbl, seq_off, kv_len, program)
         self.desc = M.mori_tokens(self.num_seqs, self.num_tokens, int(max_new), int(max_kv), seq_off.data_ptr(),
                                   kv_len.data_ptr(), program.data_ptr() if program is not None else None,
@@ -105,11 +114,39 @@ class TokenBatch:
         return cls(tier_pool.geom, tier_pool.tbl_off, tier_pool.tbl, dev(off), dev(length), dev(prog),
                    num_tokens=int(off[-1]), max_new=int(n.max(initial=0)), max_kv=max(1, int(length.max(initial=1))))
 
+    def _enter(self, handle: int) -> None:
+        """A call is about to use the stream: its first one, or the first after another's."""
+        if handle not in self._used and handle != self._made:
+            stream = torch.cuda.ExternalStream(handle, self.device)
+            with torch.cuda.stream(stream):
+                capturing = torch.cuda.is_current_stream_capturing()
+            if not capturing:  # a graph's inputs are ready before it is replayed
+                if self._ready is not None:
+                    stream.wait_event(self._ready)
+                for x in (self.error, *self._keep):
+                    if x is not None:
+                        x.record_stream(stream)
+        self._used.add(handle)
+        self._last = handle
+
     def check(self) -> None:
-        """Raises MoriError if the device found fault with the batch since the last check."""
+        """Raises MoriError if the device found fault with the batch since the last check.
+        Waits for every call since then, on whichever stream it was made.  Replays of a
+        captured graph are work of the stream that replays it: check on that stream, or
+        behind it."""
+        here = torch.cuda.current_stream(self.device)
+        if self._ready is not None and here.cuda_stream != self._made:
+            here.wait_event(self._ready)
+        for handle in self._used:
+            if handle != here.cuda_stream:
+                here.wait_stream(torch.cuda.ExternalStream(handle, self.device))
         bits = int(self.error.item())
         if bits:
             self.error.zero_()
+            here.synchronize()  # cleared before any stream's next call
+        self._used.clear()
+        self._last = self._ready = None
+        if bits:
             raise MoriError("token batch", M.MORI_EDEVICE, bits)
 
 
