@@ -7,7 +7,8 @@ which programs; it is made once a step and used in every layer.
 Like ``mori``, this only marshals arguments: the work runs in libmori's kernels,
 on the current stream unless one is given, and nothing here waits for the device
 (but ``TokenBatch.check``).  Arguments that do not fit raise ``MoriError`` before
-anything is enqueued.
+anything is enqueued.  The operators serve: where gradients are recorded, tensors
+that require them are refused, and what is written counts as changed in place.
 """
 from __future__ import annotations
 
@@ -45,6 +46,13 @@ def _stream_of(batch, stream) -> int:
     if handle != batch._last:
         batch._enter(handle)
     return handle
+
+
+def _needs_gradients(what: str) -> MoriError:
+    """These operators have no backward pass: where gradients are recorded, tensors
+    that need them are refused instead of being left out of the record."""
+    return MoriError(f"{what}: no gradients pass through a paged pool (detach, or call under torch.no_grad())",
+                     M.MORI_EINVAL)
 
 
 def _on(stream):
@@ -194,40 +202,50 @@ def kv_append(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, k: torch.
     copied, v [T][1][rot] rotated behind it.  q, if given, is rotated the same way
     ([T][q_heads][head_dim], or [T][q_heads][rot] with planes 1) into q_out, which
     may be q; returns q_out (allocated if not given)."""
-    _need(k.dtype in DTYPES, "kv_append: float16 or bfloat16")
-    _need(style in STYLES, f"kv_append: style {style!r}")
-    _need(k.dim() == 3 and v.dim() == 3, "kv_append: k and v are [tokens][heads][elements]")
-    latent = geom.planes == 1
-    dim = k.shape[2] + v.shape[2] if latent else k.shape[2]
-    rot = 0
+    if torch.is_grad_enabled() and (k.requires_grad or v.requires_grad or pool.requires_grad or
+                                    (q is not None and q.requires_grad) or (q_out is not None and q_out.requires_grad) or
+                                    (rope is not None and rope.requires_grad)):
+        raise _needs_gradients("kv_append")
+    dtype = k.dtype
+    if dtype not in DTYPES or style not in STYLES:
+        raise MoriError("kv_append: float16 or bfloat16, style 'half' or 'pairs'", M.MORI_EINVAL)
+    if k.dim() != 3 or v.dim() != 3:
+        raise MoriError("kv_append: k and v are [tokens][heads][elements]", M.MORI_EINVAL)
+    latent, heads, dim = geom.planes == 1, k.shape[1], k.shape[2]
+    if latent:
+        dim += v.shape[2]
+    rot = positions = 0
     if rope is not None:
-        _need(rope.dtype == torch.float32 and rope.dim() == 2 and rope.is_contiguous() and rope.device == batch.device,
-              "kv_append: rope is a contiguous float32 [positions][rot_dim] on the batch's device")
-        rot = int(rope.shape[1])
-    kw = dict(batch=batch, dtype=k.dtype)
-    a = M.mori_append(DTYPES[k.dtype], k.shape[1], dim, 0, rot, STYLES[style], 0 if rope is None else rope.shape[0],
-                      None if rope is None else rope.data_ptr())
-    a.k = _rows("k", k, heads=1 if latent else None, **kw)
-    a.v = _rows("v", v, heads=k.shape[1], dim=rot if latent else dim, **kw)
+        if rope.dtype != torch.float32 or rope.dim() != 2 or not rope.is_contiguous() or rope.device != batch.device:
+            raise MoriError("kv_append: rope is a contiguous float32 [positions][rot_dim] on the batch's device",
+                            M.MORI_EINVAL)
+        positions, rot = rope.shape
+    a = M.mori_append(DTYPES[dtype], heads, dim, 0, rot, STYLES[style], positions, rope.data_ptr() if rot else None)
+    a.k = _rows("k", k, batch, dtype, 1 if latent else None)
+    a.v = _rows("v", v, batch, dtype, heads, rot if latent else dim)
     if q is not None:
-        a.q = _rows("q", q, dim=rot if latent else dim, **kw)
+        a.q = _rows("q", q, batch, dtype, None, rot if latent else dim)
         if q_out is None:
             with _on(stream):
                 q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        a.q_out = _rows("q_out", q_out, heads=q.shape[1], dim=q.shape[2], written=True, **kw)
+        a.q_out = _rows("q_out", q_out, batch, dtype, q.shape[1], q.shape[2], True)
         a.q_heads = q.shape[1]
-    check(M.mori_kv_append(_pool(pool, geom, batch, k.dtype), int(layer), batch.desc, a, batch.error.data_ptr(),
+    check(M.mori_kv_append(_pool(pool, geom, batch, dtype), int(layer), batch.desc, a, batch.error.data_ptr(),
                            _stream_of(batch, stream)), "mori_kv_append")
+    torch.autograd.graph.increment_version((pool,) if q is None else (pool, q_out))
     return q_out
 
 
-def _attend_desc(geom, batch: TokenBatch, q: torch.Tensor, scale: float | None):
-    _need(q.dtype in DTYPES and q.dim() == 3, "kv_attend: q is [tokens][heads][elements] of float16 or bfloat16")
-    dim = int(q.shape[2])
-    _need(dim > 0 and geom.row_bytes % (2 * dim) == 0, f"kv_attend: rows of {geom.row_bytes} B hold no heads of {dim}")
+def _attend_desc(geom, q: torch.Tensor, scale: float | None) -> M.mori_attend:
+    shape, dtype = q.shape, DTYPES.get(q.dtype)
+    if dtype is None or len(shape) != 3:
+        raise MoriError("kv_attend: q is [tokens][heads][elements] of float16 or bfloat16", M.MORI_EINVAL)
+    dim = shape[2]
     value = dim - LATENT_ROPE if geom.planes == 1 else dim
-    return M.mori_attend(DTYPES[q.dtype], q.shape[1], geom.row_bytes // (2 * dim), dim, value,
-                         dim ** -0.5 if scale is None else float(scale)), value
+    if value <= 0 or geom.row_bytes % (2 * dim):
+        raise MoriError(f"kv_attend: rows of {geom.row_bytes} B hold no heads of {dim}", M.MORI_EINVAL)
+    return M.mori_attend(dtype, shape[1], geom.row_bytes // (2 * dim), dim, value,
+                         dim ** -0.5 if scale is None else float(scale))
 
 
 def _empty_pool(geom) -> M.mori_pool:
@@ -239,7 +257,7 @@ def kv_attend_workspace(geom, batch: TokenBatch, q: torch.Tensor) -> torch.Tenso
     """Device workspace for kv_attend of this batch, in every layer; calls that may
     overlap (on other streams) need one each."""
     _same_geometry(geom, batch)
-    a, _ = _attend_desc(geom, batch, q, None)
+    a = _attend_desc(geom, q, None)
     rc, n = M.mori_kv_attend_workspace(_empty_pool(geom), batch.desc, a)
     check(rc, "mori_kv_attend_workspace")
     return torch.empty(n, dtype=torch.uint8, device=batch.device)
@@ -254,17 +272,20 @@ def kv_attend(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, q: torch.
     [head_dim] (latent pools: 512), allocated if not given; lse, a float32
     [T][q_heads] tensor, takes the logarithms of the rows' sums.  The workspace is
     allocated here unless given."""
-    a, value = _attend_desc(geom, batch, q, scale)
-    a.q = _rows("q", q, batch, q.dtype)
+    if torch.is_grad_enabled() and (q.requires_grad or pool.requires_grad or (out is not None and out.requires_grad) or
+                                    (lse is not None and lse.requires_grad)):
+        raise _needs_gradients("kv_attend")
+    a, dtype = _attend_desc(geom, q, scale), q.dtype
+    a.q = _rows("q", q, batch, dtype)
     if out is None:
         with _on(stream):
-            out = torch.empty(q.shape[0], q.shape[1], value, dtype=q.dtype, device=q.device)
-    a.out = _rows("out", out, batch, q.dtype, q.shape[1], value, True)
+            out = torch.empty(q.shape[0], a.q_heads, a.value_dim, dtype=dtype, device=q.device)
+    a.out = _rows("out", out, batch, dtype, a.q_heads, a.value_dim, True)
     if lse is not None:
         _need(lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2] and
               lse.device == batch.device, "kv_attend: lse is a contiguous float32 [tokens][heads]")
         a.lse = lse.data_ptr()
-    desc = _pool(pool, geom, batch, q.dtype)
+    desc = _pool(pool, geom, batch, dtype)
     if workspace is not None:
         if workspace.device != batch.device or not workspace.is_contiguous():
             raise MoriError("kv_attend: workspace is contiguous and on the batch's device", M.MORI_EINVAL)
@@ -275,4 +296,5 @@ def kv_attend(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, q: torch.
             workspace = torch.empty(n, dtype=torch.uint8, device=batch.device)
     check(M.mori_kv_attend(desc, int(layer), batch.desc, a, workspace.data_ptr(), workspace.nbytes,
                            batch.error.data_ptr(), _stream_of(batch, stream)), "mori_kv_attend")
+    torch.autograd.graph.increment_version((out,) if lse is None else (out, lse))
     return out

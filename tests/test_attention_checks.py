@@ -112,3 +112,54 @@ def test_inputs_elsewhere(calls):
     refused(attend, calls, out=torch.zeros(T, H, DIM, dtype=BF16, device="meta"))
     refused(attend, calls, lse=torch.zeros(T, H, device="meta"))
     assert not calls
+
+
+def test_gradients_are_refused(calls):
+    """Where they are recorded; under no_grad the same tensors are taken."""
+    x = lambda h: torch.zeros(T, h, DIM, dtype=BF16)
+    needs = lambda h: x(h).requires_grad_()
+    for k, v, kw in ((needs(KV), x(KV), {}), (x(KV), needs(KV), {}), (x(KV), x(KV), dict(q=needs(H))),
+                     (x(KV), x(KV), dict(q=x(H), q_out=needs(H))),
+                     (x(KV), x(KV), dict(rope=torch.zeros(40, DIM, requires_grad=True)))):
+        go = lambda: A.kv_append(pool(), geometry(), 0, batch(), k, v, **kw)
+        with pytest.raises(MoriError) as e:
+            go()
+        assert e.value.code == M.MORI_EINVAL and not calls
+        with torch.no_grad():
+            go()
+        assert calls.pop()
+    for q, kw in ((needs(H), {}), (x(H), dict(out=needs(H))), (x(H), dict(lse=torch.zeros(T, H, requires_grad=True)))):
+        go = lambda: A.kv_attend(pool(), geometry(), 0, batch(), q, **kw)
+        with pytest.raises(MoriError) as e:
+            go()
+        assert e.value.code == M.MORI_EINVAL and not calls
+        with torch.no_grad():
+            go()
+        assert calls.pop()
+
+
+def test_what_is_written_counts_as_changed(calls):
+    """A tensor saved for a backward pass and then rewritten here is noticed there."""
+    p, q, out, lse = pool(), torch.zeros(T, H, DIM, dtype=BF16), torch.zeros(T, H, DIM, dtype=BF16), torch.zeros(T, H)
+    k = torch.zeros(T, KV, DIM, dtype=BF16)
+    w = torch.ones(DIM, dtype=BF16, requires_grad=True)
+    y = (q * w).sum()
+    before = p._version, out._version, lse._version
+    A.kv_append(p, geometry(), 0, batch(), k, k, q=q, q_out=q)
+    A.kv_attend(p, geometry(), 0, batch(), q, out=out, lse=lse)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    assert (p._version, out._version, lse._version) == tuple(b + 1 for b in before)
+    with torch.inference_mode():
+        q = torch.zeros(T, H, DIM, dtype=BF16)
+        A.kv_append(p, geometry(), 0, batch(), k, k, q=q, q_out=q)
+        A.kv_attend(p, geometry(), 0, batch(), q)
+
+
+def test_query_widths_that_no_row_holds(calls):
+    for shape, kw in (((T, H, 0), {}), ((T, H, 48), {}), ((T, H), {}), ((T, H, 64), dict(planes=1, layers=4)),
+                      ((T, H, 32), dict(planes=1, layers=4))):
+        q = torch.zeros(*shape, dtype=BF16)
+        with pytest.raises(MoriError):
+            A.kv_attend(pool(), geometry(**kw), 0, batch(**kw), q)
+    assert not calls
