@@ -22,6 +22,7 @@ from .tiering import MoriError, PoolGeometry, check
 
 DTYPES = {torch.float16: M.MORI_DT_F16, torch.bfloat16: M.MORI_DT_BF16}
 STYLES = {"half": M.MORI_ROPE_HALF, "pairs": M.MORI_ROPE_PAIRS}
+_current_device = torch._C._cuda_getDevice
 LATENT_ROPE = 64  # rotated elements behind the latent part of a latent row
 
 
@@ -43,6 +44,8 @@ def _stream_of(batch, stream) -> int:
     """The handle of the stream that a call runs on, by default the current one of the
     batch's device; the batch's error word is ready for it."""
     handle = torch._C._cuda_getCurrentRawStream(batch.index) if stream is None else stream.cuda_stream
+    if stream is not None and stream.device != batch.device:
+        raise MoriError(f"a stream of {stream.device} for a batch on {batch.device}", M.MORI_EINVAL)
     if handle != batch._last:
         batch._enter(handle)
     return handle
@@ -202,6 +205,9 @@ def kv_append(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, k: torch.
     copied, v [T][1][rot] rotated behind it.  q, if given, is rotated the same way
     ([T][q_heads][head_dim], or [T][q_heads][rot] with planes 1) into q_out, which
     may be q; returns q_out (allocated if not given)."""
+    if _current_device() != batch.index:  # launches go to the current device
+        with torch.cuda.device(batch.index):
+            return kv_append(pool, geom, layer, batch, k, v, q=q, q_out=q_out, rope=rope, style=style, stream=stream)
     if torch.is_grad_enabled() and (k.requires_grad or v.requires_grad or pool.requires_grad or
                                     (q is not None and q.requires_grad) or (q_out is not None and q_out.requires_grad) or
                                     (rope is not None and rope.requires_grad)):
@@ -272,6 +278,9 @@ def kv_attend(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, q: torch.
     [head_dim] (latent pools: 512), allocated if not given; lse, a float32
     [T][q_heads] tensor, takes the logarithms of the rows' sums.  The workspace is
     allocated here unless given."""
+    if _current_device() != batch.index:  # launches go to the current device
+        with torch.cuda.device(batch.index):
+            return kv_attend(pool, geom, layer, batch, q, scale=scale, out=out, lse=lse, workspace=workspace, stream=stream)
     if torch.is_grad_enabled() and (q.requires_grad or pool.requires_grad or (out is not None and out.requires_grad) or
                                     (lse is not None and lse.requires_grad)):
         raise _needs_gradients("kv_attend")

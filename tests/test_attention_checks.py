@@ -27,6 +27,7 @@ def calls(monkeypatch):
     monkeypatch.setattr(M, "mori_kv_attend", lambda *a, **k: seen.append(("attend", a)) or M.MORI_OK)
     monkeypatch.setattr(M, "mori_kv_attend_workspace", lambda *a, **k: (M.MORI_OK, 512))
     monkeypatch.setattr(A, "_stream_of", lambda *a, **k: 0)
+    monkeypatch.setattr(A, "_current_device", lambda: 0, raising=False)
     return seen
 
 
@@ -163,3 +164,36 @@ def test_query_widths_that_no_row_holds(calls):
         with pytest.raises(MoriError):
             A.kv_attend(pool(), geometry(**kw), 0, batch(**kw), q)
     assert not calls
+
+
+@pytest.mark.parametrize("call", [append, attend])
+def test_another_device_is_current(calls, monkeypatch, call):
+    """The library launches on the current device: the batch's is made that for the call."""
+    now = [1]
+
+    class Device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            self.before, now[0] = now[0], self.index
+
+        def __exit__(self, *_):
+            now[0] = self.before
+
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(A, "_current_device", lambda: now[0], raising=False)
+    for name in ("mori_kv_append", "mori_kv_attend"):
+        monkeypatch.setattr(M, name, lambda *a, **k: calls.append(now[0]) or M.MORI_OK)
+    call()
+    assert calls == [0] and now == [1]
+
+
+def test_a_stream_of_another_device(monkeypatch):
+    class Stream:
+        cuda_stream, device = 64, torch.device("cuda", 1)
+
+    b = batch()
+    b._last = 0
+    with pytest.raises(MoriError):
+        A._stream_of(b, Stream())
