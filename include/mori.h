@@ -469,7 +469,8 @@ typedef struct {
 
 /* Writes the batch's keys and values of one layer into the pool.  *error
  * (device, may be NULL) collects MORI_DEV_* bits by OR; the caller clears it.
- * EINVAL: null pointers, alignment, sizes that do not fit each other. */
+ * EINVAL: null pointers, alignment, sizes that do not fit each other, 2^36
+ * elements or more in a batch (queries, keys and values; a launch's threads). */
 int mori_kv_append(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, const mori_append* append,
                    uint32_t* error, void* stream);
 
@@ -501,7 +502,8 @@ int mori_kv_attend_workspace(const mori_pool* pool, const mori_tokens* tokens, c
  * while the call's work runs; its contents before do not matter.  The result is
  * the same for every call with the same arguments, bit for bit.  error as in
  * mori_kv_append.  EINVAL: null pointers, alignment, sizes or head dimensions
- * other than the above, a short workspace. */
+ * other than the above, a short workspace, a batch of more tokens than a launch has
+ * threads for (num_tokens * q_heads below 2^27 always fits). */
 int mori_kv_attend(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, const mori_attend* attend,
                    void* workspace, uint64_t workspace_bytes, uint32_t* error, void* stream);
 

@@ -74,7 +74,8 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
   // runs have `least` units or more, so short contexts give fewer items than slots
   const uint64_t runs = tiles * (((uint64_t)a.b.max_kv + a.unit - 1) / a.unit) / a.least;
   const uint64_t items = tiles + (a.splits ? std::min<uint64_t>(a.slots, runs + 1) : 0);
-  if (items * a.kv_heads >= (1ull << 31)) return false;
+  const uint64_t threads = p.latent && a.tile_rows == 128 ? 512 : 256;  // of a workgroup
+  if (items * a.kv_heads * threads >= (1ull << 32)) return false;  // a launch has fewer
   a.items = (uint32_t)items;
   const uint64_t n = a.splits ? items * a.kv_heads * a.tile_rows : 0;
   p.ml_at = n * p.value * sizeof(float);
