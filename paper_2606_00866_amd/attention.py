@@ -13,6 +13,7 @@ that require them are refused, and what is written counts as changed in place.
 from __future__ import annotations
 
 import contextlib
+import warnings
 
 import numpy as np
 import torch
@@ -274,13 +275,18 @@ def kv_attend(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, q: torch.
               workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Causal attention of the batch's tokens over their programs' pages in one
     layer.  q [T][q_heads][head_dim] (latent pools: [T][q_heads][576], in the latent
-    space); scale: head_dim ** -0.5 unless given.  Returns out [T][q_heads]
+    space).  scale: head_dim ** -0.5 unless given; a latent row's width says nothing
+    of the model's own (its heads' width before compression, 128 + 64 where rows are
+    512 + 64), so on latent pools leaving it out warns.  Returns out [T][q_heads]
     [head_dim] (latent pools: 512), allocated if not given; lse, a float32
     [T][q_heads] tensor, takes the logarithms of the rows' sums.  The workspace is
     allocated here unless given."""
     if _current_device() != batch.index:  # launches go to the current device
         with torch.cuda.device(batch.index):
             return kv_attend(pool, geom, layer, batch, q, scale=scale, out=out, lse=lse, workspace=workspace, stream=stream)
+    if scale is None and geom.planes == 1:
+        warnings.warn("kv_attend: no scale given for a latent pool; 576 ** -0.5 is taken, which is not that of the "
+                      "model's heads", stacklevel=2)
     if torch.is_grad_enabled() and (q.requires_grad or pool.requires_grad or (out is not None and out.requires_grad) or
                                     (lse is not None and lse.requires_grad)):
         raise _needs_gradients("kv_attend")

@@ -197,3 +197,18 @@ def test_a_stream_of_another_device(monkeypatch):
     b._last = 0
     with pytest.raises(MoriError):
         A._stream_of(b, Stream())
+
+
+def test_latent_pools_ask_for_the_model_s_scale(calls):
+    """The row's width is not the width of the model's heads: taking it is not silent."""
+    import warnings
+
+    b, g = batch(planes=1, row_bytes=1152), geometry(planes=1, row_bytes=1152)
+    p, q = torch.zeros(g.pool_bytes, dtype=torch.uint8), torch.zeros(T, H, 576, dtype=BF16)
+    with pytest.warns(UserWarning, match="scale"):
+        A.kv_attend(p, g, 0, b, q)
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        A.kv_attend(p, g, 0, b, q, scale=192 ** -0.5)
+        attend()
+    assert [c[1][3].scale for c in calls] == pytest.approx([576 ** -0.5, 192 ** -0.5, DIM ** -0.5])
