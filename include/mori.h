@@ -480,7 +480,9 @@ int mori_kv_append(const mori_pool* pool, uint32_t layer, const mori_tokens* tok
  *   planes 2   head_dim 64 or 128, value_dim the same
  *   planes 1   head_dim 576, value_dim 512 (the row's first 512 elements)
  * Scores, maxima, sums and outputs are kept in 32 bits; the weights are rounded
- * to dtype for the matrix product with the values. */
+ * to dtype for the matrix product with the values.  fp16 weights keep all their
+ * bits down to 2^-26 of the largest and are 0 below 2^-37 (bf16: where 32 bits end);
+ * an infinite value under a weight that is 0 so gives NaN. */
 typedef struct {
   uint32_t dtype;     /* MORI_DT_* */
   uint32_t q_heads;   /* multiple of kv_heads, <= 1024 */

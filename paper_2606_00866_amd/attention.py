@@ -85,7 +85,8 @@ class TokenBatch:
 
     def __init__(self, geom, tbl_off: torch.Tensor, tbl: torch.Tensor, seq_off: torch.Tensor, kv_len: torch.Tensor,
                  program: torch.Tensor | None = None, *, num_tokens: int, max_new: int, max_kv: int):
-        self.shape = tuple(int(x) for x in (geom.layers, geom.planes, geom.block_tokens, geom.row_bytes, geom.num_blocks))
+        self.shape = tuple(int(getattr(geom, name)) for name in
+                           ("layers", "planes", "block_tokens", "row_bytes", "num_blocks"))
         self.geom = PoolGeometry(*self.shape)
         self.pool_bytes = self.geom.pool_bytes
         self.num_seqs, self.num_tokens = int(kv_len.numel()), int(num_tokens)
@@ -210,7 +211,8 @@ def kv_append(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, k: torch.
         with torch.cuda.device(batch.index):
             return kv_append(pool, geom, layer, batch, k, v, q=q, q_out=q_out, rope=rope, style=style, stream=stream)
     if torch.is_grad_enabled() and (k.requires_grad or v.requires_grad or pool.requires_grad or
-                                    (q is not None and q.requires_grad) or (q_out is not None and q_out.requires_grad) or
+                                    (q is not None and q.requires_grad) or
+                                    (q_out is not None and q_out.requires_grad) or
                                     (rope is not None and rope.requires_grad)):
         raise _needs_gradients("kv_append")
     dtype = k.dtype
@@ -283,7 +285,8 @@ def kv_attend(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, q: torch.
     allocated here unless given."""
     if _current_device() != batch.index:  # launches go to the current device
         with torch.cuda.device(batch.index):
-            return kv_attend(pool, geom, layer, batch, q, scale=scale, out=out, lse=lse, workspace=workspace, stream=stream)
+            return kv_attend(pool, geom, layer, batch, q, scale=scale, out=out, lse=lse, workspace=workspace,
+                             stream=stream)
     if scale is None and geom.planes == 1:
         warnings.warn("kv_attend: no scale given for a latent pool; 576 ** -0.5 is taken, which is not that of the "
                       "model's heads", stacklevel=2)

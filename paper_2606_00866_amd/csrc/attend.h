@@ -94,9 +94,11 @@ struct Item {
 // and two, the one that takes the least time.  In units: each round its run and an
 // item's fixed cost (queries, first keys), about 3, and for every 64 items of split
 // tiles one more to write and join 256 KiB of partial sums each.  No choice is below
-// c, so the bound on the items stands.  48 sequences of 8600 keys on average, 128
-// heads: 184-190 us (kernels alone), 204-210 with c; two chunks of 754 tokens in all at
-// 3550 keys, 32 heads: 311, 317 with c (before its join was made shorter).
+// c, so the bound on the items stands.  The 3 and the 64 were fitted to the two cases
+// measured: 48 sequences of 8600 keys on average, 128 heads, 197-200 us a call, 223
+// with c; two chunks of 754 tokens in all at 3550 keys, 32 heads, 296-298, 314 with c.
+// Batches of up to 64 sequences, one a lane: more would be summed anew for every length
+// tried, which has not been measured.
 __device__ inline uint32_t run_of_rounds(const AttendArgs& a, const Share& own, uint64_t total, uint32_t c) {
   const uint32_t tiles = wave::sum(own.tiles);
   const auto items = [&](uint32_t run) { return wave::sum(own.tiles * ((own.units + run - 1) / run)); };

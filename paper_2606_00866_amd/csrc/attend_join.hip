@@ -3,7 +3,9 @@
 // A token whose tile was one run has nothing to join.  Bound by reading the partial
 // sums (2 KiB a row and run where rows are latent): 18 us where 250 items of 128
 // latent rows are joined, 30 for 25856 rows of mixed chunks; 5 to 9 us for the rows of
-// one to eight sequences, where it is the launch, the search and two dependent reads.
+// one to eight sequences, where it is the launch, the search and two dependent reads,
+// and 11 us for 24128 latent rows of which none was split (it is launched where tiles
+// may be split, which only the device knows).
 #include <algorithm>
 #include <type_traits>
 
@@ -67,7 +69,7 @@ __global__ __launch_bounds__(64 * NW) void attend_join_kernel(AttendArgs a, uint
             v[u] = *reinterpret_cast<const vec*>(a.part + (at0 + (i0 + min(i + u, m - 1)) * step) * DV + W * lane);
 #pragma unroll
           for (uint32_t u = 0; u < U; ++u) {
-            if (i + u >= m || (skip >> (i + u) & 1)) continue;  // a run without keys wrote no rows
+            if (i + u >= m || (skip >> (i + u) & 1)) continue;  // a run without keys
             y += v[u] * bits<float>((uint32_t)__builtin_amdgcn_readlane((int)bits<uint32_t>(f), (int)(i + u)));
           }
         }

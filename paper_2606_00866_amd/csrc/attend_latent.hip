@@ -13,7 +13,8 @@
 //         other wavefronts compute, keep enough loads in flight;
 //   RG 2  up to 32 rows, two groups with two areas each: the next keys load behind
 //         this step's products;
-//   RG 4  up to 64 rows, one group, two workgroups a CU.
+//   RG 4  up to 64 rows, one group, two workgroups a CU (256 registers a lane, three
+//         words of which go to scratch).
 // More rows than that have a kernel of their own, below.
 //
 // 256 sequences of 2.25 M keys in all, 16 heads (2.6 GB): 549 us, 4.7 TB/s of the
@@ -282,23 +283,24 @@ __global__ __launch_bounds__(256, RG == 4 ? 2 : 1) void attend_latent_kernel(Att
 //   have arrived, new ones set out - add, weights, to LDS - barrier 2 - values
 // Two barriers a step are enough: what is overwritten behind a barrier was last read
 // before it (halves before barrier 2, weights and keys before barrier 1 of the next
-// step).  Keys are staged in three areas: two steps' loads are under way.
+// step).  Keys are staged in three areas: one is read, one has arrived, one is loaded;
+// a step's loads have the whole of the next one to arrive in.
 //
-// 48 sequences of 0.41 M keys in all, 128 heads (0.49 GB, 0.115 TFLOP): 182 us, 631
-// TFLOP/s; two chunks of 754 tokens in all, 32 heads (0.177 TFLOP): 294 us, 600
-// TFLOP/s on 189 of 256 CUs.  Of a step's cycles about 1300 are the score products,
-// 1160 the values, 575 setting out the loads and 575 the weights; the rest waits at
-// the barriers for the slowest wavefront: with one workgroup a CU nothing else runs
-// then.  At the same run lengths eight wavefronts that each kept 16 rows to themselves
-// took 236 us for the first, this 209.
+// 48 sequences of 0.41 M keys in all, 128 heads (0.49 GB, 0.115 TFLOP): 183 us, 627
+// TFLOP/s; two chunks of 754 tokens in all, 32 heads (0.177 TFLOP): 295 us, 599
+// TFLOP/s on 189 of 256 CUs.  The matrix units are busy 33% of the first's cycles: the
+// products of a step, its weights and its loads follow one another between the
+// barriers, and with one workgroup a CU nothing else runs while wavefronts wait there.
+// At the same run lengths eight wavefronts that each kept 16 rows to themselves took
+// 236 us for the first, this 209.
 namespace wide {
 
 constexpr int NW = 8, AREAS = 3, LOADS = 5;
 constexpr uint32_t AREA = LOADS * NW * 1024;  // 32 rows and a tail that is loaded but not read
 constexpr int KS = DK / 64, DB = DV / 32;  // steps and value blocks of a half
 
-// Barrier for data in LDS that wavefronts wrote themselves (loads into LDS may be
-// under way; those are waited for by count).
+// Barrier for data in LDS that wavefronts wrote themselves.  It does not wait for the
+// loads into LDS under way; wait_loads() and the barrier behind it do.
 __device__ inline void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 // Stores to LDS that the compiler does not set behind the loads into LDS under way
 // (it orders any store after all of them); barrier() waits for these.

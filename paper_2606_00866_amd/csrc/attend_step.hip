@@ -20,8 +20,9 @@
 // LDS would add writes, reads and barriers and share nothing.
 //
 // 64 sequences of 1.19 M keys in all (8 key heads of 128, groups of 4; 4.86 GB):
-// 895 us, 5.4 TB/s of the 6.2 that a copy reaches; a step's loads ahead in two
-// wavefronts a SIMD is what the registers hold.  One sequence of 65502 keys, one key
+// 892 us, 5.4 TB/s of the 6.2 that a copy reaches, a step's loads ahead in two
+// wavefronts a SIMD (200 registers a lane of the 256 they may have at head dimension
+// 128; with 17 to 32 rows 292, one wavefront a SIMD).  One sequence of 65502 keys, one key
 // head (34 MB): 17 us with the join, 2 TB/s: finding the item, two rounds of dependent
 // reads (table, keys) and the second launch.  Eight sequences of 760 keys: 10 us.
 #include "attend.h"

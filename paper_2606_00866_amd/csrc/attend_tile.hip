@@ -19,10 +19,10 @@
 // (64 rows a wavefront in one workgroup a CU, half the LDS reads, took the same time.)
 //
 // Three prompts of 19215 tokens in all (32 heads over 8 key heads of 128; 1.05
-// TFLOP): 1091 us, 961 TFLOP/s of the 1330 that a large product reaches; the matrix
-// units are busy 48% of the cycles, and the rest are the weights: 32 exponentials, a
-// maximum and roundings a lane for 32 products, which run beside the other
-// workgroup's products in part only.  Chunks of four sequences (0.2 TFLOP): 287 us,
+// TFLOP): 1070 to 1119 us, 937 to 979 TFLOP/s of the 1330 that a large product reaches;
+// the matrix units are busy 49% of the cycles, and the rest are the weights: 32
+// exponentials, a maximum and roundings a lane for 32 products, which run beside the
+// other workgroup's products in part only.  Chunks of four sequences (0.2 TFLOP): 287 us,
 // 687 TFLOP/s, with uneven last items and the join; decode steps and chunks mixed
 // (32 sequences, 0.51 GB, 0.12 TFLOP): 270 us.
 #include "attend.h"

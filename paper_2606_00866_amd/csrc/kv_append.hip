@@ -242,7 +242,7 @@ extern "C" int mori_kv_append(const mori_pool* pool, uint32_t layer, const mori_
   a.by_units = fast_div(a.units);
   a.by_q = fast_div(a.uq);
   a.by_k = fast_div(a.uk);
-  if ((uint64_t)a.b.T * a.units > (1ull << 32) - NT) return MORI_EINVAL;  // a launch has fewer than 2^32 threads
+  if ((uint64_t)a.b.T * a.units > (1ull << 32) - NT) return MORI_EINVAL;  // a launch has fewer threads than 2^32
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (ap->dtype == MORI_DT_F16) launch<F16>(a, s);
   else launch<BF16>(a, s);

@@ -6,8 +6,11 @@ import torch
 
 from test_attention_host import M, append, attend, pool, rows, tokens  # noqa: F401 (M is a fixture)
 
-if torch.cuda.is_available():
-    pytest.skip("the calls that fit would run", allow_module_level=True)
+
+@pytest.fixture(autouse=True)
+def no_device():
+    if torch.cuda.is_available():
+        pytest.skip("the calls that fit would run")
 
 
 @pytest.mark.parametrize("q_heads", [0, 8])
