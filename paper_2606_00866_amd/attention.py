@@ -104,7 +104,8 @@ class TokenBatch:
         self.error = torch.zeros(1, dtype=torch.int32, device=self.device)
         # Streams other than the one that clears the word wait for that, and check waits for them.
         made = torch.cuda.current_stream(self.device)
-        self._made, self._used, self._last = made.cuda_stream, set(), None
+        self._made, self._last = made.cuda_stream, None
+        self._used, self._ordered = set(), {self._made}
         self._ready = None if torch.cuda.is_current_stream_capturing() else made.record_event()
         self._keep = (tbl_off, tbl, seq_off, kv_len, program)
         self.desc = M.mori_tokens(self.num_seqs, self.num_tokens, int(max_new), int(max_kv), seq_off.data_ptr(),
@@ -129,18 +130,21 @@ class TokenBatch:
 
     def _enter(self, handle: int) -> None:
         """A call is about to use the stream: its first one, or the first after another's."""
-        if handle not in self._used and handle != self._made:
-            stream = torch.cuda.ExternalStream(handle, self.device)
-            with torch.cuda.stream(stream):
-                capturing = torch.cuda.is_current_stream_capturing()
-            if not capturing:  # a graph's inputs are ready before it is replayed
-                if self._ready is not None:
-                    stream.wait_event(self._ready)
-                for x in (self.error, *self._keep):
-                    if x is not None:
-                        x.record_stream(stream)
         self._used.add(handle)
         self._last = handle
+        if handle in self._ordered:
+            return
+        stream = torch.cuda.ExternalStream(handle, self.device)
+        with torch.cuda.stream(stream):
+            if torch.cuda.is_current_stream_capturing():  # a graph's inputs are ready before it is replayed
+                self._last = None
+                return
+        if self._ready is not None:
+            stream.wait_event(self._ready)
+        for x in (self.error, *self._keep):
+            if x is not None:
+                x.record_stream(stream)
+        self._ordered.add(handle)
 
     def check(self) -> None:
         """Raises MoriError if the device found fault with the batch since the last check.
@@ -158,6 +162,7 @@ class TokenBatch:
             self.error.zero_()
             here.synchronize()  # cleared before any stream's next call
         self._used.clear()
+        self._ordered = {self._made}
         self._last = self._ready = None
         if bits:
             raise MoriError("token batch", M.MORI_EDEVICE, bits)

@@ -119,6 +119,35 @@ def test_the_word_outlives_its_batch():
     assert all(int(x) == 0 for x in later)
 
 
+def test_the_word_outlives_its_batch_after_a_capture():
+    """The other stream's first call was captured: its next one is not in the graph."""
+    c, side = Case(), torch.cuda.Stream()
+    b = c.batch()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        c.call("append", b)
+    with torch.cuda.stream(side):
+        c.busy()
+    c.call("append", b, stream=side)
+    del b
+    later = [torch.zeros(1, dtype=torch.int32, device="cuda") for _ in range(64)]
+    torch.cuda.synchronize()
+    assert all(int(x) == 0 for x in later)
+
+
+def test_made_on_a_side_stream():
+    """And used on the default one, at once."""
+    c, side = Case(), torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        c.busy()
+        b = c.batch()
+    c.call("append", b)
+    found(b)
+    c.call("attend", b)
+    with torch.cuda.stream(side):
+        found(b)
+
+
 def test_the_numbers_outlive_their_batch():
     """What ``TokenBatch.of`` copies to the device belongs to the batch alone: dropped while a
     call of another stream is under way, it is read as it was."""
