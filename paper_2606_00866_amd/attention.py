@@ -59,6 +59,12 @@ def _needs_gradients(what: str) -> MoriError:
                      M.MORI_EINVAL)
 
 
+def _stream_at(handle: int, device: torch.device) -> torch.cuda.Stream:
+    """The stream of a handle; that of the default stream is 0, which ExternalStream does
+    not take for it."""
+    return torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device)
+
+
 def _on(stream):
     """Where this module's own allocations belong: the stream that uses them, so
     that the allocator hands their memory on in that stream's order."""
@@ -134,7 +140,7 @@ class TokenBatch:
         self._last = handle
         if handle in self._ordered:
             return
-        stream = torch.cuda.ExternalStream(handle, self.device)
+        stream = _stream_at(handle, self.device)
         with torch.cuda.stream(stream):
             if torch.cuda.is_current_stream_capturing():  # a graph's inputs are ready before it is replayed
                 self._last = None
@@ -156,7 +162,7 @@ class TokenBatch:
             here.wait_event(self._ready)
         for handle in self._used:
             if handle != here.cuda_stream:
-                here.wait_stream(torch.cuda.ExternalStream(handle, self.device))
+                here.wait_stream(_stream_at(handle, self.device))
         bits = int(self.error.item())
         if bits:
             self.error.zero_()

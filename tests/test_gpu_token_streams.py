@@ -136,16 +136,21 @@ def test_the_word_outlives_its_batch_after_a_capture():
 
 
 def test_made_on_a_side_stream():
-    """And used on the default one, at once."""
+    """And used on the default one, at once; what is checked on the side waits for it."""
     c, side = Case(), torch.cuda.Stream()
     with torch.cuda.stream(side):
+        c.batch()  # what a first batch allocates there is there
+        c.busy()
+        torch.cuda.synchronize()
         c.busy()
         b = c.batch()
     c.call("append", b)
     found(b)
+    c.busy()
     c.call("attend", b)
     with torch.cuda.stream(side):
         found(b)
+        b.check()
 
 
 def test_the_numbers_outlive_their_batch():
