@@ -20,8 +20,11 @@
  *                        allocated for them (CPU -> GPU, Sec. 4.1: a CPU-tier
  *                        program resumes over PCIe).
  *
- * Beside them the two calls a model makes on the pool's pages in every layer:
- * mori_kv_append writes new tokens' keys and values, mori_kv_attend reads them.
+ * Beside them the calls of a model's step: mori_tables_grow gives programs that
+ * take new tokens the pages they need, and in every layer mori_kv_append writes
+ * the tokens' keys and values and mori_kv_attend reads them (mori_kv_append_axes and
+ * mori_kv_attend_sight: with positions of several axes, and with more to say of
+ * scores and of what a token sees).
  *
  * Conventions
  *   - Every call returns an int: MORI_OK (0) or a negative MORI_E* code.
@@ -39,8 +42,8 @@
  *     direction has read its address table.
  *   - Threads: a context is driven by one host thread at a time (its calls
  *     are not synchronised against each other); distinct contexts share no
- *     state, and mori_evict_order, mori_replica_admit, mori_kv_append and
- *     mori_kv_attend keep none.
+ *     state, and mori_evict_order, mori_replica_admit, mori_tables_grow and
+ *     the calls on tokens keep none.
  *   - Ownership: the caller owns the pool, the program arrays, the host
  *     buffers and the streams.  The context owns its device scratch, a small
  *     pinned mirror of the plan and, for copy-engine swaps, device staging
@@ -82,7 +85,7 @@ extern "C" {
 #define MORI_DEV_PAGE_DUP 0x020u      /* a page owned twice, or owned and marked free */
 #define MORI_DEV_PAGE_LEAK 0x040u     /* a page neither free nor owned */
 #define MORI_DEV_NONRES_PAGE 0x080u   /* a CPU/Waiting program's table holds a page */
-#define MORI_DEV_NOSPC 0x100u         /* not enough pages (unreachable for a consistent pool) */
+#define MORI_DEV_NOSPC 0x100u         /* not enough pages (plans: unreachable for a consistent pool) or table entries */
 #define MORI_DEV_HOST_ADDR 0x200u     /* swap address not 16-B aligned or outside registered memory */
 #define MORI_DEV_BAD_BLOCK 0x400u     /* eviction order: type label > 2 or last access >= 2^62 */
 #define MORI_DEV_BAD_STATUS 0x800u    /* incremental policy: status value > 2 */
@@ -389,7 +392,7 @@ int mori_evict_order_noalloc(const mori_blocks* blocks, uint32_t tier, uint64_t 
                              uint64_t* prefix, uint32_t* result, void* stream);
 
 /* ---- tokens: writing and reading the pool's pages for a model ------------ */
-/* The two calls a model makes in every layer, on the pages of the GPU-resident
+/* The calls a model makes in every layer, on the pages of the GPU-resident
  * programs: mori_kv_append writes new tokens' keys and values into the pool,
  * mori_kv_attend lets their queries attend to everything the program holds.
  * Both read the same block tables that mori_rank_partition rewrites, in stream
@@ -432,6 +435,69 @@ typedef struct {
   const uint32_t* tbl_off;  /* device [P+1], as in mori_programs */
   const uint32_t* tbl;      /* device [tbl_len] */
 } mori_tokens;
+
+/* Programs that take new tokens: their tables grow by pages of the free map, and
+ * what the batch's calls need is made in the same go, all of it on the device.
+ * Sequence b is new_tokens[b] new tokens of its program, behind the held[p] that it
+ * holds.  Its program gets the pages that are missing for them: the lowest free ids,
+ * in batch order, a sequence's blocks in their order.  Tables stay contiguous:
+ * entries behind a program's move up.  tbl_len bounds the grown tables; entries past
+ * them are left alone.  No page is ever given back (a plan does that).
+ *
+ * What was before (tbl_off, tbl, free_map, held) is read, what is after goes to
+ * tbl_off_to, tbl_to, free_to and held_to: each the array itself (then a captured
+ * graph of steps replays with programs that grow) or one that overlaps no other.
+ * seq_off, kv_len, program and the grown tables are a mori_tokens' arrays.
+ * slots[t] = page * block_tokens + row of token t, positions[t] its position; -1 for
+ * places of the arrays past the batch's tokens.
+ *
+ * All or nothing: where something does not fit, the arrays after are those before,
+ * the batch is empty (offsets and lengths 0, slots and positions -1) and error gets
+ *   MORI_DEV_BAD_TOKENS    a program out of range or twice in the batch, held past the
+ *                          program's blocks, new_tokens above max_new, a length above
+ *                          max_kv, more than num_tokens tokens in all
+ *   MORI_DEV_NOT_RESIDENT  a program whose tier is not MORI_TIER_GPU
+ *   MORI_DEV_NOSPC         too few free pages or table entries
+ *   MORI_DEV_BAD_TBL_OFF   offsets that do not start at 0, decrease or pass tbl_len;
+ *                          tables and offsets after are then not written
+ * An old block of a new token without a page (or with one past the pool) gives slot -1
+ * and MORI_DEV_NOT_RESIDENT (MORI_DEV_PAGE_RANGE); the rest stands.
+ *
+ * Swaps of a plan read its tables and may still be reading pages that it has marked
+ * free: grow once both swaps are enqueued, ordered behind MORI_Q_OUT_EVENT. */
+typedef struct {
+  uint32_t num_seqs;          /* B, 1..MORI_MAX_PROGRAMS */
+  uint32_t num_tokens;        /* T, places of slots and positions */
+  uint32_t max_new, max_kv;   /* as in mori_tokens */
+  const uint32_t* new_tokens; /* device [B] */
+  const uint32_t* program;    /* device [B], or NULL: sequence b is program b */
+  uint32_t num_programs;      /* P, 1..MORI_MAX_PROGRAMS */
+  uint32_t tbl_len;           /* entries allocated in tbl and in tbl_to */
+  const uint8_t* tier;        /* device [P], or NULL: every program is on the GPU */
+  const uint32_t* tbl_off;    /* device [P+1] */
+  const uint32_t* tbl;        /* device [tbl_len] */
+  const uint8_t* free_map;    /* device [num_blocks], 16-B aligned: 0 = in use */
+  const uint32_t* held;       /* device [P] tokens that each program holds */
+  uint32_t* tbl_off_to;
+  uint32_t* tbl_to;
+  uint8_t* free_to;
+  uint32_t* held_to;
+  uint32_t* seq_off;          /* device [B+1] */
+  uint32_t* kv_len;           /* device [B] */
+  int64_t* slots;             /* device [T], or NULL */
+  int32_t* positions;         /* device [T], or NULL */
+} mori_growth;
+
+/* Device workspace mori_tables_grow needs (more where tbl_to is tbl). */
+int mori_tables_grow_workspace(const mori_pool* pool, const mori_growth* growth, uint64_t* bytes);
+
+/* Enqueues the above; of the pool block_tokens (at most 2^18) and num_blocks are read.
+ * workspace: 256-B aligned device memory of at least mori_tables_grow_workspace bytes, used only
+ * while the call's work runs; its contents before do not matter.  *error (device, may
+ * be NULL) collects MORI_DEV_* bits by OR; the caller clears it.  EINVAL: null pointers,
+ * alignment, counts out of range, a short workspace. */
+int mori_tables_grow(const mori_pool* pool, const mori_growth* growth, void* workspace, uint64_t workspace_bytes,
+                     uint32_t* error, void* stream);
 
 /* A [tokens][heads][elements] array of 16-bit floats on the device: element e
  * of head h of token t is at data + 2 * (t * token_stride + h * head_stride + e).

@@ -113,6 +113,7 @@ class TokenBatch:
         self._made, self._last = made.cuda_stream, None
         self._used, self._ordered = set(), {self._made}
         self._ready = None if torch.cuda.is_current_stream_capturing() else made.record_event()
+        self.seq_off, self.kv_len = seq_off, kv_len
         self._keep = (tbl_off, tbl, seq_off, kv_len, program)
         self.desc = M.mori_tokens(self.num_seqs, self.num_tokens, int(max_new), int(max_kv), seq_off.data_ptr(),
                                   kv_len.data_ptr(), program.data_ptr() if program is not None else None,
@@ -172,6 +173,102 @@ class TokenBatch:
         self._last = self._ready = None
         if bits:
             raise MoriError("token batch", M.MORI_EDEVICE, bits)
+
+
+class TokenGrowth:
+    """Programs that take new tokens, counted on the device: their tables grow by pages
+    of the free map, and the batch of those tokens is made, in one call a step.
+
+    tbl_off, tbl, free_map, tier (None: every program is on the GPU): as ``TierPool``
+    keeps them.  held int32 [P]: tokens that each program holds.  new_tokens int32 [B]:
+    those that sequence b brings, to program[b] (int32 [B]; None: program b).
+    num_tokens, max_new, max_kv: bounds of the batch, as in ``TokenBatch``.
+
+    ``run`` reads these tensors as they are then and rewrites tbl_off, tbl, free_map and
+    held in place, or leaves them and writes ``into`` (tbl_off, tbl, free_map, held).  It
+    returns ``batch``, a ``TokenBatch`` over the grown tables, the same one every time;
+    ``slots`` (int64 [num_tokens]: page * block_tokens + row, -1 behind the last token)
+    and ``positions`` (int32) are those of its tokens.  Nothing waits, so a step of run,
+    append and attention can be captured whole and replayed while programs grow.  What
+    does not fit leaves everything as it was and the batch empty; ``batch.check`` says so."""
+
+    def __init__(self, geom, tbl_off: torch.Tensor, tbl: torch.Tensor, free_map: torch.Tensor, held: torch.Tensor,
+                 new_tokens: torch.Tensor, program: torch.Tensor | None = None, *, tier: torch.Tensor | None = None,
+                 num_tokens: int, max_new: int, max_kv: int, into: tuple | None = None):
+        P, B, dev = int(tbl_off.numel()) - 1, int(new_tokens.numel()), new_tokens.device
+        to = tuple(into) if into is not None else (tbl_off, tbl, free_map, held)
+        _need(len(to) == 4, "TokenGrowth: into is (tbl_off, tbl, free_map, held)")
+        for name, x, n, dtype in (
+                ("tbl_off", tbl_off, P + 1, torch.int32), ("tbl", tbl, None, torch.int32),
+                ("free_map", free_map, geom.num_blocks, torch.uint8), ("held", held, P, torch.int32),
+                ("new_tokens", new_tokens, B, torch.int32), ("program", program, B, torch.int32),
+                ("tier", tier, P, torch.uint8), ("into[0]", to[0], P + 1, torch.int32),
+                ("into[1]", to[1], tbl.numel(), torch.int32), ("into[2]", to[2], geom.num_blocks, torch.uint8),
+                ("into[3]", to[3], P, torch.int32)):
+            if x is None and name in ("program", "tier"):
+                continue
+            _need(x.dtype == dtype and x.is_contiguous() and x.dim() == 1 and x.device == dev,
+                  f"TokenGrowth: {name} is a contiguous {dtype} vector on new_tokens' device")
+            _need(n is None or x.numel() == n, f"TokenGrowth: {name} has {x.numel()} entries, not {n}")
+        _need(0 < P <= M.MORI_MAX_PROGRAMS and 0 < B <= M.MORI_MAX_PROGRAMS and (program is not None or B <= P),
+              "TokenGrowth: programs or sequences out of range")
+        _need(0 <= num_tokens < 1 << 31, "TokenGrowth: bounds out of range")
+        _need(_apart(to, (tbl_off, tbl, free_map, held), [x for x in (new_tokens, program, tier) if x is not None]),
+              "TokenGrowth: into is the tensors themselves or some that overlap no others")
+        self.slots = torch.empty(num_tokens, dtype=torch.int64, device=dev)
+        self.positions = torch.empty(num_tokens, dtype=torch.int32, device=dev)
+        with torch.cuda.device(dev):
+            self.batch = TokenBatch(geom, to[0], to[1], torch.zeros(B + 1, dtype=torch.int32, device=dev),
+                                    torch.zeros(B, dtype=torch.int32, device=dev), program, num_tokens=num_tokens,
+                                    max_new=max_new, max_kv=max_kv)
+        self.desc = M.mori_growth(
+            B, int(num_tokens), int(max_new), int(max_kv), new_tokens.data_ptr(),
+            program.data_ptr() if program is not None else None, P, tbl.numel(),
+            tier.data_ptr() if tier is not None else None, tbl_off.data_ptr(), tbl.data_ptr(), free_map.data_ptr(),
+            held.data_ptr(), *(x.data_ptr() for x in to), self.batch.seq_off.data_ptr(), self.batch.kv_len.data_ptr(),
+            self.slots.data_ptr() or None, self.positions.data_ptr() or None)
+        self._pool = _empty_pool(geom)
+        rc, n = M.mori_tables_grow_workspace(self._pool, self.desc)
+        check(rc, "mori_tables_grow_workspace")
+        self._workspace = torch.empty(n, dtype=torch.uint8, device=dev)
+        # other streams' calls keep all of it from reuse
+        self.batch._keep += (tbl_off, tbl, free_map, held, new_tokens, tier, *to[2:], self.slots, self.positions,
+                             self._workspace)
+        self._written = (*to, self.batch.seq_off, self.batch.kv_len, self.slots, self.positions)
+
+    @classmethod
+    def of(cls, tier_pool, held: torch.Tensor, new_tokens: torch.Tensor, program: torch.Tensor | None = None, *,
+           num_tokens: int, max_new: int, max_kv: int) -> "TokenGrowth":
+        """Of a ``TierPool``'s programs, in place; those on the GPU grow.  Make room in the
+        table first (``TierPool.reserve``), and run it when a step's swaps have ended."""
+        tier_pool.grows = True  # its sizes are read back before the next swaps
+        return cls(tier_pool.geom, tier_pool.tbl_off, tier_pool.tbl, tier_pool.free_map, held, new_tokens, program,
+                   tier=tier_pool.tier, num_tokens=num_tokens, max_new=max_new, max_kv=max_kv)
+
+    def run(self, stream=None) -> TokenBatch:
+        """Calls that may overlap, on other streams, need a growth each (and tables)."""
+        batch = self.batch
+        if _current_device() != batch.index:  # launches go to the current device
+            with torch.cuda.device(batch.index):
+                return self.run(stream)
+        check(M.mori_tables_grow(self._pool, self.desc, self._workspace.data_ptr(), self._workspace.nbytes,
+                                 batch.error.data_ptr(), _stream_of(batch, stream)), "mori_tables_grow")
+        torch.autograd.graph.increment_version(self._written)
+        return batch
+
+
+def _apart(to, before, others) -> bool:
+    """Whether every tensor of `to` is its counterpart or overlaps nothing else."""
+    span = lambda x: (x.data_ptr(), x.data_ptr() + x.nbytes)
+    for i, x in enumerate(to):
+        lo, hi = span(x)
+        for j, y in enumerate((*before, *others, *to[:i])):
+            if j == i and (lo, hi) == span(y):
+                continue
+            a, b = span(y)
+            if lo < b and a < hi:
+                return False
+    return True
 
 
 def _same_geometry(geom, batch: TokenBatch) -> None:

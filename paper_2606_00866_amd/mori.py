@@ -40,7 +40,7 @@ EXPORTS = ("mori_create", "mori_destroy", "mori_register", "mori_host_alloc", "m
            "mori_rank_partition", "mori_plan_wait", "mori_kv_swap_out", "mori_kv_swap_in", "mori_query",
            "mori_strerror", "mori_profile", "mori_profile_read", "mori_evict_workspace", "mori_evict_order",
            "mori_replica_admit", "mori_evict_order_noalloc", "mori_kv_append", "mori_kv_attend_workspace",
-           "mori_kv_attend")
+           "mori_kv_attend", "mori_tables_grow_workspace", "mori_tables_grow")
 
 
 class mori_pool(C.Structure):
@@ -68,6 +68,13 @@ class mori_tokens(C.Structure):
     _fields_ = [("num_seqs", C.c_uint32), ("num_tokens", C.c_uint32), ("max_new", C.c_uint32), ("max_kv", C.c_uint32),
                 ("seq_off", C.c_void_p), ("kv_len", C.c_void_p), ("program", C.c_void_p), ("num_programs", C.c_uint32),
                 ("tbl_len", C.c_uint32), ("tbl_off", C.c_void_p), ("tbl", C.c_void_p)]
+
+
+class mori_growth(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("num_seqs", "num_tokens", "max_new", "max_kv")] + [
+        ("new_tokens", C.c_void_p), ("program", C.c_void_p), ("num_programs", C.c_uint32), ("tbl_len", C.c_uint32)] + [
+        (n, C.c_void_p) for n in ("tier", "tbl_off", "tbl", "free_map", "held", "tbl_off_to", "tbl_to", "free_to",
+                                  "held_to", "seq_off", "kv_len", "slots", "positions")]
 
 
 class mori_rows(C.Structure):
@@ -129,6 +136,8 @@ def lib():
         L.mori_kv_append.argtypes = [PP, U32, PT, C.POINTER(mori_append), V, V]
         L.mori_kv_attend_workspace.argtypes = [PP, PT, C.POINTER(mori_attend), C.POINTER(U64)]
         L.mori_kv_attend.argtypes = [PP, U32, PT, C.POINTER(mori_attend), V, U64, V, V]
+        L.mori_tables_grow_workspace.argtypes = [PP, C.POINTER(mori_growth), C.POINTER(U64)]
+        L.mori_tables_grow.argtypes = [PP, C.POINTER(mori_growth), V, U64, V, V]
         L.mori_strerror.restype = C.c_char_p
         for name in EXPORTS:
             if name != "mori_strerror":
@@ -236,6 +245,18 @@ def mori_kv_attend(pool: mori_pool, layer: int, tokens: mori_tokens, attend: mor
                    workspace_bytes: int, error: int = 0, stream: int = 0) -> int:
     return lib().mori_kv_attend(C.byref(pool), layer, C.byref(tokens), C.byref(attend), workspace or None,
                                 workspace_bytes, error or None, stream)
+
+
+def mori_tables_grow_workspace(pool: mori_pool, growth: mori_growth):
+    b = C.c_uint64()
+    rc = lib().mori_tables_grow_workspace(C.byref(pool), C.byref(growth), C.byref(b))
+    return rc, b.value
+
+
+def mori_tables_grow(pool: mori_pool, growth: mori_growth, workspace: int, workspace_bytes: int, error: int = 0,
+                     stream: int = 0) -> int:
+    return lib().mori_tables_grow(C.byref(pool), C.byref(growth), workspace or None, workspace_bytes, error or None,
+                                  stream)
 
 
 def mori_replica_admit(bytes_, idleness, status, room, flags: int = 0):

@@ -163,6 +163,20 @@ class TierPool:
         check(M.mori_register(self.ctx, self.arena.ptr, self.arena.nbytes), "mori_register(arena)")
         self._keep = []
         self.plan = None
+        self.grows = False  # programs' sizes change on the device
+
+    def reserve(self, entries: int) -> None:
+        """Room for `entries` table entries in all, for programs that grow.  The table moves:
+        batches made before keep the old one."""
+        if entries > self.tbl.numel():
+            more = torch.full((entries,), -1, dtype=torch.int32, device=self.device)
+            more[:self.tbl_len] = self.tbl[:self.tbl_len]
+            self.tbl = more
+        self.tbl_len = max(self.tbl_len, entries)
+
+    def read_sizes(self) -> None:
+        """The programs' blocks as the device has them now (waits for the current stream)."""
+        self.nblk = np.diff(self.tbl_off.cpu().numpy().view(np.uint32).astype(np.int64))
 
     # ---- host extents -------------------------------------------------------
     def program_bytes(self, p: int) -> int:
@@ -245,6 +259,8 @@ class TierPool:
         rc, p = self.plan_wait()
         if rc != M.MORI_OK:
             raise MoriError("mori_plan_wait", rc, p.device_error)
+        if self.grows:
+            self.read_sizes()
         self.place_host_buffers()
         check(self.swap_out(mode, s_out), "mori_kv_swap_out")
         check(self.swap_in(mode, s_in if s_in is not None else s_out), "mori_kv_swap_in")
