@@ -11,20 +11,22 @@
 // Two launches, bound by their latency and dependent reads: a byte of the free map per
 // page, an entry of the tables in and out, 12 bytes a token.
 //   grow_count   one workgroup checks and scans the sequences and programs; the others
-//                count free pages by tiles of 4096 and, where the tables grow in place,
+//                count free pages, 512 at a time, and, where the tables grow in place,
 //                copy the old entries aside
 //   grow_assign  workgroups take a tile each (pages to table entries and to the slots of
 //                the tokens in new blocks), or old entries (to where they lie now), or
 //                tokens in old blocks, or programs.  Every workgroup sums the tile counts
 //                for itself, so all of them know whether there are pages enough: nothing
 //                is changed unless everything is.
+#include <algorithm>
+
 #include "tokens.h"
 
 namespace mori {
 namespace {
 
-constexpr uint32_t TILE = 4096;    // pages of a workgroup of grow_assign, 16 a thread
-constexpr uint32_t COUNT_NT = 1024, NT = 256;
+constexpr uint32_t NT = 256;
+constexpr uint32_t COUNTED = 512;   // pages of a count: the smallest tile
 constexpr uint32_t ENTRIES = 1024;  // table entries of a workgroup
 constexpr uint32_t MOST = MORI_MAX_PROGRAMS;
 
@@ -37,7 +39,7 @@ struct Head {
 };
 
 struct GrowArgs {
-  uint32_t B, T, max_new, max_kv, P, tbl_len, bt, num_blocks, ntiles;
+  uint32_t B, T, max_new, max_kv, P, tbl_len, bt, num_blocks, counts, ntiles, tile;
   FastDiv by_bt;
   const uint32_t *new_tokens, *program;
   const uint8_t* tier;
@@ -56,216 +58,211 @@ struct GrowArgs {
   uint32_t* aside;
 };
 
-// Sums of every thread's value before it (by thread) and of all; a workgroup of up to
-// 16 wavefronts, all of it here.
-struct Scan {
-  uint32_t before, total;
-};
-__device__ inline Scan scan_of(uint32_t v, uint32_t* s_wave, uint32_t waves) {
-  const uint32_t lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  const uint32_t in = wave::incl_add(v);
-  if (lane == 63) s_wave[wv] = in;
-  __syncthreads();
-  Scan s{in - v, 0};
-  for (uint32_t i = 0; i < waves; ++i) {
-    const uint32_t x = s_wave[i];
-    if (i < wv) s.before += x;
-    s.total += x;
-  }
-  __syncthreads();
-  return s;
-}
-
-// Bytes that are not 0.
+// Bytes that are not 0, a bit for each.
 __device__ inline uint32_t set_bytes(uint32_t w) {
   return (((w & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | w) & 0x80808080u;
 }
 
-// 16 pages of the free map from `page` on; those past the pool are not free.
-__device__ inline uint4 free_pages(const GrowArgs& a, uint32_t page) {
-  if ((uint64_t)page + 16 <= a.num_blocks) return *reinterpret_cast<const uint4*>(a.free_map + page);
-  uint32_t w[4] = {0, 0, 0, 0};
+// N pages of the free map from `page` on (N = 2 or 16, a multiple of it), 4 a word; those
+// past the pool are not free.
+template <int N>
+struct Pages {
+  static constexpr int W = N < 4 ? 1 : N / 4;
+  uint32_t w[W];
+  __device__ __forceinline__ void load(const uint8_t* map, uint32_t num_blocks, uint64_t page) {
+    if (page + N <= num_blocks) {
+      if constexpr (N == 2) {
+        w[0] = *reinterpret_cast<const uint16_t*>(map + page);
+      } else {
+        const uint4 x = *reinterpret_cast<const uint4*>(map + page);
+        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+      }
+      return;
+    }
 #pragma unroll
-  for (uint32_t i = 0; i < 16; ++i)
-    if ((uint64_t)page + i < a.num_blocks) w[i / 4] |= (uint32_t)a.free_map[page + i] << (8 * (i % 4));
-  return uint4{w[0], w[1], w[2], w[3]};
-}
-__device__ inline uint32_t count_set(uint4 w) {
-  return __popc(set_bytes(w.x)) + __popc(set_bytes(w.y)) + __popc(set_bytes(w.z)) + __popc(set_bytes(w.w));
-}
+    for (int i = 0; i < W; ++i) w[i] = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (page + i < num_blocks) w[i / 4] |= (uint32_t)map[page + i] << (8 * (i % 4));
+  }
+  __device__ __forceinline__ void store(uint8_t* map, uint32_t num_blocks, uint64_t page) const {
+    if (page + N <= num_blocks) {
+      if constexpr (N == 2) *reinterpret_cast<uint16_t*>(map + page) = (uint16_t)w[0];
+      else *reinterpret_cast<uint4*>(map + page) = uint4{w[0], w[1], w[2], w[3]};
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (page + i < num_blocks) map[page + i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
+  }
+  __device__ __forceinline__ uint32_t count() const {
+    uint32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) n += __popc(set_bytes(w[i]));
+    return n;
+  }
+};
 
-// The batch and the programs: checks, scans, and what grow_assign reads of them.
+// The batch and the programs: checks, scans, and what grow_assign reads of them.  One
+// workgroup of W threads, K neighbouring programs and sequences each: every read of global
+// memory is under way before the first barrier, the rest is in LDS and three barriers long.
+// Sums are of 64 bits, so none wraps unseen; where something does not fit, what is written
+// here is not used.
+template <int W, int K>
 __device__ void scan_batch(const GrowArgs& a) {
-  constexpr uint32_t K = MOST / COUNT_NT;
-  __shared__ uint32_t s_more[MOST], s_len[MOST];  // by program; NONE: no sequence of the batch
-  __shared__ uint32_t s_wave[COUNT_NT / 64], s_error;
-  constexpr uint32_t NONE = 0xFFFFFFFFu, CLAIMED = 0xFFFFFFFEu;
-  const uint32_t tid = threadIdx.x;
-  uint32_t err = 0, bad_off = 0;
-  if (tid == 0) s_error = 0;
-  for (uint32_t p = tid; p < a.P; p += COUNT_NT) s_more[p] = NONE;
-  // neighbouring programs and sequences a thread
-  uint32_t lo[K], hi[K], n[K], prog[K], more[K], len[K];
+  constexpr uint32_t WAVES = W / 64, NONE = 0xFFFFFFFFu, CLAIMED = 0xFFFFFFFEu;
+  __shared__ uint32_t s_more[W * K], s_len[W * K], s_held[W * K], s_blocks[W * K];  // by program
+  __shared__ uint8_t s_tier[W * K];
+  __shared__ uint64_t s_n[WAVES], s_m[WAVES], s_e[WAVES];
+  __shared__ uint32_t s_error[WAVES], s_bad[WAVES];
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  uint32_t lo[K], blocks[K], held[K], n[K], prog[K], bad = 0, err = 0;
 #pragma unroll
-  for (uint32_t k = 0; k < K; ++k) {
+  for (int k = 0; k < K; ++k) {
     const uint32_t p = K * tid + k;
-    lo[k] = hi[k] = 0;
+    prog[k] = p < a.B ? a.program ? a.program[p] : p : NONE;
+    n[k] = p < a.B ? a.new_tokens[p] : 0;
+    lo[k] = blocks[k] = held[k] = 0;
+    s_more[p] = NONE;
     if (p < a.P) {
       lo[k] = a.tbl_off[p];
-      hi[k] = a.tbl_off[p + 1];
-      bad_off |= lo[k] > hi[k] || hi[k] > a.tbl_len || (p == 0 && lo[k]);
+      const uint32_t hi = a.tbl_off[p + 1];
+      held[k] = a.held[p];
+      s_tier[p] = a.tier ? a.tier[p] : (uint8_t)MORI_TIER_GPU;
+      bad |= lo[k] > hi || hi > a.tbl_len || (p == 0 && lo[k]);
+      blocks[k] = hi - lo[k];
+      s_held[p] = held[k];
+      s_blocks[p] = blocks[k];
     }
   }
+  bad = __ballot(bad) != 0;
+  if (lane == 0) s_bad[wv] = bad;
   __syncthreads();
-  const bool sound = !__syncthreads_or(bad_off);
-  if (!sound) err |= MORI_DEV_BAD_TBL_OFF;
+  uint32_t more[K], len[K];
+  uint64_t v = 0, m = 0;
 #pragma unroll
-  for (uint32_t k = 0; k < K; ++k) {
-    const uint32_t b = K * tid + k;
-    n[k] = more[k] = len[k] = 0;
-    prog[k] = NONE;
-    if (b >= a.B) continue;
-    const uint32_t p = a.program ? a.program[b] : b, x = a.new_tokens[b];
+  for (int k = 0; k < K; ++k) {
+    const uint32_t p = prog[k], x = n[k];
+    more[k] = len[k] = n[k] = 0;
+    if (K * tid + k >= a.B) continue;
     if (p >= a.P || atomicCAS(&s_more[p], NONE, CLAIMED) != NONE) {  // no program, or one that is here already
       err |= MORI_DEV_BAD_TOKENS;
       continue;
     }
-    prog[k] = p;
-    const uint32_t h = a.held[p], blocks = sound ? a.tbl_off[p + 1] - a.tbl_off[p] : 0;
-    if (a.tier && a.tier[p] != MORI_TIER_GPU) err |= MORI_DEV_NOT_RESIDENT;
-    if (x > a.max_new || (uint64_t)h + x > a.max_kv || h > (uint64_t)blocks * a.bt) {
+    const uint32_t h = s_held[p], have = s_blocks[p];
+    if (s_tier[p] != MORI_TIER_GPU) err |= MORI_DEV_NOT_RESIDENT;
+    if (x > a.max_new || (uint64_t)h + x > a.max_kv || h > (uint64_t)have * a.bt) {
       err |= MORI_DEV_BAD_TOKENS;
       continue;
     }
     n[k] = x;
-    len[k] = h + x;  // below 2^31
+    len[k] = h + x;  // with the rounding below 2^31
     const uint32_t need = divide(len[k] + a.bt - 1, a.by_bt);
-    more[k] = need > blocks ? need - blocks : 0;
+    more[k] = need > have ? need - have : 0;
+    s_more[p] = more[k];
+    s_len[p] = len[k];
+    v += x;
+    m += more[k];
+  }
+  const uint64_t v_in = wave::incl_add(v), m_in = wave::incl_add(m);
+  err = wave::all_or(err);
+  if (lane == 63) {
+    s_n[wv] = v_in;
+    s_m[wv] = m_in;
+    s_error[wv] = err;
   }
   __syncthreads();
+  uint64_t e = 0;
+  uint32_t grown[K];
 #pragma unroll
-  for (uint32_t k = 0; k < K; ++k)
-    if (prog[k] != NONE) {
-      s_more[prog[k]] = more[k];
-      s_len[prog[k]] = len[k];
-    }
-  // sums in 64 bits first, so that none wraps unseen
-  uint64_t n_sum = 0, m_sum = 0, e_sum = 0;
-#pragma unroll
-  for (uint32_t k = 0; k < K; ++k) {
-    n_sum += n[k];
-    m_sum += more[k];
-  }
-  __shared__ uint64_t s_n, s_m, s_e;
-  if (tid == 0) s_n = s_m = s_e = 0;
-  __syncthreads();
-#pragma unroll
-  for (uint32_t k = 0; k < K; ++k) {
+  for (int k = 0; k < K; ++k) {
     const uint32_t p = K * tid + k;
+    grown[k] = 0;
     if (p < a.P) {
-      const uint32_t m = s_more[p];
-      hi[k] -= lo[k];  // blocks from here on
-      e_sum += (uint64_t)(sound ? hi[k] : 0) + (m < CLAIMED ? m : 0);
-    }
-  }
-  n_sum = wave::sum(n_sum);
-  m_sum = wave::sum(m_sum);
-  e_sum = wave::sum(e_sum);
-  if ((tid & 63) == 0) {
-    atomicAdd(reinterpret_cast<unsigned long long*>(&s_n), n_sum);
-    atomicAdd(reinterpret_cast<unsigned long long*>(&s_m), m_sum);
-    atomicAdd(reinterpret_cast<unsigned long long*>(&s_e), e_sum);
-  }
-  __syncthreads();
-  if (s_n > a.T) err |= MORI_DEV_BAD_TOKENS;
-  if (s_m > a.num_blocks || s_e > a.tbl_len) err |= MORI_DEV_NOSPC;
-  if (err) atomicOr(&s_error, err);
-  __syncthreads();
-  const uint32_t error = s_error;
-  if (error) {  // nothing grows
-#pragma unroll
-    for (uint32_t k = 0; k < K; ++k) n[k] = more[k] = len[k] = 0;
-  }
-  uint32_t v = 0, w = 0;
-#pragma unroll
-  for (uint32_t k = 0; k < K; ++k) {
-    v += n[k];
-    w += more[k];
-  }
-  const Scan t = scan_of(v, s_wave, COUNT_NT / 64), m = scan_of(w, s_wave, COUNT_NT / 64);
-  v = t.before;
-  w = m.before;
-#pragma unroll
-  for (uint32_t k = 0; k < K; ++k) {
-    const uint32_t b = K * tid + k;
-    if (b < a.B) {
-      a.tok[b] = v;
-      a.ahead[b] = w;
-      a.len[b] = len[k];
-      a.prog[b] = prog[k];
-    }
-    v += n[k];
-    w += more[k];
-  }
-  uint32_t e = 0;
-#pragma unroll
-  for (uint32_t k = 0; k < K; ++k) {
-    const uint32_t p = K * tid + k;
-    more[k] = 0;
-    if (p < a.P && sound) {
       const uint32_t x = s_more[p];
-      more[k] = hi[k] + (x < CLAIMED && !error ? x : 0);
+      const bool takes = x < CLAIMED;
+      grown[k] = blocks[k] + (takes ? x : 0);
+      a.held_new[p] = takes ? s_len[p] : held[k];
     }
-    e += more[k];
+    e += grown[k];
   }
-  const Scan all = scan_of(e, s_wave, COUNT_NT / 64);
-  e = all.before;
+  const uint64_t e_in = wave::incl_add(e);
+  if (lane == 63) s_e[wv] = e_in;
+  __syncthreads();
+  v = v_in - v;
+  m = m_in - m;
+  e = e_in - e;
+  uint64_t v_all = 0, m_all = 0, e_all = 0;
+  bad = 0;
+#pragma unroll 2
+  for (uint32_t i = 0; i < WAVES; ++i) {
+    if (i < wv) {
+      v += s_n[i];
+      m += s_m[i];
+      e += s_e[i];
+    }
+    v_all += s_n[i];
+    m_all += s_m[i];
+    e_all += s_e[i];
+    err |= s_error[i];
+    bad |= s_bad[i];
+  }
+  if (v_all > a.T) err |= MORI_DEV_BAD_TOKENS;
+  if (bad) err |= MORI_DEV_BAD_TBL_OFF;
+  else if (m_all > a.num_blocks || e_all > a.tbl_len) err |= MORI_DEV_NOSPC;
 #pragma unroll
-  for (uint32_t k = 0; k < K; ++k) {
-    const uint32_t p = K * tid + k;
-    if (p < a.P) {
-      a.new_off[p] = e;
-      a.old_off[p] = lo[k];
-      a.held_new[p] = s_more[p] < CLAIMED && !error ? s_len[p] : a.held[p];
+  for (int k = 0; k < K; ++k) {
+    const uint32_t i = K * tid + k;
+    if (i < a.B) {
+      a.tok[i] = (uint32_t)v;
+      a.ahead[i] = (uint32_t)m;
+      a.len[i] = len[k];
+      a.prog[i] = prog[k];
     }
-    e += more[k];
-    if (p == a.P - 1) {
-      a.new_off[a.P] = e;
-      a.old_off[a.P] = lo[k] + hi[k];
-      *a.head = Head{error, m.total, t.total, sound ? lo[k] + hi[k] : 0, sound};
+    v += n[k];
+    m += more[k];
+    if (i < a.P) {
+      a.new_off[i] = (uint32_t)e;
+      a.old_off[i] = lo[k];
+      if (i == a.P - 1) {
+        a.new_off[a.P] = (uint32_t)e + grown[k];
+        a.old_off[a.P] = lo[k] + blocks[k];
+        *a.head = Head{err, (uint32_t)m_all, (uint32_t)v_all, bad ? 0 : lo[k] + blocks[k], !bad};
+        a.tok[a.B] = (uint32_t)v_all;
+        a.ahead[a.B] = (uint32_t)m_all;
+        if (err && a.error) atomicOr(a.error, err);
+      }
     }
-  }
-  if (tid == 0) {
-    a.tok[a.B] = t.total;
-    a.ahead[a.B] = m.total;
-    if (error && a.error) atomicOr(a.error, error);
+    e += grown[k];
   }
 }
 
-__global__ __launch_bounds__(COUNT_NT) void grow_count_kernel(GrowArgs a) {
+template <int W, int K>
+__global__ __launch_bounds__(W) void grow_count_kernel(GrowArgs a) {
   if (blockIdx.x == 0) {
-    scan_batch(a);
+    scan_batch<W, K>(a);
     return;
   }
   const uint32_t tid = threadIdx.x, i = blockIdx.x - 1;
   if (i < a.copies) {
     const uint32_t n = min(a.tbl_off[a.P], a.tbl_len);
-    const uint64_t e0 = (uint64_t)i * (4 * COUNT_NT) + tid;
+    const uint64_t e0 = (uint64_t)i * ENTRIES + tid;
 #pragma unroll
-    for (uint32_t k = 0; k < 4; ++k)
-      if (e0 + k * COUNT_NT < n) a.aside[e0 + k * COUNT_NT] = a.tbl[e0 + k * COUNT_NT];
+    for (uint32_t k = 0; k < ENTRIES / W; ++k)
+      if (e0 + k * W < n) a.aside[e0 + k * W] = a.tbl[e0 + k * W];
     return;
   }
-  // four tiles, four wavefronts each
-  __shared__ uint32_t s_count[COUNT_NT / 64];
-  const uint32_t tile0 = (i - a.copies) * (COUNT_NT / NT);
-  const uint64_t page = (uint64_t)tile0 * TILE + 16ull * tid;
-  const uint32_t n = page < a.num_blocks ? count_set(free_pages(a, (uint32_t)page)) : 0;
-  const uint32_t sum = wave::sum(n);
-  if ((tid & 63) == 0) s_count[tid >> 6] = sum;
-  __syncthreads();
-  if (tid < COUNT_NT / NT && tile0 + tid < a.ntiles)
-    a.tile_cnt[tile0 + tid] = s_count[4 * tid] + s_count[4 * tid + 1] + s_count[4 * tid + 2] + s_count[4 * tid + 3];
+  // a wavefront takes 1024 pages: two small tiles or a quarter of a large one
+  const uint64_t page = ((uint64_t)(i - a.copies) * W + tid) * 16;
+  Pages<16> x;
+  x.load(a.free_map, a.num_blocks, page);
+  const uint32_t in = wave::incl_add(x.count());
+  const uint64_t at = page / 1024;
+  if ((tid & 31) == 31) {
+    const uint32_t half = tid & 32 ? in - (uint32_t)__builtin_amdgcn_readlane((int)in, 31) : in;
+    const uint64_t c = 2 * at + (tid & 32 ? 1 : 0);
+    if (c < a.counts) a.tile_cnt[c] = half;
+  }
 }
 
 // The last of x[0..n-1] (ascending, x[0] <= v) that is not above v: 64 of them at a time.
@@ -290,65 +287,69 @@ __device__ inline uint32_t last_not_above(const uint32_t* x, uint32_t lo, uint32
   return lo;
 }
 
-// A tile's pages: to the programs that take them, and out of the free map.
+// A tile's pages, N a thread: to the programs that take them, and out of the free map.
+template <int N>
 __device__ void assign_tile(const GrowArgs& a, const Head& h, bool ok, uint32_t tile, uint32_t base) {
-  __shared__ uint32_t s_page[TILE], s_seq[TILE], s_ahead[MOST + 1], s_wave[NT / 64];
-  const uint32_t tid = threadIdx.x;
-  const uint64_t page0 = (uint64_t)tile * TILE + 16ull * tid;
-  uint4 w{0, 0, 0, 0};
-  if (page0 < a.num_blocks) w = free_pages(a, (uint32_t)page0);
-  const uint32_t mine = count_set(w), more = ok ? h.more : 0;
-  const bool some = base < more;  // of this tile's pages some are taken
+  constexpr uint32_t TILE = N * NT;
+  struct Taken {
+    uint32_t page, pos, rows;  // position of its first token, tokens in it
+    uint32_t t;                // index of its first token in the batch
+  };
+  __shared__ Taken s_taken[TILE];
+  __shared__ uint32_t s_ahead[MOST], s_wave[NT / 64];
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const uint64_t page0 = (uint64_t)tile * TILE + (uint64_t)N * tid;
+  const uint32_t more = ok ? h.more : 0;
+  const bool some = base < more;  // pages from here on are taken
+  if (!some && a.free_to == a.free_map) return;
+  Pages<N> x;
+  x.load(a.free_map, a.num_blocks, page0);
   if (some) {
-    for (uint32_t b = tid; b <= a.B; b += NT) s_ahead[b] = a.ahead[b];
-    const Scan s = scan_of(mine, s_wave, NT / 64);
-    uint32_t r = base + s.before;
-    uint32_t v[4] = {w.x, w.y, w.z, w.w};
+    for (uint32_t b = tid; b < a.B; b += NT) s_ahead[b] = a.ahead[b];
+    const uint32_t mine = x.count(), in = wave::incl_add(mine);
+    if (lane == 63) s_wave[wv] = in;
+    __syncthreads();
+    uint32_t r = in - mine, count = 0;  // index among the tile's free pages
 #pragma unroll
-    for (uint32_t i = 0; i < 16; ++i) {
-      const uint32_t bit = 0xFFu << (8 * (i % 4));
-      if (v[i / 4] & bit) {
-        if (r < more) {
-          s_page[r - base] = (uint32_t)page0 + i;
-          v[i / 4] &= ~bit;
+    for (uint32_t i = 0; i < NT / 64; ++i) {
+      if (i < wv) r += s_wave[i];
+      count += s_wave[i];
+    }
+    count = min(count, more - base);
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) {
+      const uint32_t byte = 0xFFu << (8 * (i % 4));
+      if (x.w[i / 4] & byte) {
+        if (r < count) {
+          s_taken[r].page = (uint32_t)page0 + i;
+          x.w[i / 4] &= ~byte;
         }
         ++r;
       }
     }
-    w = uint4{v[0], v[1], v[2], v[3]};
     __syncthreads();
-    const uint32_t count = min(more - base, s.total);
     for (uint32_t i = tid; i < count; i += NT) {
       // sequences that take none share their number with the next: the last of them takes it
       const uint32_t b = last_not_above(s_ahead, 0, a.B - 1, base + i), p = a.prog[b];
-      s_seq[i] = b;
       const uint32_t block = a.old_off[p + 1] - a.old_off[p] + (base + i - s_ahead[b]);
-      a.tbl_to[a.new_off[p] + block] = s_page[i];
+      const uint32_t pos = block * a.bt, len = a.len[b];  // the block holds a token: pos < len
+      a.tbl_to[a.new_off[p] + block] = s_taken[i].page;
+      s_taken[i].pos = pos;
+      s_taken[i].rows = min(a.bt, len - pos);
+      s_taken[i].t = a.tok[b + 1] - (len - pos);
     }
     __syncthreads();
     if (a.slots || a.positions) {  // every token of a new block is new
-      for (uint32_t x = tid; x < count * a.bt; x += NT) {  // below 2^30
-        const uint32_t i = divide(x, a.by_bt), row = x - i * a.bt, b = s_seq[i], p = a.prog[b];
-        const uint32_t block = a.old_off[p + 1] - a.old_off[p] + (base + i - s_ahead[b]);
-        const uint64_t pos = (uint64_t)block * a.bt + row;
-        const uint32_t len = a.len[b], held = len - (a.tok[b + 1] - a.tok[b]);
-        if (pos >= len) continue;
-        const uint32_t t = a.tok[b] + ((uint32_t)pos - held);
-        if (a.slots) a.slots[t] = (int64_t)((uint64_t)s_page[i] * a.bt + row);
-        if (a.positions) a.positions[t] = (int32_t)pos;
+      for (uint32_t y = tid; y < count * a.bt; y += NT) {  // below 2^30
+        const uint32_t i = divide(y, a.by_bt), row = y - i * a.bt;
+        const Taken k = s_taken[i];
+        if (row >= k.rows) continue;
+        if (a.slots) a.slots[k.t + row] = (int64_t)((uint64_t)k.page * a.bt + row);
+        if (a.positions) a.positions[k.t + row] = (int32_t)(k.pos + row);
       }
     }
   }
-  if (page0 < a.num_blocks && (some || a.free_to != a.free_map)) {
-    if (page0 + 16 <= a.num_blocks) {
-      *reinterpret_cast<uint4*>(a.free_to + page0) = w;
-    } else {
-      const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-      for (uint32_t i = 0; i < 16; ++i)
-        if (page0 + i < a.num_blocks) a.free_to[page0 + i] = (uint8_t)(v[i / 4] >> (8 * (i % 4)));
-    }
-  }
+  x.store(a.free_to, a.num_blocks, page0);
 }
 
 // Old entries to where they lie now.
@@ -395,6 +396,7 @@ __device__ void place_tokens(const GrowArgs& a, const Head& h, bool ok, uint32_t
   if (a.positions) a.positions[t] = at;
 }
 
+template <int N>
 __global__ __launch_bounds__(NT) void grow_assign_kernel(GrowArgs a, uint32_t movers, uint32_t placers) {
   __shared__ uint32_t s_before[NT / 64], s_total[NT / 64];
   const uint32_t tid = threadIdx.x, lane = tid & 63;
@@ -403,10 +405,11 @@ __global__ __launch_bounds__(NT) void grow_assign_kernel(GrowArgs a, uint32_t mo
   // free pages in the tiles before this one and in all; neither is needed where nothing is taken
   uint32_t before = 0, total = 0;
   if (h.more) {
-    for (uint32_t k = tid; k < a.ntiles; k += NT) {
+    const uint64_t mine = (uint64_t)i * (a.tile / COUNTED);
+    for (uint32_t k = tid; k < a.counts; k += NT) {
       const uint32_t n = a.tile_cnt[k];
       total += n;
-      if (k < i) before += n;
+      if (k < mine) before += n;
     }
     before = wave::sum(before);
     total = wave::sum(total);
@@ -420,7 +423,7 @@ __global__ __launch_bounds__(NT) void grow_assign_kernel(GrowArgs a, uint32_t mo
   }
   const bool ok = !h.error && total >= h.more;
   if (i < a.ntiles) {
-    assign_tile(a, h, ok, i, before);
+    assign_tile<N>(a, h, ok, i, before);
     return;
   }
   i -= a.ntiles;
@@ -456,7 +459,7 @@ Layout layout_of(const GrowArgs& a) {
     at += (4 * n + 63) / 64 * 64;
     return here;
   };
-  l.tile_cnt = take(a.ntiles);
+  l.tile_cnt = take(a.counts);
   l.old_off = take(a.P + 1);
   l.new_off = take(a.P + 1);
   l.held_new = take(a.P);
@@ -486,7 +489,9 @@ bool args_of(const mori_pool* pool, const mori_growth* g, GrowArgs* out) {
   a.tbl_len = g->tbl_len;
   a.bt = pool->block_tokens;
   a.num_blocks = pool->num_blocks;
-  a.ntiles = (uint32_t)(((uint64_t)a.num_blocks + TILE - 1) / TILE);
+  a.counts = (uint32_t)(((uint64_t)a.num_blocks + COUNTED - 1) / COUNTED);
+  a.tile = a.counts <= 1024 ? 512 : 4096;
+  a.ntiles = (uint32_t)(((uint64_t)a.num_blocks + a.tile - 1) / a.tile);
   a.by_bt = fast_div(a.bt);
   a.new_tokens = g->new_tokens;
   a.program = g->program;
@@ -504,7 +509,7 @@ bool args_of(const mori_pool* pool, const mori_growth* g, GrowArgs* out) {
   a.slots = g->slots;
   a.positions = g->positions;
   a.in_place = g->tbl_to == g->tbl;
-  a.copies = a.in_place ? (uint32_t)(((uint64_t)a.tbl_len + 4 * COUNT_NT - 1) / (4 * COUNT_NT)) : 0;
+  a.copies = a.in_place ? (uint32_t)(((uint64_t)a.tbl_len + ENTRIES - 1) / ENTRIES) : 0;
   return true;
 }
 
@@ -540,12 +545,20 @@ extern "C" int mori_tables_grow(const mori_pool* pool, const mori_growth* growth
   a.aside = at(l.aside);
   a.error = error;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const uint32_t counters = (a.ntiles + COUNT_NT / NT - 1) / (COUNT_NT / NT);
-  hipLaunchKernelGGL(grow_count_kernel, dim3(1 + a.copies + counters), dim3(COUNT_NT), 0, s, a);
+  const uint32_t most = std::max(a.P, a.B);
+  const auto count = [&](auto kernel, uint32_t threads) {
+    const uint64_t pages = 16ull * threads;
+    hipLaunchKernelGGL(kernel, dim3(1 + a.copies + (uint32_t)((a.num_blocks + pages - 1) / pages)), dim3(threads), 0, s, a);
+  };
+  if (most <= 64) count(grow_count_kernel<64, 1>, 64);
+  else if (most <= 256) count(grow_count_kernel<256, 1>, 256);
+  else if (most <= 1024) count(grow_count_kernel<1024, 1>, 1024);
+  else count(grow_count_kernel<1024, 4>, 1024);
   const uint32_t movers = (uint32_t)(((uint64_t)a.tbl_len + ENTRIES - 1) / ENTRIES);
   const uint32_t placers = a.slots || a.positions ? (a.T + NT - 1) / NT : 0;
-  const uint32_t rest = (max(a.P, a.B) + NT) / NT;
-  hipLaunchKernelGGL(grow_assign_kernel, dim3(a.ntiles + movers + placers + rest), dim3(NT), 0, s, a, movers, placers);
+  const dim3 grid(a.ntiles + movers + placers + (most + NT) / NT);
+  if (a.tile == 512) hipLaunchKernelGGL(grow_assign_kernel<2>, grid, dim3(NT), 0, s, a, movers, placers);
+  else hipLaunchKernelGGL(grow_assign_kernel<16>, grid, dim3(NT), 0, s, a, movers, placers);
   if (hipGetLastError() != hipSuccess) return MORI_EHIP;
   return MORI_OK;
 }
