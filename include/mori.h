@@ -540,6 +540,32 @@ typedef struct {
 int mori_kv_append(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, const mori_append* append,
                    uint32_t* error, void* stream);
 
+/* Positions with several axes (time, height and width of a patch in an image or a
+ * video): the pair i of token t turns by rope[at[a][t]][i] with a the axis of i, in place
+ * of the token's position in its program, which still says where it is stored.
+ *   MORI_AXES_BLOCKS  the first sections[0] pairs have axis 0, the next sections[1]
+ *                     axis 1 and so on
+ *   MORI_AXES_TURNS   pair i has axis i % num_axes, if i / num_axes < sections of it,
+ *                     else axis 0, whose section is the rest
+ * A column of the table has its own frequency, so axes whose frequencies start anew are
+ * a table made that way.  A position below 0 or past rope_len: MORI_DEV_BAD_TOKENS, the
+ * token is not stored and its query is 0; padding's positions do not matter. */
+#define MORI_MAX_AXES 4u
+#define MORI_AXES_BLOCKS 0u
+#define MORI_AXES_TURNS 1u
+typedef struct {
+  uint32_t num_axes;                /* 1..MORI_MAX_AXES */
+  uint32_t order;                   /* MORI_AXES_* */
+  uint32_t sections[MORI_MAX_AXES]; /* pairs of each axis: rot_dim / 2 together */
+  const int32_t* at;                /* device [num_axes][axis_stride], a token an entry */
+  uint64_t axis_stride;             /* >= num_tokens, where there is more than one axis */
+} mori_axes;
+
+/* mori_kv_append with such positions.  EINVAL: as there, no axes, sections that do not
+ * give every axis its pairs, rot_dim 0. */
+int mori_kv_append_axes(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, const mori_append* append,
+                        const mori_axes* axes, uint32_t* error, void* stream);
+
 /* What attends: out[t][h] = sum over the program's tokens j up to and with t's
  * own position of softmax_j(scale * q[t][h] . key_j) value_j, with head h
  * reading key head h / (q_heads / kv_heads); an empty sum is 0.

@@ -13,6 +13,8 @@ that require them are refused, and what is written counts as changed in place.
 from __future__ import annotations
 
 import contextlib
+import ctypes as C
+import functools
 import warnings
 
 import numpy as np
@@ -24,6 +26,7 @@ from .tiering import MoriError, PoolGeometry, check
 DTYPES = {torch.float16: M.MORI_DT_F16, torch.bfloat16: M.MORI_DT_BF16}
 STYLES = {"half": M.MORI_ROPE_HALF, "pairs": M.MORI_ROPE_PAIRS}
 _current_device = torch._C._cuda_getDevice
+ORDERS = {"blocks": M.MORI_AXES_BLOCKS, "turns": M.MORI_AXES_TURNS}
 LATENT_ROPE = 64  # rotated elements behind the latent part of a latent row
 
 
@@ -32,12 +35,17 @@ def _need(ok: bool, what: str) -> None:
         raise MoriError(what, M.MORI_EINVAL)
 
 
-def rope_table(positions: int, rot_dim: int, theta: float = 10000.0, device="cuda") -> torch.Tensor:
+def rope_table(positions: int, rot_dim: int, theta: float = 10000.0, device="cuda", restart=None) -> torch.Tensor:
     """float32 [positions][rot_dim]: the cosines of every pair's angle, then the
     sines; pair i turns by position * theta^(-2i / rot_dim).  Angles are taken in
-    64 bits, so long contexts keep their precision."""
-    angle = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * \
-        theta ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64, device=device) / rot_dim)
+    64 bits, so long contexts keep their precision.  restart: numbers of pairs, whose
+    frequencies start anew each, as if n pairs were all (theta^(-2i / 2n)): for axes with
+    frequencies of their own."""
+    parts = [(rot_dim + 1) // 2] if restart is None else list(restart)
+    _need(restart is None or 2 * sum(parts) == rot_dim, "rope_table: restart gives the pairs of every part")
+    share = torch.cat([torch.arange(0, 2 * n, 2, dtype=torch.float64, device=device) /
+                       (rot_dim if restart is None else 2 * n) for n in parts])
+    angle = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * theta ** -share
     return torch.cat([angle.cos(), angle.sin()], 1).float()
 
 
@@ -307,17 +315,26 @@ def _rows(name: str, x: torch.Tensor, batch: TokenBatch, dtype: torch.dtype, hea
 
 def kv_append(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, k: torch.Tensor, v: torch.Tensor, *,
               q: torch.Tensor | None = None, q_out: torch.Tensor | None = None, rope: torch.Tensor | None = None,
-              style: str = "half", stream=None):
+              style: str = "half", stream=None, positions: torch.Tensor | None = None, sections=None,
+              order: str = "blocks"):
     """Stores the batch's keys and values in one layer of the pool.
 
     planes 2: k, v [T][kv_heads][head_dim]; the first rope.shape[1] elements of
     every key head turn with the token's position.  planes 1: k [T][1][latent]
     copied, v [T][1][rot] rotated behind it.  q, if given, is rotated the same way
     ([T][q_heads][head_dim], or [T][q_heads][rot] with planes 1) into q_out, which
-    may be q; returns q_out (allocated if not given)."""
+    may be q; returns q_out (allocated if not given).
+
+    positions int32 [axes][T]: the rotation goes by these (time, height, width: up to
+    four axes) and not by the tokens' places in their programs.  sections: pairs of each
+    axis, rope.shape[1] / 2 together; order 'blocks': one section of pairs behind the
+    other, 'turns': pair i has axis i % axes while that has pairs left, else axis 0
+    (``pair_axes`` lists them).  A token with a position that rope does not have is not
+    stored, which ``TokenBatch.check`` reports."""
     if _current_device() != batch.index:  # launches go to the current device
         with torch.cuda.device(batch.index):
-            return kv_append(pool, geom, layer, batch, k, v, q=q, q_out=q_out, rope=rope, style=style, stream=stream)
+            return kv_append(pool, geom, layer, batch, k, v, q=q, q_out=q_out, rope=rope, style=style, stream=stream,
+                             positions=positions, sections=sections, order=order)
     if torch.is_grad_enabled() and (k.requires_grad or v.requires_grad or pool.requires_grad or
                                     (q is not None and q.requires_grad) or
                                     (q_out is not None and q_out.requires_grad) or
@@ -331,13 +348,13 @@ def kv_append(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, k: torch.
     latent, heads, dim = geom.planes == 1, k.shape[1], k.shape[2]
     if latent:
         dim += v.shape[2]
-    rot = positions = 0
+    rot = rope_len = 0
     if rope is not None:
         if rope.dtype != torch.float32 or rope.dim() != 2 or not rope.is_contiguous() or rope.device != batch.device:
             raise MoriError("kv_append: rope is a contiguous float32 [positions][rot_dim] on the batch's device",
                             M.MORI_EINVAL)
-        positions, rot = rope.shape
-    a = M.mori_append(DTYPES[dtype], heads, dim, 0, rot, STYLES[style], positions, rope.data_ptr() if rot else None)
+        rope_len, rot = rope.shape
+    a = M.mori_append(DTYPES[dtype], heads, dim, 0, rot, STYLES[style], rope_len, rope.data_ptr() if rot else None)
     a.k = _rows("k", k, batch, dtype, 1 if latent else None)
     a.v = _rows("v", v, batch, dtype, heads, rot if latent else dim)
     if q is not None:
@@ -347,10 +364,51 @@ def kv_append(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, k: torch.
                 q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         a.q_out = _rows("q_out", q_out, batch, dtype, q.shape[1], q.shape[2], True)
         a.q_heads = q.shape[1]
-    check(M.mori_kv_append(_pool(pool, geom, batch, dtype), int(layer), batch.desc, a, batch.error.data_ptr(),
-                           _stream_of(batch, stream)), "mori_kv_append")
+    if positions is None and sections is None:
+        check(M.mori_kv_append(_pool(pool, geom, batch, dtype), int(layer), batch.desc, a, batch.error.data_ptr(),
+                               _stream_of(batch, stream)), "mori_kv_append")
+    else:
+        axes = _axes(positions, sections, order, batch, rot)
+        check(M.mori_kv_append_axes(_pool(pool, geom, batch, dtype), int(layer), batch.desc, a, axes,
+                                    batch.error.data_ptr(), _stream_of(batch, stream)), "mori_kv_append_axes")
     torch.autograd.graph.increment_version((pool,) if q is None else (pool, q_out))
     return q_out
+
+
+def _axes(positions, sections, order, batch: TokenBatch, rot: int) -> M.mori_axes:
+    if positions is None or sections is None:
+        raise MoriError("kv_append: positions and sections go together", M.MORI_EINVAL)
+    shape, strides = positions.shape, positions.stride()
+    if positions.dtype != torch.int32 or len(shape) != 2 or positions.device != batch.device or \
+            shape[1] != batch.num_tokens or not 0 < shape[0] <= M.MORI_MAX_AXES or (shape[1] > 1 and strides[1] != 1) or \
+            (shape[0] > 1 and strides[0] < shape[1]):
+        raise MoriError(f"kv_append: positions is an int32 [axes][{batch.num_tokens}] on the batch's device, up to "
+                        f"{M.MORI_MAX_AXES} axes, tokens adjacent", M.MORI_EINVAL)
+    pairs, sizes = _sections(tuple(sections), order)
+    if len(sections) != shape[0] or 2 * pairs != rot:
+        raise MoriError(f"kv_append: sections {tuple(sections)} of {shape[0]} axes for {rot} rotated elements",
+                        M.MORI_EINVAL)
+    return M.mori_axes(shape[0], ORDERS[order], sizes, positions.data_ptr() or None,
+                       strides[0] if shape[0] > 1 else shape[1])
+
+
+def pair_axes(sections, order: str = "blocks") -> list:
+    """The axis that every pair turns by."""
+    if order not in ORDERS or not 0 < len(sections) <= M.MORI_MAX_AXES or any(int(n) != n or n < 0 for n in sections):
+        raise MoriError("kv_append: up to four sections, order 'blocks' or 'turns'", M.MORI_EINVAL)
+    if order == "blocks":
+        return [a for a, n in enumerate(sections) for _ in range(n)]
+    A = len(sections)
+    axes = [i % A if i // A < sections[i % A] else 0 for i in range(sum(sections))]
+    if any(axes.count(a) != n for a, n in enumerate(sections)):
+        raise MoriError(f"kv_append: sections {tuple(sections)} do not fit in turns", M.MORI_EINVAL)
+    return axes
+
+
+@functools.lru_cache(maxsize=64)  # the same few in every layer
+def _sections(sections: tuple, order: str):
+    """Their pairs and the library's form of them, if they fit."""
+    return len(pair_axes(sections, order)), (C.c_uint32 * M.MORI_MAX_AXES)(*sections)
 
 
 def _attend_desc(geom, q: torch.Tensor, scale: float | None) -> M.mori_attend:

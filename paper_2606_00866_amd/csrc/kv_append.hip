@@ -11,6 +11,10 @@
 // loads, then its wavefronts find the tokens' places (sequence, position, page)
 // while those are in flight, then it rotates and stores.
 //
+// Positions may have several axes (time, height, width): a pair then turns by the
+// table row of its axis's position.  A token's positions lie with its place in LDS;
+// the rows are read four pairs at a time where those have one axis, else pair by pair.
+//
 // Bound by bytes: prompt chunks of five programs (16587 tokens, 32 query and 8 key
 // heads of 128; 416 MB) take 77 us, 5.4 TB/s; a decode step of eight agents (4 key
 // heads of 64) 3.7 us, where the launch and two dependent reads are the time.
@@ -32,12 +36,22 @@ struct AppendArgs {
   uint32_t q_units, k_units;      // units of all queries, of all keys (latent: of the latent part)
   FastDiv by_units, by_q, by_k;   // by units of a token, of a query head, of a key head
   uint32_t uq, uk;                // units of one query head, of one key (and value) head
+  // positions of several axes
+  const int32_t* at;              // [axes][at_stride]
+  uint64_t at_stride;
+  uint32_t axes, turns;           // turns: MORI_AXES_TURNS
+  uint32_t upto[MORI_MAX_AXES];   // pairs of this axis and of those before it; turns: of this axis alone
+  FastDiv by_axes;
 };
 
 struct Place {
   uint64_t slot;   // byte offset of the token's row in a plane
   uint32_t pos;
   uint32_t state;  // LEFT_ALONE, PADDING, ROTATED (queries only) or STORED
+};
+// The token's rows in the table, by axis.
+struct Axes {
+  uint32_t at[MORI_MAX_AXES];
 };
 constexpr uint32_t LEFT_ALONE = 0, PADDING = 1, ROTATED = 2, STORED = 3;
 
@@ -57,8 +71,11 @@ __device__ inline uint32_t find_sequence(const Batch& b, uint32_t t, uint32_t la
              b.B - 1);
 }
 
-__device__ inline Place place_of(const AppendArgs& a, uint32_t t, uint32_t lane, uint32_t* err) {
+// `axis`: of the lanes below the number of axes, the token's position on theirs.
+template <bool AXES>
+__device__ inline Place place_of(const AppendArgs& a, uint32_t t, uint32_t lane, uint32_t* err, uint32_t* axis) {
   Place p{};
+  if constexpr (AXES) *axis = lane < a.axes ? (uint32_t)a.at[lane * a.at_stride + t] : 0u;
   const uint32_t b = find_sequence(a.b, t, lane);
   const Seq s = sequence(a.b, b);
   *err |= s.error;
@@ -66,7 +83,7 @@ __device__ inline Place place_of(const AppendArgs& a, uint32_t t, uint32_t lane,
   const int32_t pos = s.position(t - s.t0);
   p.state = PADDING;
   if (s.error || pos < 0) return p;
-  if (a.rot && (uint32_t)pos >= a.rope_len) {
+  if (AXES ? __any(lane < a.axes && *axis >= a.rope_len) : a.rot && (uint32_t)pos >= a.rope_len) {
     *err |= MORI_DEV_BAD_TOKENS;
     return p;
   }
@@ -135,17 +152,48 @@ __device__ inline Unit unit_of(const AppendArgs& a, uint32_t t, uint32_t u) {
   return x;
 }
 
-template <typename DT>
-__device__ inline void rotate(const AppendArgs& a, const Unit& x, uint32_t pos, u32x4& lo, u32x4& hi) {
-  const float* row = a.rope + (uint64_t)pos * a.rot;
-  const uint32_t half = a.rot / 2;
+// Cosines and sines of the four pairs from i on (i a multiple of 4).
+struct Turn {
+  f32x4 c, s;
+};
+__device__ inline Turn turn_of(const AppendArgs& a, uint32_t pos, uint32_t i) {
+  const float* row = a.rope + (uint64_t)pos * a.rot + i;
+  return {*reinterpret_cast<const f32x4*>(row), *reinterpret_cast<const f32x4*>(row + a.rot / 2)};
+}
+__device__ inline Turn turn_of(const AppendArgs& a, const Axes& at, uint32_t i) {
+  uint32_t axis[4];
+  if (a.turns) {
+    uint32_t round = divide(i, a.by_axes), k = i - round * a.axes;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      axis[j] = round < a.upto[k] ? k : 0;
+      if (++k == a.axes) k = 0, ++round;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)  // the last axis ends where the pairs do
+      axis[j] = (i + j >= a.upto[0]) + (i + j >= a.upto[1]) + (i + j >= a.upto[2]);
+    if (axis[0] == axis[3]) return turn_of(a, at.at[axis[0]], i);
+  }
+  Turn x;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float* row = a.rope + (uint64_t)at.at[axis[j]] * a.rot + i + j;
+    x.c[j] = row[0];
+    x.s[j] = row[a.rot / 2];
+  }
+  return x;
+}
+
+// `at`: the token's position, or its positions by axis.
+template <typename DT, typename At>
+__device__ inline void rotate(const AppendArgs& a, const Unit& x, const At& at, u32x4& lo, u32x4& hi) {
   float p[8], q[8];
   widen<DT>(lo, p);
   widen<DT>(hi, q);
   if (!a.pairs) {  // element 8 pair + i of the first half with the same of the second
-    const f32x4* cs = reinterpret_cast<const f32x4*>(row + 8 * x.pair);
-    const f32x4* sn = reinterpret_cast<const f32x4*>(row + half + 8 * x.pair);
-    const f32x4 c0 = cs[0], c1 = cs[1], s0 = sn[0], s1 = sn[1];
+    const Turn t0 = turn_of(a, at, 8 * x.pair), t1 = turn_of(a, at, 8 * x.pair + 4);
+    const f32x4 c0 = t0.c, c1 = t1.c, s0 = t0.s, s1 = t1.s;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float c = i < 4 ? c0[i & 3] : c1[i & 3], s = i < 4 ? s0[i & 3] : s1[i & 3];
@@ -154,9 +202,8 @@ __device__ inline void rotate(const AppendArgs& a, const Unit& x, uint32_t pos, 
       q[i] = g * c + f * s;
     }
   } else {  // neighbours within each chunk
-    const uint32_t i0 = 4 * x.pair, i1 = i0 + a.rot / 4;
-    const f32x4 c0 = *reinterpret_cast<const f32x4*>(row + i0), s0 = *reinterpret_cast<const f32x4*>(row + half + i0);
-    const f32x4 c1 = *reinterpret_cast<const f32x4*>(row + i1), s1 = *reinterpret_cast<const f32x4*>(row + half + i1);
+    const Turn t0 = turn_of(a, at, 4 * x.pair), t1 = turn_of(a, at, 4 * x.pair + a.rot / 4);
+    const f32x4 c0 = t0.c, c1 = t1.c, s0 = t0.s, s1 = t1.s;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float f = p[2 * i], g = p[2 * i + 1];
@@ -171,9 +218,10 @@ __device__ inline void rotate(const AppendArgs& a, const Unit& x, uint32_t pos, 
   hi = narrow<DT>(q);
 }
 
-template <typename DT>
+template <typename DT, bool AXES>
 __global__ __launch_bounds__(NT) void append_kernel(AppendArgs a) {
   __shared__ Place s_place[NT / 2 + 2];  // a token has two units at least
+  __shared__ Axes s_axes[AXES ? NT / 2 + 2 : 1];
   const uint32_t tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   const uint64_t u_first = (uint64_t)blockIdx.x * NT;
   const uint32_t t_first = (uint32_t)(u_first / a.units);
@@ -186,8 +234,10 @@ __global__ __launch_bounds__(NT) void append_kernel(AppendArgs a) {
   u32x4 hi = *reinterpret_cast<const u32x4*>(x.src + x.at + x.gap);
   uint32_t err = 0;
   for (uint32_t i = wv; i <= t_last - t_first; i += NT / 64) {
-    const Place p = place_of(a, t_first + i, lane, &err);
+    uint32_t axis;
+    const Place p = place_of<AXES>(a, t_first + i, lane, &err, &axis);
     if (lane == 0) s_place[i] = p;
+    if (AXES && lane < a.axes) s_axes[i].at[lane] = axis;
   }
   if (lane == 0) report(a.b, err);
   __syncthreads();
@@ -195,7 +245,10 @@ __global__ __launch_bounds__(NT) void append_kernel(AppendArgs a) {
   const Place p = s_place[tl];
   if (p.state == LEFT_ALONE || (!x.query && p.state != STORED)) return;
   if (p.state == PADDING) lo = hi = u32x4{0, 0, 0, 0};
-  else if (x.turn) rotate<DT>(a, x, p.pos, lo, hi);
+  else if (x.turn) {
+    if constexpr (AXES) rotate<DT>(a, x, s_axes[tl], lo, hi);
+    else rotate<DT>(a, x, p.pos, lo, hi);
+  }
   uint8_t* dst = x.dst + (x.query ? 0 : p.slot) + x.at;
   *reinterpret_cast<u32x4*>(dst) = lo;
   *reinterpret_cast<u32x4*>(dst + x.gap) = hi;
@@ -204,15 +257,36 @@ __global__ __launch_bounds__(NT) void append_kernel(AppendArgs a) {
 template <typename DT>
 void launch(const AppendArgs& a, hipStream_t s) {
   const uint64_t total = (uint64_t)a.b.T * a.units;
-  hipLaunchKernelGGL(append_kernel<DT>, dim3((uint32_t)((total + NT - 1) / NT)), dim3(NT), 0, s, a);
+  const dim3 grid((uint32_t)((total + NT - 1) / NT));
+  if (a.axes) hipLaunchKernelGGL((append_kernel<DT, true>), grid, dim3(NT), 0, s, a);
+  else hipLaunchKernelGGL((append_kernel<DT, false>), grid, dim3(NT), 0, s, a);
 }
 
-}  // namespace
-}  // namespace mori
+// Which axis every pair turns by; what a call says of it has to give each axis its pairs.
+bool axes_of(const mori_axes& x, AppendArgs& a) {
+  if (!x.num_axes || x.num_axes > MORI_MAX_AXES || x.order > MORI_AXES_TURNS || !a.rot) return false;
+  const uint32_t pairs = a.rot / 2;
+  uint64_t sum = 0;
+  for (uint32_t i = 0; i < MORI_MAX_AXES; ++i) {
+    const uint32_t n = i < x.num_axes ? x.sections[i] : 0;
+    sum += n;
+    a.upto[i] = x.order == MORI_AXES_TURNS ? n : (uint32_t)sum;
+    // in turns axis i's pairs are i, i + num_axes, ...: all of them have to be there
+    if (x.order == MORI_AXES_TURNS && i && n && (uint64_t)x.num_axes * (n - 1) + i >= pairs) return false;
+  }
+  if (sum != pairs) return false;
+  if (a.b.T && (!x.at || (reinterpret_cast<uintptr_t>(x.at) & 3u))) return false;
+  if (x.num_axes > 1 && x.axis_stride < a.b.T) return false;
+  a.at = x.at;
+  a.at_stride = x.num_axes > 1 ? x.axis_stride : 0;
+  a.axes = x.num_axes;
+  a.turns = x.order == MORI_AXES_TURNS;
+  a.by_axes = fast_div(a.axes);
+  return true;
+}
 
-extern "C" int mori_kv_append(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, const mori_append* ap,
-                              uint32_t* error, void* stream) {
-  using namespace mori;
+int append(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, const mori_append* ap,
+           const mori_axes* axes, uint32_t* error, void* stream) {
   AppendArgs a{};
   if (!ap || !batch_of(pool, layer, tokens, error, &a.b)) return MORI_EINVAL;
   if (ap->dtype > MORI_DT_BF16 || ap->rope_style > MORI_ROPE_PAIRS) return MORI_EINVAL;
@@ -224,6 +298,7 @@ extern "C" int mori_kv_append(const mori_pool* pool, uint32_t layer, const mori_
   if ((uint64_t)a.kv_heads * a.hd * 2 != pool->row_bytes) return MORI_EINVAL;
   if (a.latent && (a.kv_heads != 1 || a.rot < 16 || a.rot > a.hd - 16)) return MORI_EINVAL;
   if (a.rot && (!ap->rope || (reinterpret_cast<uintptr_t>(ap->rope) & 15u) || !ap->rope_len)) return MORI_EINVAL;
+  if (axes && !axes_of(*axes, a)) return MORI_EINVAL;
   if (a.b.T == 0) return MORI_OK;
   if (!rows_valid(ap->k) || !rows_valid(ap->v)) return MORI_EINVAL;
   const bool with_q = ap->q.data != nullptr;
@@ -248,4 +323,18 @@ extern "C" int mori_kv_append(const mori_pool* pool, uint32_t layer, const mori_
   else launch<BF16>(a, s);
   if (hipGetLastError() != hipSuccess) return MORI_EHIP;
   return MORI_OK;
+}
+
+}  // namespace
+}  // namespace mori
+
+extern "C" int mori_kv_append(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens,
+                              const mori_append* append, uint32_t* error, void* stream) {
+  return mori::append(pool, layer, tokens, append, nullptr, error, stream);
+}
+
+extern "C" int mori_kv_append_axes(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens,
+                                   const mori_append* append, const mori_axes* axes, uint32_t* error, void* stream) {
+  if (!axes) return MORI_EINVAL;
+  return mori::append(pool, layer, tokens, append, axes, error, stream);
 }

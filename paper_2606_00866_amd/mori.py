@@ -33,6 +33,7 @@ MORI_ADMIT_BEST_FIT = 1
 MORI_EVICT_NOALLOC_MAX_BLOCKS = 1 << 19
 MORI_DT_F16, MORI_DT_BF16 = 0, 1
 MORI_ROPE_HALF, MORI_ROPE_PAIRS = 0, 1
+MORI_MAX_AXES, MORI_AXES_BLOCKS, MORI_AXES_TURNS = 4, 0, 1
 MORI_Q_LAST_HIP_ERROR, MORI_Q_DEVICE_ERROR, MORI_Q_LAST_MODE = 1, 2, 3
 MORI_Q_PLAN_EVENT, MORI_Q_OUT_EVENT, MORI_Q_IN_EVENT = 4, 5, 6
 
@@ -40,7 +41,7 @@ EXPORTS = ("mori_create", "mori_destroy", "mori_register", "mori_host_alloc", "m
            "mori_rank_partition", "mori_plan_wait", "mori_kv_swap_out", "mori_kv_swap_in", "mori_query",
            "mori_strerror", "mori_profile", "mori_profile_read", "mori_evict_workspace", "mori_evict_order",
            "mori_replica_admit", "mori_evict_order_noalloc", "mori_kv_append", "mori_kv_attend_workspace",
-           "mori_kv_attend", "mori_tables_grow_workspace", "mori_tables_grow")
+           "mori_kv_attend", "mori_tables_grow_workspace", "mori_tables_grow", "mori_kv_append_axes")
 
 
 class mori_pool(C.Structure):
@@ -85,6 +86,11 @@ class mori_append(C.Structure):
     _fields_ = [(n, C.c_uint32) for n in ("dtype", "kv_heads", "head_dim", "q_heads", "rot_dim", "rope_style",
                                           "rope_len")] + [
         ("rope", C.c_void_p), ("k", mori_rows), ("v", mori_rows), ("q", mori_rows), ("q_out", mori_rows)]
+
+
+class mori_axes(C.Structure):
+    _fields_ = [("num_axes", C.c_uint32), ("order", C.c_uint32), ("sections", C.c_uint32 * MORI_MAX_AXES),
+                ("at", C.c_void_p), ("axis_stride", C.c_uint64)]
 
 
 class mori_attend(C.Structure):
@@ -134,6 +140,7 @@ def lib():
         L.mori_evict_order_noalloc.argtypes = [C.POINTER(mori_blocks), U32, U64, V, V, V, V]
         PP, PT = C.POINTER(mori_pool), C.POINTER(mori_tokens)
         L.mori_kv_append.argtypes = [PP, U32, PT, C.POINTER(mori_append), V, V]
+        L.mori_kv_append_axes.argtypes = [PP, U32, PT, C.POINTER(mori_append), C.POINTER(mori_axes), V, V]
         L.mori_kv_attend_workspace.argtypes = [PP, PT, C.POINTER(mori_attend), C.POINTER(U64)]
         L.mori_kv_attend.argtypes = [PP, U32, PT, C.POINTER(mori_attend), V, U64, V, V]
         L.mori_tables_grow_workspace.argtypes = [PP, C.POINTER(mori_growth), C.POINTER(U64)]
@@ -233,6 +240,12 @@ def mori_kv_append(pool: mori_pool, layer: int, tokens: mori_tokens, append: mor
                    stream: int = 0) -> int:
     """error: device address of the word that collects MORI_DEV_* bits, or 0."""
     return lib().mori_kv_append(C.byref(pool), layer, C.byref(tokens), C.byref(append), error or None, stream)
+
+
+def mori_kv_append_axes(pool: mori_pool, layer: int, tokens: mori_tokens, append: mori_append, axes: mori_axes,
+                        error: int = 0, stream: int = 0) -> int:
+    return lib().mori_kv_append_axes(C.byref(pool), layer, C.byref(tokens), C.byref(append), C.byref(axes),
+                                     error or None, stream)
 
 
 def mori_kv_attend_workspace(pool: mori_pool, tokens: mori_tokens, attend: mori_attend):
