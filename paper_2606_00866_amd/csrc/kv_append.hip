@@ -12,8 +12,9 @@
 // while those are in flight, then it rotates and stores.
 //
 // Positions may have several axes (time, height, width): a pair then turns by the
-// table row of its axis's position.  A token's positions lie with its place in LDS;
-// the rows are read four pairs at a time where those have one axis, else pair by pair.
+// table row of its axis's position.  All heads of a token share them, so a workgroup puts
+// its tokens' cosines and sines together in LDS once: (256 / units + 2) rows of them, two
+// reads a pair, beside which 32 bytes a unit are little.
 //
 // Bound by bytes: prompt chunks of five programs (16587 tokens, 32 query and 8 key
 // heads of 128; 416 MB) take 77 us, 5.4 TB/s; a decode step of eight agents (4 key
@@ -41,17 +42,13 @@ struct AppendArgs {
   uint64_t at_stride;
   uint32_t axes, turns;           // turns: MORI_AXES_TURNS
   uint32_t upto[MORI_MAX_AXES];   // pairs of this axis and of those before it; turns: of this axis alone
-  FastDiv by_axes;
+  FastDiv by_axes, by_pairs;
 };
 
 struct Place {
   uint64_t slot;   // byte offset of the token's row in a plane
   uint32_t pos;
   uint32_t state;  // LEFT_ALONE, PADDING, ROTATED (queries only) or STORED
-};
-// The token's rows in the table, by axis.
-struct Axes {
-  uint32_t at[MORI_MAX_AXES];
 };
 constexpr uint32_t LEFT_ALONE = 0, PADDING = 1, ROTATED = 2, STORED = 3;
 
@@ -156,43 +153,23 @@ __device__ inline Unit unit_of(const AppendArgs& a, uint32_t t, uint32_t u) {
 struct Turn {
   f32x4 c, s;
 };
-__device__ inline Turn turn_of(const AppendArgs& a, uint32_t pos, uint32_t i) {
-  const float* row = a.rope + (uint64_t)pos * a.rot + i;
-  return {*reinterpret_cast<const f32x4*>(row), *reinterpret_cast<const f32x4*>(row + a.rot / 2)};
+__device__ inline Turn turn_of(const AppendArgs& a, const float* row, uint32_t i) {
+  return {*reinterpret_cast<const f32x4*>(row + i), *reinterpret_cast<const f32x4*>(row + i + a.rot / 2)};
 }
-__device__ inline Turn turn_of(const AppendArgs& a, const Axes& at, uint32_t i) {
-  uint32_t axis[4];
-  if (a.turns) {
-    uint32_t round = divide(i, a.by_axes), k = i - round * a.axes;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      axis[j] = round < a.upto[k] ? k : 0;
-      if (++k == a.axes) k = 0, ++round;
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)  // the last axis ends where the pairs do
-      axis[j] = (i + j >= a.upto[0]) + (i + j >= a.upto[1]) + (i + j >= a.upto[2]);
-    if (axis[0] == axis[3]) return turn_of(a, at.at[axis[0]], i);
-  }
-  Turn x;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float* row = a.rope + (uint64_t)at.at[axis[j]] * a.rot + i + j;
-    x.c[j] = row[0];
-    x.s[j] = row[a.rot / 2];
-  }
-  return x;
+// The axis of a pair.
+__device__ inline uint32_t axis_of(const AppendArgs& a, uint32_t i) {
+  if (!a.turns) return (i >= a.upto[0]) + (i >= a.upto[1]) + (i >= a.upto[2]);  // the last axis ends where the pairs do
+  const uint32_t round = divide(i, a.by_axes), k = i - round * a.axes;
+  return round < a.upto[k] ? k : 0;
 }
-
-// `at`: the token's position, or its positions by axis.
-template <typename DT, typename At>
-__device__ inline void rotate(const AppendArgs& a, const Unit& x, const At& at, u32x4& lo, u32x4& hi) {
+// `row`: the token's cosines and sines, in the table or put together in LDS.
+template <typename DT>
+__device__ inline void rotate(const AppendArgs& a, const Unit& x, const float* row, u32x4& lo, u32x4& hi) {
   float p[8], q[8];
   widen<DT>(lo, p);
   widen<DT>(hi, q);
   if (!a.pairs) {  // element 8 pair + i of the first half with the same of the second
-    const Turn t0 = turn_of(a, at, 8 * x.pair), t1 = turn_of(a, at, 8 * x.pair + 4);
+    const Turn t0 = turn_of(a, row, 8 * x.pair), t1 = turn_of(a, row, 8 * x.pair + 4);
     const f32x4 c0 = t0.c, c1 = t1.c, s0 = t0.s, s1 = t1.s;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -202,7 +179,7 @@ __device__ inline void rotate(const AppendArgs& a, const Unit& x, const At& at, 
       q[i] = g * c + f * s;
     }
   } else {  // neighbours within each chunk
-    const Turn t0 = turn_of(a, at, 4 * x.pair), t1 = turn_of(a, at, 4 * x.pair + a.rot / 4);
+    const Turn t0 = turn_of(a, row, 4 * x.pair), t1 = turn_of(a, row, 4 * x.pair + a.rot / 4);
     const f32x4 c0 = t0.c, c1 = t1.c, s0 = t0.s, s1 = t1.s;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -221,7 +198,8 @@ __device__ inline void rotate(const AppendArgs& a, const Unit& x, const At& at, 
 template <typename DT, bool AXES>
 __global__ __launch_bounds__(NT) void append_kernel(AppendArgs a) {
   __shared__ Place s_place[NT / 2 + 2];  // a token has two units at least
-  __shared__ Axes s_axes[AXES ? NT / 2 + 2 : 1];
+  __shared__ uint32_t s_axes[AXES ? NT / 2 + 2 : 1][MORI_MAX_AXES];
+  extern __shared__ __align__(16) float s_turn[];  // [tokens][rot]
   const uint32_t tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   const uint64_t u_first = (uint64_t)blockIdx.x * NT;
   const uint32_t t_first = (uint32_t)(u_first / a.units);
@@ -237,18 +215,25 @@ __global__ __launch_bounds__(NT) void append_kernel(AppendArgs a) {
     uint32_t axis;
     const Place p = place_of<AXES>(a, t_first + i, lane, &err, &axis);
     if (lane == 0) s_place[i] = p;
-    if (AXES && lane < a.axes) s_axes[i].at[lane] = axis;
+    if (AXES && lane < a.axes) s_axes[i][lane] = p.state < ROTATED ? 0 : axis;  // no row may be read for the others
   }
   if (lane == 0) report(a.b, err);
   __syncthreads();
+  if constexpr (AXES) {
+    const uint32_t pairs = a.rot / 2;
+    for (uint32_t y = tid; y < (t_last - t_first + 1) * pairs; y += NT) {
+      const uint32_t i = divide(y, a.by_pairs), j = y - i * pairs;
+      const float* row = a.rope + (uint64_t)s_axes[i][axis_of(a, j)] * a.rot + j;
+      s_turn[i * a.rot + j] = row[0];
+      s_turn[i * a.rot + pairs + j] = row[pairs];
+    }
+    __syncthreads();
+  }
   if (t_first + tl > t_last) return;
   const Place p = s_place[tl];
   if (p.state == LEFT_ALONE || (!x.query && p.state != STORED)) return;
   if (p.state == PADDING) lo = hi = u32x4{0, 0, 0, 0};
-  else if (x.turn) {
-    if constexpr (AXES) rotate<DT>(a, x, s_axes[tl], lo, hi);
-    else rotate<DT>(a, x, p.pos, lo, hi);
-  }
+  else if (x.turn) rotate<DT>(a, x, AXES ? s_turn + tl * a.rot : a.rope + (uint64_t)p.pos * a.rot, lo, hi);
   uint8_t* dst = x.dst + (x.query ? 0 : p.slot) + x.at;
   *reinterpret_cast<u32x4*>(dst) = lo;
   *reinterpret_cast<u32x4*>(dst + x.gap) = hi;
@@ -258,7 +243,8 @@ template <typename DT>
 void launch(const AppendArgs& a, hipStream_t s) {
   const uint64_t total = (uint64_t)a.b.T * a.units;
   const dim3 grid((uint32_t)((total + NT - 1) / NT));
-  if (a.axes) hipLaunchKernelGGL((append_kernel<DT, true>), grid, dim3(NT), 0, s, a);
+  const size_t turns = sizeof(float) * (NT / a.units + 2) * a.rot;  // a workgroup's tokens
+  if (a.axes) hipLaunchKernelGGL((append_kernel<DT, true>), grid, dim3(NT), turns, s, a);
   else hipLaunchKernelGGL((append_kernel<DT, false>), grid, dim3(NT), 0, s, a);
 }
 
@@ -282,6 +268,7 @@ bool axes_of(const mori_axes& x, AppendArgs& a) {
   a.axes = x.num_axes;
   a.turns = x.order == MORI_AXES_TURNS;
   a.by_axes = fast_div(a.axes);
+  a.by_pairs = fast_div(pairs);
   return true;
 }
 
