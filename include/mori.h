@@ -601,6 +601,34 @@ int mori_kv_attend_workspace(const mori_pool* pool, const mori_tokens* tokens, c
 int mori_kv_attend(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, const mori_attend* attend,
                    void* workspace, uint64_t workspace_bytes, uint32_t* error, void* stream);
 
+/* What a call may say of scores and of what a token sees, K/V pools only:
+ *   s = scale * q . key_j
+ *   cap > 0:  s = cap * tanh(s / cap)
+ *   slopes:   s = s - slopes[h] * |i - j|, i and j positions in the program
+ * and token i of the program sees key j where
+ *   max(first[t], i + 1 - window, 0) <= j < min(end[t], the program's length)
+ * with end[t] = i + 1 unless it is given, so one may also see what is behind it.  Ranges
+ * make documents that do not see each other (first: where a token's document starts),
+ * prefixes that all of it see (end: the larger of the prefix's and the token's own) and
+ * the like.  A token that sees nothing gets 0, lse -inf.  Keys that no token sees are not
+ * read: their pages need not be there. */
+typedef struct {
+  float cap;            /* 0: none; finite, not negative */
+  uint32_t window;      /* positions up to and with the token's own; 0: all */
+  const float* slopes;  /* device [q_heads] or NULL */
+  const int32_t* first; /* device [T] or NULL */
+  const int32_t* end;   /* device [T] or NULL */
+} mori_sight;
+
+/* mori_kv_attend and its workspace with that; EINVAL as there, and for a cap or
+ * alignment that does not fit, no sight, or a latent pool.  A workspace for a sight
+ * without a window serves all others of the batch. */
+int mori_kv_attend_sight_workspace(const mori_pool* pool, const mori_tokens* tokens, const mori_attend* attend,
+                                   const mori_sight* sight, uint64_t* bytes);
+int mori_kv_attend_sight(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, const mori_attend* attend,
+                         const mori_sight* sight, void* workspace, uint64_t workspace_bytes, uint32_t* error,
+                         void* stream);
+
 /* ---- kernel timing ------------------------------------------------------ */
 /* With profiling on, every gather/scatter kernel launch of the swaps is
  * bracketed by timing events recorded on the stream it is launched on (up to

@@ -423,24 +423,43 @@ def _attend_desc(geom, q: torch.Tensor, scale: float | None) -> M.mori_attend:
                          dim ** -0.5 if scale is None else float(scale))
 
 
+def _sight(geom, batch: TokenBatch, heads: int, cap, slopes, window, first, end) -> M.mori_sight:
+    _need(geom.planes == 2, "kv_attend: caps, slopes, windows and ranges are for K/V pools")
+    _need(cap is None or 0 < cap < float("inf"), "kv_attend: cap is a finite number above 0")
+    _need(window is None or 0 < window < 1 << 32, "kv_attend: window is a number of positions, its own among them")
+    for name, x, dtype, n in (("slopes", slopes, torch.float32, heads), ("first", first, torch.int32, batch.num_tokens),
+                              ("end", end, torch.int32, batch.num_tokens)):
+        if x is not None and not (x.dtype == dtype and x.shape == (n,) and x.is_contiguous() and x.device == batch.device):
+            raise MoriError(f"kv_attend: {name} is a contiguous {dtype} [{n}] on the batch's device", M.MORI_EINVAL)
+    ptr = lambda x: x.data_ptr() or None if x is not None else None
+    return M.mori_sight(cap or 0.0, window or 0, ptr(slopes), ptr(first), ptr(end))
+
+
 def _empty_pool(geom) -> M.mori_pool:
     """The pool as a description only (the workspace call reads no memory)."""
     return M.mori_pool(geom.layers, geom.planes, geom.block_tokens, geom.row_bytes, geom.num_blocks, 256)
 
 
-def kv_attend_workspace(geom, batch: TokenBatch, q: torch.Tensor) -> torch.Tensor:
+def kv_attend_workspace(geom, batch: TokenBatch, q: torch.Tensor, sight: bool = False) -> torch.Tensor:
     """Device workspace for kv_attend of this batch, in every layer; calls that may
-    overlap (on other streams) need one each."""
+    overlap (on other streams) need one each.  sight: also for calls with a cap, slopes,
+    a window or ranges, whatever they are."""
     _same_geometry(geom, batch)
     a = _attend_desc(geom, q, None)
     rc, n = M.mori_kv_attend_workspace(_empty_pool(geom), batch.desc, a)
     check(rc, "mori_kv_attend_workspace")
+    if sight:
+        rc, more = M.mori_kv_attend_sight_workspace(_empty_pool(geom), batch.desc, a, M.mori_sight())
+        check(rc, "mori_kv_attend_sight_workspace")
+        n = max(n, more)
     return torch.empty(n, dtype=torch.uint8, device=batch.device)
 
 
 def kv_attend(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, q: torch.Tensor, *, scale: float | None = None,
               out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
-              workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+              workspace: torch.Tensor | None = None, stream=None, cap: float | None = None,
+              slopes: torch.Tensor | None = None, window: int | None = None, first: torch.Tensor | None = None,
+              end: torch.Tensor | None = None) -> torch.Tensor:
     """Causal attention of the batch's tokens over their programs' pages in one
     layer.  q [T][q_heads][head_dim] (latent pools: [T][q_heads][576], in the latent
     space).  scale: head_dim ** -0.5 unless given; a latent row's width says nothing
@@ -448,18 +467,30 @@ def kv_attend(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, q: torch.
     512 + 64), so on latent pools leaving it out warns.  Returns out [T][q_heads]
     [head_dim] (latent pools: 512), allocated if not given; lse, a float32
     [T][q_heads] tensor, takes the logarithms of the rows' sums.  The workspace is
-    allocated here unless given."""
+    allocated here unless given.
+
+    On K/V pools a call may say more.  cap: scores become cap * tanh(score / cap).
+    slopes float32 [q_heads]: slopes[h] * |i - j| is taken from the score of a token at
+    position i and a key at j (behind the cap).  window: a token sees the last `window`
+    positions up to its own.  first, end int32 [T]: it sees keys from first[t] up to, not
+    with, end[t]; without end up to its own.  So documents are first (where the token's
+    begins), prefixes that all tokens see end (the larger of the prefix's length and the
+    token's own position + 1).  A token that sees nothing gets zeros."""
     if _current_device() != batch.index:  # launches go to the current device
         with torch.cuda.device(batch.index):
             return kv_attend(pool, geom, layer, batch, q, scale=scale, out=out, lse=lse, workspace=workspace,
-                             stream=stream)
+                             stream=stream, cap=cap, slopes=slopes, window=window, first=first, end=end)
     if scale is None and geom.planes == 1:
         warnings.warn("kv_attend: no scale given for a latent pool; 576 ** -0.5 is taken, which is not that of the "
                       "model's heads", stacklevel=2)
     if torch.is_grad_enabled() and (q.requires_grad or pool.requires_grad or (out is not None and out.requires_grad) or
-                                    (lse is not None and lse.requires_grad)):
+                                    (lse is not None and lse.requires_grad) or
+                                    (slopes is not None and slopes.requires_grad)):
         raise _needs_gradients("kv_attend")
     a, dtype = _attend_desc(geom, q, scale), q.dtype
+    sight = None
+    if not (cap is None and slopes is None and window is None and first is None and end is None):
+        sight = _sight(geom, batch, a.q_heads, cap, slopes, window, first, end)
     a.q = _rows("q", q, batch, dtype)
     if out is None:
         with _on(stream):
@@ -474,11 +505,16 @@ def kv_attend(pool: torch.Tensor, geom, layer: int, batch: TokenBatch, q: torch.
         if workspace.device != batch.device or not workspace.is_contiguous():
             raise MoriError("kv_attend: workspace is contiguous and on the batch's device", M.MORI_EINVAL)
     else:
-        rc, n = M.mori_kv_attend_workspace(desc, batch.desc, a)
+        rc, n = M.mori_kv_attend_workspace(desc, batch.desc, a) if sight is None else \
+            M.mori_kv_attend_sight_workspace(desc, batch.desc, a, sight)
         check(rc, "mori_kv_attend_workspace")
         with _on(stream):
             workspace = torch.empty(n, dtype=torch.uint8, device=batch.device)
-    check(M.mori_kv_attend(desc, int(layer), batch.desc, a, workspace.data_ptr(), workspace.nbytes,
-                           batch.error.data_ptr(), _stream_of(batch, stream)), "mori_kv_attend")
+    if sight is None:
+        check(M.mori_kv_attend(desc, int(layer), batch.desc, a, workspace.data_ptr(), workspace.nbytes,
+                               batch.error.data_ptr(), _stream_of(batch, stream)), "mori_kv_attend")
+    else:
+        check(M.mori_kv_attend_sight(desc, int(layer), batch.desc, a, sight, workspace.data_ptr(), workspace.nbytes,
+                                     batch.error.data_ptr(), _stream_of(batch, stream)), "mori_kv_attend_sight")
     torch.autograd.graph.increment_version((out,) if lse is None else (out, lse))
     return out

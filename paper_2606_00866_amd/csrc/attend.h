@@ -123,8 +123,8 @@ __device__ inline uint32_t run_of_rounds(const AttendArgs& a, const Share& own, 
 
 // The sequence that `want(first item, number of items, b)` picks, the same for
 // the whole wavefront (all of whose lanes are active).
-template <typename F>
-__device__ inline Item find_item(const AttendArgs& a, uint32_t lane, F want) {
+template <typename Args, typename F>
+__device__ inline Item find_item(const Args& a, uint32_t lane, F want) {
   const uint32_t k = (a.b.B + 63) / 64, b0 = lane * k;
   Share own{0, 1, 0, false};  // the lane's only sequence, for batches of up to 64
   if (b0 < a.b.B) own = share_of(a, b0);
@@ -173,7 +173,9 @@ struct Work {
   uint32_t item, kv;       // index of the item, key head
   uint32_t row0, rows;     // the tile's rows of the sequence: row0 .. row0 + rows - 1
   uint32_t lo, hi;         // keys; lo >= hi: none
-  uint32_t open;           // keys below this are allowed to every row of the tile
+  uint32_t open;           // keys below this, and from `from` on, are allowed to every row of the tile
+  uint32_t from;
+  uint32_t key0;           // no row of the tile may see a key below it
   uint32_t per_tile;
   bool some;
 };
@@ -223,6 +225,19 @@ __device__ inline uint32_t row_limit(const AttendArgs& a, const Work& w, uint32_
   if (r >= w.rows) return 0;
   return (uint32_t)max(w.s.position(divide(w.row0 + r, a.by_group)) + 1, 0);
 }
+
+// Keys that a row may see: lo .. hi - 1, none where that is empty.
+struct Keys {
+  uint32_t lo, hi;
+  __device__ bool none() const { return lo >= hi; }
+};
+__device__ inline Keys row_keys(const AttendArgs& a, const Work& w, uint32_t r) { return {0, row_limit(a, w, r)}; }
+
+// Where the rows of a tile may see different keys, or none, in this step of n keys.
+__device__ inline bool differ(const Work& w, uint32_t k0, uint32_t n) {
+  return (k0 + n > w.open && w.open < w.hi) || k0 < w.from;
+}
+__device__ inline bool differ(const Work& w) { return w.open < w.hi || w.from > w.lo; }
 
 // Token and query head of a row of the tile.
 struct RowAt {
@@ -357,13 +372,18 @@ __device__ inline bool odd_pair(F16, uint32_t x) {
   return (x & 0x7C00u) == 0x7C00u || (x & 0x7C000000u) == 0x7C000000u;
 }
 
+// A row's score in the softmax's units from the product of query and key.
+__device__ inline auto score_of(const AttendArgs& a, const Work&, uint32_t, uint32_t) {
+  return [c = a.c](float s, uint32_t) { return s * c; };
+}
+
 // A tile whose rows see different numbers of keys, among them one with an
 // infinity or a NaN: in the matrix products it would reach the rows before it
 // (weight 0 times NaN).  Such a run of keys is taken again row by row, a wavefront
 // a row with plain arithmetic over the keys it may see, and that result counts.
 // Nothing of the matrix kernels' state is needed, so this costs them no registers.
-template <typename DT, int DK, int DV>
-__device__ inline void rows_one_by_one(const AttendArgs& a, const Work& w, uint32_t first_row, uint32_t row_step,
+template <typename DT, int DK, int DV, typename Args>
+__device__ inline void rows_one_by_one(const Args& a, const Work& w, uint32_t first_row, uint32_t row_step,
                                        uint32_t lane) {
   constexpr int W = DV / 64;
   typedef float vec __attribute__((ext_vector_type(W)));  // vectors, not arrays: those would end up in LDS
@@ -373,11 +393,13 @@ __device__ inline void rows_one_by_one(const AttendArgs& a, const Work& w, uint3
   uint32_t err = 0;  // reported by the pass before
   for (uint32_t r = first_row; r < w.rows; r += row_step) {
     const RowAt at = row_at(a, w, r);
-    const uint32_t allowed = row_limit(a, w, r), hi = min(allowed, w.hi);
+    const Keys allowed = row_keys(a, w, r);
+    const uint32_t lo = max(allowed.lo, w.lo), hi = min(allowed.hi, w.hi);
+    const auto shape = score_of(a, w, r, at.h);
     const u32x4* const q = reinterpret_cast<const u32x4*>(q_row(a, at));
     float top = NO_TOP, sum = 0;
     vec o = 0;
-    for (uint32_t k0 = w.lo; k0 < hi; k0 += 64) {
+    for (uint32_t k0 = lo; k0 < hi; k0 += 64) {
       const uint32_t key = k0 + lane;
       const uint8_t* row = a.b.plane;
       float s = -INFINITY;
@@ -389,7 +411,7 @@ __device__ inline void rows_one_by_one(const AttendArgs& a, const Work& w, uint3
                           __builtin_convertvector(bits<typename DT::x8>(q_signed(a, q[c])), f32x8);
           s += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
         }
-        s *= a.c;
+        s = shape(s, key);
       }
       float m = s;
 #pragma unroll
@@ -418,16 +440,22 @@ __device__ inline void rows_one_by_one(const AttendArgs& a, const Work& w, uint3
     } else {
       scalar* const out = reinterpret_cast<scalar*>(a.out.data + at.t * a.out.token + at.h * a.out.head);
 #pragma unroll
-      for (int i = 0; i < W; ++i) out[64 * i + lane] = (scalar)(allowed ? o[i] / sum : 0.f);
-      if (lane == 0) store_lse(a, at, top, sum, allowed == 0);
+      for (int i = 0; i < W; ++i) out[64 * i + lane] = (scalar)(allowed.none() ? 0.f : o[i] / sum);
+      if (lane == 0) store_lse(a, at, top, sum, allowed.none());
     }
   }
 }
 
+struct SightArgs;
+
 // Launchers, by kernel.
 void launch_attend_step(const AttendArgs& a, bool f16, uint32_t dim, hipStream_t s);
+void launch_attend_step(const SightArgs& a, bool f16, uint32_t dim, hipStream_t s);
 void launch_attend_tile(const AttendArgs& a, bool f16, uint32_t dim, hipStream_t s);
+void launch_attend_tile(const SightArgs& a, bool f16, uint32_t dim, hipStream_t s);
 void launch_attend_latent(const AttendArgs& a, bool f16, hipStream_t s);
 void launch_attend_join(const AttendArgs& a, bool f16, uint32_t value, hipStream_t s);
+void launch_attend_join(const SightArgs& a, bool f16, uint32_t value, hipStream_t s);
+void launch_sight_tiles(const SightArgs& a, hipStream_t s);
 
 }  // namespace mori

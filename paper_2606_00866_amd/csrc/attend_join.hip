@@ -9,37 +9,59 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "attend.h"
+#include "sight.h"
 
 namespace mori {
 namespace {
 
 // WPH wavefronts share a head's runs (8 when there are few rows, so that all runs
 // are on the way at once), else a wavefront takes `some` heads of a token.
-template <typename DT, int DV, int NW, int WPH>
-__global__ __launch_bounds__(64 * NW) void attend_join_kernel(AttendArgs a, uint32_t some) {
+template <typename DT, int DV, int NW, int WPH, typename Args>
+__global__ __launch_bounds__(64 * NW) void attend_join_kernel(Args a, uint32_t some) {
+  constexpr bool SIGHT = IsSight<Args>::value;
   constexpr int W = DV / 64;                // elements of a lane
   typedef float vec __attribute__((ext_vector_type(W)));
   __shared__ float s_y[WPH > 1 ? NW : 1][DV], s_l[NW];
   const uint32_t lane = threadIdx.x & 63, wv = wave_index();
   const uint32_t heads_wg = WPH > 1 ? 1 : NW * some, per_token = (a.heads + heads_wg - 1) / heads_wg;
   const uint32_t t = blockIdx.x / per_token, h0 = (blockIdx.x - t * per_token) * heads_wg + (WPH > 1 ? 0 : wv * some);
-  const Item it = find_item(a, lane, [&](uint32_t, uint32_t n, uint32_t b) {
+  Item it;
+  bool lines = false;  // tiles are written down, with runs of their own
+  if constexpr (SIGHT) lines = a.span != nullptr;
+  if (lines) it.b = find_sequence(a.b, t, lane);
+  else it = find_item(a, lane, [&](uint32_t, uint32_t n, uint32_t b) {
     return n && a.b.seq_off[b] <= t && t < a.b.seq_off[b + 1];
   });
-  if (!it.found || it.per_tile < 2) return;
-  const uint32_t t0 = same(a.b.seq_off[it.b]), n = same(a.b.seq_off[it.b + 1]) - t0;
+  if (!lines && (!it.found || it.per_tile < 2)) return;
+  const uint32_t t0 = same(a.b.seq_off[it.b]), t1 = same(a.b.seq_off[it.b + 1]), n = t1 - t0;
+  if (lines && (t0 > t || t >= t1 || t1 > a.b.T)) return;
   const Seq s = sequence(a.b, it.b);
-  const bool none = s.position(t - s.t0) < 0;
+  bool none;
+  if constexpr (SIGHT) none = token_keys(a, s, t - s.t0).none();
+  else none = s.position(t - s.t0) < 0;
   const uint32_t tiles = (n * a.group + a.tile_rows - 1) / a.tile_rows;
   const uint64_t step = (uint64_t)a.kv_heads * a.tile_rows;
-  const uint32_t runs = it.per_tile;
-  const uint32_t r0 = WPH > 1 ? (uint32_t)((uint64_t)runs * wv / NW) : 0;
-  const uint32_t r1 = WPH > 1 ? (uint32_t)((uint64_t)runs * (wv + 1) / NW) : runs;
+  uint32_t known = 0xFFFFFFFFu;  // the tile whose runs are known
   for (uint32_t h = h0; h < min(h0 + some, a.heads); ++h) {
     const uint32_t kv = divide(h, a.by_group), x = (t - t0) * a.group + (h - kv * a.group);
     const uint32_t tile = x / a.tile_rows;
-    const uint64_t item = it.first + (uint64_t)(tiles - 1 - tile) * it.per_tile;
+    uint64_t item = it.first;
+    if constexpr (SIGHT) {
+      if (lines) {
+        if (tile != known) {
+          known = tile;
+          const TileRun r = find_tile(a, lane, 0, same(a.seq_tile[it.b]) + (tiles - 1 - tile), false);
+          it.first = r.first;
+          it.per_tile = r.found ? r.per_tile : 0;
+        }
+        if (it.per_tile < 2) continue;
+        item = it.first;
+      }
+    }
+    if (!lines) item = it.first + (uint64_t)(tiles - 1 - tile) * it.per_tile;
+    const uint32_t runs = it.per_tile;
+    const uint32_t r0 = WPH > 1 ? (uint32_t)((uint64_t)runs * wv / NW) : 0;
+    const uint32_t r1 = WPH > 1 ? (uint32_t)((uint64_t)runs * (wv + 1) / NW) : runs;
     if (item + it.per_tile > a.items) continue;  // sequences that overlap: more items than tokens give, which were not run
     const uint64_t at0 = (item * a.kv_heads + kv) * a.tile_rows + (x - tile * a.tile_rows);
 
@@ -106,31 +128,35 @@ __global__ __launch_bounds__(64 * NW) void attend_join_kernel(AttendArgs a, uint
   }
 }
 
-template <typename DT, int DV>
-void launch(const AttendArgs& a, hipStream_t s) {
+template <typename DT, int DV, typename Args>
+void launch(const Args& a, hipStream_t s) {
   // Few rows: a workgroup each, so that all of their runs are read at once.  Else as many
   // wavefronts as the chip holds: each finds its sequence once for all of its heads
   // (1610 tokens, 32 heads: 302 us for the attention with one head each, 287 so).
   const uint64_t rows = (uint64_t)a.b.T * a.heads;
   if (rows <= 1024) {
-    hipLaunchKernelGGL((attend_join_kernel<DT, DV, 8, 8>), dim3((uint32_t)rows), dim3(512), 0, s, a, 1u);
+    hipLaunchKernelGGL((attend_join_kernel<DT, DV, 8, 8, Args>), dim3((uint32_t)rows), dim3(512), 0, s, a, 1u);
   } else {
     const uint32_t most = (uint32_t)std::min<uint64_t>((rows + 8191) / 8192, (a.heads + 3) / 4);
     const uint32_t per_token = (a.heads + 4 * most - 1) / (4 * most);
     const uint32_t some = (a.heads + 4 * per_token - 1) / (4 * per_token);  // the same for each
-    hipLaunchKernelGGL((attend_join_kernel<DT, DV, 4, 1>), dim3(a.b.T * per_token), dim3(256), 0, s, a, some);
+    hipLaunchKernelGGL((attend_join_kernel<DT, DV, 4, 1, Args>), dim3(a.b.T * per_token), dim3(256), 0, s, a, some);
   }
 }
-template <typename DT>
-void launch(const AttendArgs& a, uint32_t value, hipStream_t s) {
+template <typename DT, typename Args>
+void launch(const Args& a, uint32_t value, hipStream_t s) {
   if (value == 64) launch<DT, 64>(a, s);
   else if (value == 128) launch<DT, 128>(a, s);
-  else launch<DT, 512>(a, s);
+  else if constexpr (!IsSight<Args>::value) launch<DT, 512>(a, s);
 }
 
 }  // namespace
 
 void launch_attend_join(const AttendArgs& a, bool f16, uint32_t value, hipStream_t s) {
+  if (f16) launch<F16>(a, value, s);
+  else launch<BF16>(a, value, s);
+}
+void launch_attend_join(const SightArgs& a, bool f16, uint32_t value, hipStream_t s) {
   if (f16) launch<F16>(a, value, s);
   else launch<BF16>(a, value, s);
 }

@@ -25,15 +25,16 @@
 // 128; with 17 to 32 rows 292, one wavefront a SIMD).  One sequence of 65502 keys, one key
 // head (34 MB): 17 us with the join, 2 TB/s: finding the item, two rounds of dependent
 // reads (table, keys) and the second launch.  Eight sequences of 760 keys: 10 us.
-#include "attend.h"
+#include "sight.h"
 
 namespace mori {
 namespace {
 
 constexpr uint32_t NW = 4, STEP = 32;
 
-template <typename DT, int D, int NB>
-__global__ __launch_bounds__(64 * NW) void attend_step_kernel(AttendArgs a) {
+template <typename DT, int D, int NB, typename Args>
+__global__ __launch_bounds__(64 * NW) void attend_step_kernel(Args a) {
+  constexpr bool SIGHT = IsSight<Args>::value;
   constexpr int KS = D / 32;       // matrix steps over the head's elements
   constexpr int E = D / 16;        // value elements of a lane: 4 or 8
   constexpr int VW = E / 2;        // their 32-bit words
@@ -49,12 +50,21 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(AttendArgs a) {
   const uint8_t* const vp = a.b.plane + a.b.plane_bytes + (uint64_t)w.kv * (2 * D) + (2 * E) * n;
 
   u32x4 q[NB][KS];
-  uint32_t limit[NB];
+  uint32_t limit[NB], low[NB];  // a row's keys
+  int32_t pos[NB];              // where it stands
+  float slope[NB];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const uint32_t r = 16 * nb + n;
-    limit[nb] = min(row_limit(a, w, r), w.hi);
-    const u32x4* src = reinterpret_cast<const u32x4*>(q_row(a, row_at(a, w, min(r, w.rows - 1))) + 16 * g);
+    const Keys keys = row_keys(a, w, r);
+    limit[nb] = min(keys.hi, w.hi);
+    const RowAt at = row_at(a, w, min(r, w.rows - 1));
+    const u32x4* src = reinterpret_cast<const u32x4*>(q_row(a, at) + 16 * g);
+    if constexpr (SIGHT) {
+      low[nb] = keys.lo;
+      pos[nb] = w.s.position(at.t - w.s.t0);
+      slope[nb] = slope_of(a, at.h);
+    }
 #pragma unroll
     for (int k = 0; k < KS; ++k) q[nb][k] = q_signed(a, src[4 * k]);
   }
@@ -121,21 +131,31 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(AttendArgs a) {
         load_keys(row);
       }
       // weights
-      const bool mixed = k0 + STEP > w.open || k0 + STEP > w.hi;
+      const bool mixed = k0 + STEP > w.open || k0 + STEP > w.hi || k0 < w.from;
       uint32_t p[NB][4];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
+        if constexpr (SIGHT) {
+          float y[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[i] = s[nb][i / 4][i % 4];
+          shape_scores(a, y, slope[nb], (int32_t)(k0 + 4 * g) - pos[nb], [](int i) { return 16 * (i / 4) + i % 4; });
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s[nb][i / 4][i % 4] = y[i];
+        }
         if (mixed) {
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (k0 + 16 * i + 4 * g + j >= limit[nb]) s[nb][i][j] = -INFINITY;
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t key = k0 + 16 * i + 4 * g + j;
+              if (key >= limit[nb] || (SIGHT && key < low[nb])) s[nb][i][j] = -INFINITY;
+            }
         }
         float m = s[nb][0][0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) m = fmaxf(m, s[nb][i / 4][i % 4]);
-        m = a.c * max_over_16(max_over_32(m));
+        m = (SIGHT ? 1.f : a.c) * max_over_16(max_over_32(m));
         if (__any(risen<DT>(m, top[nb]))) {
           const float t = follow<DT>(m, top[nb]), keep = __builtin_amdgcn_exp2f(top[nb] - t);
           top[nb] = t;
@@ -146,7 +166,8 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(AttendArgs a) {
         float f[8], part = 0;  // of this step: one by one, small weights would be lost in a large sum
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          f[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nb][i / 4][i % 4], a.c, -top[nb]));
+          f[i] = __builtin_amdgcn_exp2f(SIGHT ? s[nb][i / 4][i % 4] - top[nb]
+                                              : __builtin_fmaf(s[nb][i / 4][i % 4], a.c, -top[nb]));
           part += f[i];
         }
         sum[nb] += part;
@@ -163,7 +184,7 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(AttendArgs a) {
             for (int i = 0; i < VW; ++i) vr[j][i] = 0;
           }
       }
-      if (k0 + STEP > w.open && w.open < w.hi) {
+      if (differ(w, k0, STEP)) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -184,7 +205,7 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(AttendArgs a) {
     }
   }
   if (__any(err != 0)) report(a.b, err);
-  if (w.open < w.hi && __syncthreads_or(odd)) {
+  if (differ(w) && __syncthreads_or(odd)) {
     rows_one_by_one<DT, D, D>(a, w, wv, NW, lane);
     return;
   }
@@ -233,7 +254,7 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(AttendArgs a) {
         if (d == 0) a.part_ml[at] = float2{tt, l};
       } else {
         const RowAt at = row_at(a, w, rr);
-        const bool none = row_limit(a, w, rr) == 0;
+        const bool none = row_keys(a, w, rr).none();
         const float inv = none ? 0.f : 1.f / l;
         if (none) y = f32x4{0, 0, 0, 0};
         const u32x2 h = {pair_of<DT>(y[0] * inv, y[1] * inv), pair_of<DT>(y[2] * inv, y[3] * inv)};
@@ -244,16 +265,14 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(AttendArgs a) {
   }
 }
 
-template <typename DT, int D>
-void launch(const AttendArgs& a, hipStream_t s) {
+template <typename DT, int D, typename Args>
+void launch(const Args& a, hipStream_t s) {
   const dim3 grid(a.items * a.kv_heads);
-  if (a.tile_rows == 16) hipLaunchKernelGGL((attend_step_kernel<DT, D, 1>), grid, dim3(64 * NW), 0, s, a);
-  else hipLaunchKernelGGL((attend_step_kernel<DT, D, 2>), grid, dim3(64 * NW), 0, s, a);
+  if (a.tile_rows == 16) hipLaunchKernelGGL((attend_step_kernel<DT, D, 1, Args>), grid, dim3(64 * NW), 0, s, a);
+  else hipLaunchKernelGGL((attend_step_kernel<DT, D, 2, Args>), grid, dim3(64 * NW), 0, s, a);
 }
-
-}  // namespace
-
-void launch_attend_step(const AttendArgs& a, bool f16, uint32_t dim, hipStream_t s) {
+template <typename Args>
+void launch(const Args& a, bool f16, uint32_t dim, hipStream_t s) {
   if (dim == 64) {
     if (f16) launch<F16, 64>(a, s);
     else launch<BF16, 64>(a, s);
@@ -262,5 +281,10 @@ void launch_attend_step(const AttendArgs& a, bool f16, uint32_t dim, hipStream_t
     else launch<BF16, 128>(a, s);
   }
 }
+
+}  // namespace
+
+void launch_attend_step(const AttendArgs& a, bool f16, uint32_t dim, hipStream_t s) { launch(a, f16, dim, s); }
+void launch_attend_step(const SightArgs& a, bool f16, uint32_t dim, hipStream_t s) { launch(a, f16, dim, s); }
 
 }  // namespace mori

@@ -25,7 +25,7 @@
 // other workgroup's products in part only.  Chunks of four sequences (0.2 TFLOP): 287 us,
 // 687 TFLOP/s, with uneven last items and the join; decode steps and chunks mixed
 // (32 sequences, 0.51 GB, 0.12 TFLOP): 270 us.
-#include "attend.h"
+#include "sight.h"
 
 namespace mori {
 namespace {
@@ -45,7 +45,10 @@ struct Tile {
   u32x4 q[KS];
   f32x16 o[DB];
   float top, sum;
-  uint32_t limit, wave_hi;  // keys of a row, most of any row
+  uint32_t limit, wave_hi;  // end of a row's keys, of any row's
+  uint32_t low, wave_lo;    // first of them
+  int32_t pos;              // where the row stands
+  float slope;
   bool odd;                     // a value that rows see in part is infinite or NaN
   uint32_t entry[LD], err;
   // Byte offsets of this thread's chunks from the first row of a load.  They stay
@@ -100,13 +103,24 @@ __device__ inline void drop_tail(const Work& w, uint8_t* area, uint32_t k0, uint
   __syncthreads();
 }
 
+// The same for keys before the first that a row of the tile sees (a page's rows are
+// loaded a few at a time).
+template <typename T>
+__device__ inline void drop_head(const Work& w, uint8_t* area, uint32_t k0, uint32_t tid) {
+  for (uint32_t i = 0; i < T::LD; ++i)
+    if (k0 + i * T::RPL + tid / T::CH < w.key0)
+      *reinterpret_cast<u32x4*>(area + (i * T::NT + tid) * 16) = u32x4{0, 0, 0, 0};
+  __syncthreads();
+}
+
 // One step of 64 keys: these taken from the one area, the next ones' loads set out for the other.
-template <typename DT, int D, bool PAGED>
-__device__ __forceinline__ void step(const AttendArgs& a, const Work& w, Tile<D, PAGED>& x,
+template <typename DT, int D, bool PAGED, typename Args>
+__device__ __forceinline__ void step(const Args& a, const Work& w, Tile<D, PAGED>& x,
                                      const uint8_t* __restrict__ now_k, const uint8_t* __restrict__ now_v,
                                      uint8_t* __restrict__ then_k, uint8_t* __restrict__ then_v, uint32_t k0,
                                      uint32_t tid, uint32_t wv) {
   typedef Tile<D, PAGED> T;
+  constexpr bool SIGHT = IsSight<Args>::value;
   constexpr uint32_t NT = T::NT, ROW = T::ROW, LD = T::LD;
   constexpr int KS = T::KS, DB = T::DB;
   const uint32_t lane = tid & 63, n = lane & 31, h = lane >> 5;
@@ -116,14 +130,15 @@ __device__ __forceinline__ void step(const AttendArgs& a, const Work& w, Tile<D,
   const uint32_t vx = D == 128 ? (vrow & 3) << 2 : ((vrow >> 1) & 1) << 2;
   const uint32_t vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), vsub = 8 * (lane & 1);
   const uint32_t next = min(k0 + STEP, w.hi - 1);  // behind the last step the last key again, for nothing
-  const bool mixed = k0 + STEP > w.open || k0 + STEP > w.hi;
-  if (k0 + STEP > w.open && w.open < w.hi) {
+  const bool mixed = k0 + STEP > w.open || k0 + STEP > w.hi || k0 < w.from;
+  const bool here = k0 < x.wave_hi && (!SIGHT || k0 + STEP > x.wave_lo);
+  if (differ(w, k0, STEP)) {
     for (uint32_t i = 0; i < LD; ++i) {
       const u32x4 v = *reinterpret_cast<const u32x4*>(now_v + (i * NT + tid) * 16);
       for (int j = 0; j < 4; ++j) x.odd |= odd_pair(DT(), v[j]);
     }
   }
-  if (k0 < x.wave_hi) {
+  if (here) {
     const uint8_t* const ks = now_k + n * ROW;
     const uint8_t* const vs = now_v + vrow * ROW + vsub;
     f32x16 s[2];
@@ -140,17 +155,28 @@ __device__ __forceinline__ void step(const AttendArgs& a, const Work& w, Tile<D,
       if (k % T::BETWEEN == 0) x.fetch(a, w, next, then_k, then_v, tid, wv, k / T::BETWEEN);
     }
     uint32_t p[16];
+    if constexpr (SIGHT) {
+      float y[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) y[i] = s[i / 16][i % 16];
+      shape_scores(a, y, x.slope, (int32_t)(k0 + 4 * h) - x.pos,
+                   [](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4; });
+#pragma unroll
+      for (int i = 0; i < 32; ++i) s[i / 16][i % 16] = y[i];
+    }
     if (mixed) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (k0 + 32 * kb + 8 * (i / 4) + 4 * h + i % 4 >= x.limit) s[kb][i] = -INFINITY;
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t key = k0 + 32 * kb + 8 * (i / 4) + 4 * h + i % 4;
+          if (SIGHT ? key - x.low >= x.limit - x.low : key >= x.limit) s[kb][i] = -INFINITY;
+        }
     }
     float m = s[0][0];
 #pragma unroll
     for (int i = 1; i < 32; ++i) m = fmaxf(m, s[i / 16][i % 16]);
-    m = a.c * max_over_32(m);
+    m = (SIGHT ? 1.f : a.c) * max_over_32(m);
     if (__any(risen<DT>(m, x.top))) {
       const float t = follow<DT>(m, x.top), keep = __builtin_amdgcn_exp2f(x.top - t);
       x.top = t;
@@ -161,8 +187,9 @@ __device__ __forceinline__ void step(const AttendArgs& a, const Work& w, Tile<D,
     float part = 0;  // of this step: one by one, small weights would be lost in a large sum
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float f0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 8][2 * i % 16], a.c, -x.top));
-      const float f1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 8][2 * i % 16 + 1], a.c, -x.top));
+      const float y0 = s[i / 8][2 * i % 16], y1 = s[i / 8][2 * i % 16 + 1];
+      const float f0 = __builtin_amdgcn_exp2f(SIGHT ? y0 - x.top : __builtin_fmaf(y0, a.c, -x.top));
+      const float f1 = __builtin_amdgcn_exp2f(SIGHT ? y1 - x.top : __builtin_fmaf(y1, a.c, -x.top));
       part += f0 + f1;
       p[i] = pair_of<DT>(f0, f1);
     }
@@ -178,15 +205,16 @@ __device__ __forceinline__ void step(const AttendArgs& a, const Work& w, Tile<D,
       }
     }
   }
-  if (k0 >= x.wave_hi) {
+  if (!here) {
 #pragma unroll
     for (uint32_t i = 0; i < LD; ++i) x.fetch(a, w, next, then_k, then_v, tid, wv, i);
   }
 }
 
-template <typename DT, int D, bool PAGED>
-__global__ __launch_bounds__(64 * NW, 2) void attend_tile_kernel(AttendArgs a) {
+template <typename DT, int D, bool PAGED, typename Args>
+__global__ __launch_bounds__(64 * NW, 2) void attend_tile_kernel(Args a) {
   typedef Tile<D, PAGED> T;
+  constexpr bool SIGHT = IsSight<Args>::value;
   constexpr int KS = T::KS, DB = T::DB;
   // Arrays of their own, and the loop written out for both: a read of the one area
   // does not wait for loads into another only where the compiler can tell them apart.
@@ -194,7 +222,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tile_kernel(AttendArgs a) {
   __shared__ __align__(256) uint8_t s_v0[T::AREA], s_v1[T::AREA];
   const uint32_t tid = threadIdx.x, lane = tid & 63, wv = wave_index();
   const uint32_t n = lane & 31, h = lane >> 5;
-  const Work w = work_of(a, blockIdx.x, lane);
+  Work w;
+  if constexpr (SIGHT) w = tile_work(a, blockIdx.x, lane);
+  else w = work_of(a, blockIdx.x, lane);
   if (!w.some) return;
   T x;
   x.err = w.s.error;
@@ -209,8 +239,16 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tile_kernel(AttendArgs a) {
   }
   // rows: the wavefront's are 32 * wv + n
   const uint32_t r = 32 * wv + n;
-  x.limit = min(row_limit(a, w, r), w.hi);
-  const u32x4* src = reinterpret_cast<const u32x4*>(q_row(a, row_at(a, w, min(r, w.rows - 1))) + 16 * h);
+  const Keys keys = row_keys(a, w, r);
+  x.limit = min(keys.hi, w.hi);
+  const RowAt mine = row_at(a, w, min(r, w.rows - 1));
+  const u32x4* src = reinterpret_cast<const u32x4*>(q_row(a, mine) + 16 * h);
+  if constexpr (SIGHT) {
+    x.low = min(keys.lo, x.limit);
+    x.pos = w.s.position(mine.t - w.s.t0);
+    x.slope = slope_of(a, mine.h);
+    x.wave_lo = wave_min(x.low < x.limit ? x.low : 0xFFFFFFFFu);
+  }
 #pragma unroll
   for (int k = 0; k < KS; ++k) x.q[k] = q_signed(a, src[2 * k]);
   x.top = NO_TOP;
@@ -229,6 +267,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tile_kernel(AttendArgs a) {
     __syncthreads();
     const auto turn = [&](uint8_t* now_k, uint8_t* now_v, uint8_t* then_k, uint8_t* then_v, uint32_t k0) {
       if (k0 + STEP > w.hi) drop_tail<T>(w, now_v, k0, tid);
+      if (SIGHT && k0 < w.key0) drop_head<T>(w, now_v, k0, tid);
       step<DT>(a, w, x, now_k, now_v, then_k, then_v, k0, tid, wv);
       x.find(a, w, k0 + 2 * STEP, tid);
       wait_loads();
@@ -242,7 +281,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tile_kernel(AttendArgs a) {
     }
   }
   if (__any(x.err != 0)) report(a.b, x.err);
-  if (w.open < w.hi && __syncthreads_or(x.odd)) {
+  if (differ(w) && __syncthreads_or(x.odd)) {
     rows_one_by_one<DT, D, D>(a, w, wv, NW, lane);
     return;
   }
@@ -260,7 +299,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tile_kernel(AttendArgs a) {
     if (h == 0) a.part_ml[at] = float2{x.top, l};
   } else {
     const RowAt at = row_at(a, w, r);
-    const bool none = row_limit(a, w, r) == 0;
+    const bool none = row_keys(a, w, r).none();
     const float inv = 1.f / l;
     uint8_t* out = a.out.data + at.t * a.out.token + at.h * a.out.head;
 #pragma unroll
@@ -275,16 +314,14 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tile_kernel(AttendArgs a) {
   }
 }
 
-template <typename DT, int D>
-void launch(const AttendArgs& a, hipStream_t s) {
+template <typename DT, int D, typename Args>
+void launch(const Args& a, hipStream_t s) {
   const dim3 grid(a.items * a.kv_heads), block(64 * NW);
-  if (a.b.bt % Tile<D, true>::RPW == 0) hipLaunchKernelGGL((attend_tile_kernel<DT, D, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((attend_tile_kernel<DT, D, false>), grid, block, 0, s, a);
+  if (a.b.bt % Tile<D, true>::RPW == 0) hipLaunchKernelGGL((attend_tile_kernel<DT, D, true, Args>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((attend_tile_kernel<DT, D, false, Args>), grid, block, 0, s, a);
 }
-
-}  // namespace
-
-void launch_attend_tile(const AttendArgs& a, bool f16, uint32_t dim, hipStream_t s) {
+template <typename Args>
+void launch(const Args& a, bool f16, uint32_t dim, hipStream_t s) {
   if (dim == 64) {
     if (f16) launch<F16, 64>(a, s);
     else launch<BF16, 64>(a, s);
@@ -293,5 +330,10 @@ void launch_attend_tile(const AttendArgs& a, bool f16, uint32_t dim, hipStream_t
     else launch<BF16, 128>(a, s);
   }
 }
+
+}  // namespace
+
+void launch_attend_tile(const AttendArgs& a, bool f16, uint32_t dim, hipStream_t s) { launch(a, f16, dim, s); }
+void launch_attend_tile(const SightArgs& a, bool f16, uint32_t dim, hipStream_t s) { launch(a, f16, dim, s); }
 
 }  // namespace mori

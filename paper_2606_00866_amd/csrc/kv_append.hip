@@ -52,22 +52,6 @@ struct Place {
 };
 constexpr uint32_t LEFT_ALONE = 0, PADDING = 1, ROTATED = 2, STORED = 3;
 
-// Sequence of token t by a search of a whole wavefront: 64 (then up to 64 more)
-// offsets at once, the number of them that are not past t.
-__device__ inline uint32_t find_sequence(const Batch& b, uint32_t t, uint32_t lane) {
-  const uint32_t stride = (b.B + 63) / 64;
-  uint32_t first = 0;
-  if (stride > 1) {
-    const uint32_t i = min((lane + 1) * stride, b.B);
-    first = (uint32_t)__popcll(__ballot(b.seq_off[i] <= t && i < b.B)) * stride;
-  }
-  const uint32_t j = first + lane + 1;
-  const bool in = lane < stride && j < b.B;
-  return min(first + (uint32_t)__popcll(__ballot(stride > 1 ? in && b.seq_off[in ? j : 0] <= t
-                                                             : j < b.B && b.seq_off[min(j, b.B)] <= t)),
-             b.B - 1);
-}
-
 // `axis`: of the lanes below the number of axes, the token's position on theirs.
 template <bool AXES>
 __device__ inline Place place_of(const AppendArgs& a, uint32_t t, uint32_t lane, uint32_t* err, uint32_t* axis) {

@@ -4,28 +4,29 @@
 //   out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m), m at or near the largest s_j
 //
 // Three kernels by what bounds them (few rows per key head, many, latent rows),
-// and one that joins the runs of split contexts; see attend.h for what they share.
+// and one that joins the runs of split contexts; see attend.h for what they share, and
+// sight.h for what a call may say of scores and of the keys that a token sees.
 #include <algorithm>
 #include <cmath>
 
-#include "attend.h"
+#include "sight.h"
 
 namespace mori {
 namespace {
 
 // How a batch is run.
 struct Plan {
-  AttendArgs a;
+  SightArgs a;
   uint32_t dim, value;
   bool f16, step, latent;
-  uint64_t ml_at, bytes;  // workspace
+  uint64_t ml_at, span_at, tile_at, seq_at, bytes;  // workspace
 };
 
 // Host check of what the call and its workspace size take, and the schedule.
-bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, const mori_attend* at, uint32_t* error,
-             Plan* out) {
+bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, const mori_attend* at,
+             const mori_sight* sight, uint32_t* error, Plan* out) {
   Plan& p = *out;
-  AttendArgs& a = p.a;
+  SightArgs& a = p.a;
   if (!at || !batch_of(pool, layer, tokens, error, &a.b)) return false;
   if (at->dtype > MORI_DT_BF16 || !at->kv_heads || !at->q_heads || at->q_heads > 1024) return false;
   if (at->q_heads % at->kv_heads || !std::isfinite(at->scale)) return false;
@@ -62,6 +63,25 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
     a.unit = 64;
   }
   const uint64_t tiles = (uint64_t)a.b.T * a.group / a.tile_rows + a.b.B;  // no batch has more
+  uint64_t most = a.b.max_kv;  // keys of a tile
+  if (sight) {
+    if (p.latent || !std::isfinite(sight->cap) || sight->cap < 0) return false;
+    if ((reinterpret_cast<uintptr_t>(sight->slopes) | reinterpret_cast<uintptr_t>(sight->first) |
+         reinterpret_cast<uintptr_t>(sight->end)) & 3u)
+      return false;
+    if (sight->cap > 0) {
+      a.cap = sight->cap * 1.4426950408889634f;
+      a.cap_in = at->scale == 0 ? 1.f : std::fabs(at->scale) / sight->cap;
+      if (!std::isfinite(a.cap) || !std::isfinite(a.cap_in) || a.cap == 0) return false;
+    }
+    a.slopes = sight->slopes;
+    a.window = sight->window;
+    a.first = sight->first;
+    a.end = sight->end;
+    a.align = p.step || a.b.bt % (512 / p.dim) ? 1 : 512 / p.dim;  // rows that a wavefront loads at once from a page
+    if (a.window && !a.end) most = std::min<uint64_t>(most, (uint64_t)a.window + a.b.max_new);
+    most += a.align;
+  }
   // Items that fill the chip a few times over (measured on decode steps, chunks and mixed
   // batches: half of these leave 2-10% to uneven items, twice as many cost that in
   // partial sums and joins); 128 latent rows are 256 KiB of partial sums an item.
@@ -75,38 +95,39 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
   // That holds for lengths alike.  One context far longer than the rest is then one
   // workgroup's a key head: 256 programs behind 500 keys, one of them behind 65536, 866 us
   // against 186; a prompt of 8192 with one such program 2220 against 862.
-  a.splits = a.b.max_kv > a.least * a.unit && tiles * a.kv_heads < 2048;
+  a.splits = most > a.least * a.unit && tiles * a.kv_heads < 2048;
   // runs have `least` units or more, so short contexts give fewer items than slots
-  const uint64_t runs = tiles * (((uint64_t)a.b.max_kv + a.unit - 1) / a.unit) / a.least;
+  const uint64_t runs = tiles * ((most + a.unit - 1) / a.unit) / a.least;
   const uint64_t items = tiles + (a.splits ? std::min<uint64_t>(a.slots, runs + 1) : 0);
   const uint64_t threads = p.latent && a.tile_rows == 128 ? 512 : 256;  // of a workgroup
   if (items * a.kv_heads * threads >= (1ull << 32)) return false;  // a launch has fewer
   a.items = (uint32_t)items;
   const uint64_t n = a.splits ? items * a.kv_heads * a.tile_rows : 0;
   p.ml_at = n * p.value * sizeof(float);
-  p.bytes = p.ml_at + n * sizeof(float2);
+  p.span_at = p.bytes = p.ml_at + n * sizeof(float2);
+  if (sight && !p.step) {
+    p.span_at = (p.span_at + 15) / 16 * 16;
+    p.tile_at = p.span_at + (tiles + 1) / 2 * 16;
+    p.seq_at = p.tile_at + tiles * sizeof(uint4);
+    p.bytes = p.seq_at + (uint64_t)a.b.B * sizeof(uint32_t);
+    a.tiles = (uint32_t)tiles;
+  }
   return true;
 }
 
-}  // namespace
-}  // namespace mori
-
-extern "C" int mori_kv_attend_workspace(const mori_pool* pool, const mori_tokens* tokens, const mori_attend* attend,
-                                        uint64_t* bytes) {
-  using namespace mori;
+int workspace_of(const mori_pool* pool, const mori_tokens* tokens, const mori_attend* attend, const mori_sight* sight,
+                 uint64_t* bytes) {
   Plan p{};
-  if (!bytes || !plan_of(pool, 0, tokens, attend, nullptr, &p)) return MORI_EINVAL;
+  if (!bytes || !plan_of(pool, 0, tokens, attend, sight, nullptr, &p)) return MORI_EINVAL;
   *bytes = p.bytes;
   return MORI_OK;
 }
 
-extern "C" int mori_kv_attend(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens,
-                              const mori_attend* attend, void* workspace, uint64_t workspace_bytes, uint32_t* error,
-                              void* stream) {
-  using namespace mori;
+int attend_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, const mori_attend* attend,
+              const mori_sight* sight, void* workspace, uint64_t workspace_bytes, uint32_t* error, void* stream) {
   Plan p{};
-  if (!plan_of(pool, layer, tokens, attend, error, &p)) return MORI_EINVAL;
-  AttendArgs& a = p.a;
+  if (!plan_of(pool, layer, tokens, attend, sight, error, &p)) return MORI_EINVAL;
+  SightArgs& a = p.a;
   if (a.b.T == 0) return MORI_OK;
   if (!rows_valid(attend->q) || !rows_valid(attend->out)) return MORI_EINVAL;
   if (p.bytes && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < p.bytes))
@@ -114,13 +135,56 @@ extern "C" int mori_kv_attend(const mori_pool* pool, uint32_t layer, const mori_
   a.q = rows_of(attend->q);
   a.out = rows_of(attend->out);
   a.lse = attend->lse;
+  uint8_t* const ws = static_cast<uint8_t*>(workspace);
   a.part = static_cast<float*>(workspace);
-  a.part_ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + p.ml_at);
+  a.part_ml = reinterpret_cast<float2*>(ws + p.ml_at);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (p.step) launch_attend_step(a, p.f16, p.dim, s);
-  else if (p.latent) launch_attend_latent(a, p.f16, s);
-  else launch_attend_tile(a, p.f16, p.dim, s);
-  if (a.splits) launch_attend_join(a, p.f16, p.value, s);
+  const auto run = [&](const auto& args) {
+    if (p.step) launch_attend_step(args, p.f16, p.dim, s);
+    else launch_attend_tile(args, p.f16, p.dim, s);
+    if (a.splits) launch_attend_join(args, p.f16, p.value, s);
+  };
+  if (sight) {
+    if (!p.step) {
+      a.span = reinterpret_cast<uint2*>(ws + p.span_at);
+      a.tile = reinterpret_cast<uint4*>(ws + p.tile_at);
+      a.seq_tile = reinterpret_cast<uint32_t*>(ws + p.seq_at);
+      launch_sight_tiles(a, s);
+    }
+    run(a);
+  } else if (p.latent) {
+    launch_attend_latent(a, p.f16, s);
+    if (a.splits) launch_attend_join(static_cast<const AttendArgs&>(a), p.f16, p.value, s);
+  } else {
+    run(static_cast<const AttendArgs&>(a));
+  }
   if (hipGetLastError() != hipSuccess) return MORI_EHIP;
   return MORI_OK;
+}
+
+}  // namespace
+}  // namespace mori
+
+extern "C" int mori_kv_attend_workspace(const mori_pool* pool, const mori_tokens* tokens, const mori_attend* attend,
+                                        uint64_t* bytes) {
+  return mori::workspace_of(pool, tokens, attend, nullptr, bytes);
+}
+
+extern "C" int mori_kv_attend(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens,
+                              const mori_attend* attend, void* workspace, uint64_t workspace_bytes, uint32_t* error,
+                              void* stream) {
+  return mori::attend_of(pool, layer, tokens, attend, nullptr, workspace, workspace_bytes, error, stream);
+}
+
+extern "C" int mori_kv_attend_sight_workspace(const mori_pool* pool, const mori_tokens* tokens,
+                                              const mori_attend* attend, const mori_sight* sight, uint64_t* bytes) {
+  if (!sight) return MORI_EINVAL;
+  return mori::workspace_of(pool, tokens, attend, sight, bytes);
+}
+
+extern "C" int mori_kv_attend_sight(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens,
+                                    const mori_attend* attend, const mori_sight* sight, void* workspace,
+                                    uint64_t workspace_bytes, uint32_t* error, void* stream) {
+  if (!sight) return MORI_EINVAL;
+  return mori::attend_of(pool, layer, tokens, attend, sight, workspace, workspace_bytes, error, stream);
 }

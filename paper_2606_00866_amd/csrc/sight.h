@@ -1,0 +1,271 @@
+// Attention that is told more of its scores and of what a token sees:
+//
+//   s_ij = scale * q_i . k_j
+//   s_ij <- cap * tanh(s_ij / cap)                              (capped)
+//   s_ij <- s_ij - slope_h * |i - j|                            (a bias by distance)
+//   j is seen by i where  max(first_i, i + 1 - window, 0) <= j < min(end_i, length)
+//
+// with i, j positions in the program and end_i = i + 1 unless given.  Documents,
+// prefixes, spans that see each other and windows are such ranges, so every row's keys
+// are an interval: a tile reads the union of its rows' intervals, and only steps that
+// some row sees in part are masked.
+//
+// Items.  As in attend.h, but a tile's keys are those its rows see, so a window over a
+// long context gives as many items as the window has work for.  Batches whose sequences
+// are one tile each (decode steps) find that from the lengths and ranges themselves;
+// the others have the tiles' ranges written down by a small kernel first, since every
+// workgroup would read all tokens' ranges otherwise.
+//
+// tanh.  With all scores of a step and wavefront below the cap, tanh x is x P(x^2), P of
+// six terms with a relative error of 7e-7 (a minimax fit on [0, 1]); else 1 - 2 / (e^2x
+// + 1) where |x| >= 1.  The polynomial costs seven full-rate instructions, the other form
+// two at a quarter of the rate and three more; small scores keep their relative accuracy
+// whatever the cap.
+#pragma once
+#include "attend.h"
+
+namespace mori {
+
+struct SightArgs : AttendArgs {
+  float cap, cap_in;   // log2(e) * cap; |scale| / cap.  0: none
+  const float* slopes;
+  uint32_t window;     // 0: none
+  const int32_t *first, *end;
+  // tiles as written down (no array: a sequence is a tile)
+  uint32_t tiles;      // bound on their number
+  uint32_t align;      // a tile's keys are taken from a multiple of this on
+  uint2* span;         // [tiles] keys lo .. hi - 1 of its rows; lo > hi: no tile
+  uint4* tile;         // [tiles] from, open, sequence, first row
+  uint32_t* seq_tile;  // [B] a sequence's first one
+};
+
+// Keys of token i of a sequence.
+__device__ inline Keys token_keys(const SightArgs& a, const Seq& s, uint32_t i) {
+  const int32_t pos = s.position(i);
+  if (pos < 0) return {0, 0};
+  int32_t lo = a.window && (uint32_t)pos >= a.window ? pos + 1 - (int32_t)a.window : 0, hi = pos + 1;
+  if (a.first) lo = max(lo, a.first[s.t0 + i]);
+  if (a.end) hi = min(a.end[s.t0 + i], (int32_t)s.len);
+  if (hi <= lo) return {0, 0};
+  return {(uint32_t)lo, (uint32_t)hi};
+}
+__device__ inline Keys row_keys(const SightArgs& a, const Work& w, uint32_t r) {
+  if (r >= w.rows) return {0, 0};
+  return token_keys(a, w.s, divide(w.row0 + r, a.by_group));
+}
+
+// A sequence as one tile, for the scan over the sequences.
+__device__ inline Share share_of(const SightArgs& a, uint32_t b) {
+  Share s = share_of(static_cast<const AttendArgs&>(a), b);
+  if (s.bad || !s.n) return s;
+  s.units = 1;
+  Seq q{};
+  q.t0 = a.b.seq_off[b];
+  q.n = s.n;
+  q.len = a.b.kv_len[b];
+  if (q.n > a.b.max_new || q.len > a.b.max_kv) return s;
+  uint32_t lo = 0xFFFFFFFFu, hi = 0;
+  if (!a.first && !a.end) {  // the first token's and the last one's
+    lo = token_keys(a, q, q.len < q.n ? q.n - q.len : 0).lo;
+    hi = q.len;
+  } else {
+    for (uint32_t i = 0; i < q.n; ++i) {
+      const Keys k = token_keys(a, q, i);
+      if (k.none()) continue;
+      lo = min(lo, k.lo);
+      hi = max(hi, k.hi);
+    }
+  }
+  if (hi > lo) s.units = (hi - lo + a.unit - 1) / a.unit;
+  return s;
+}
+
+struct Max {
+  __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return max(a, b); }
+};
+__device__ inline uint32_t wave_max(uint32_t v) { return wave::lane63(wave::incl(v, Max())); }
+__device__ inline uint32_t wave_min(uint32_t v) { return ~wave_max(~v); }
+
+// What the rows of some tokens see together, and what all of them see.
+struct Union {
+  uint32_t lo, hi, from, open;
+};
+__device__ inline Union union_of(const SightArgs& a, const Seq& s, uint32_t i0, uint32_t i1, uint32_t lane) {
+  uint32_t lo = 0xFFFFFFFFu, hi = 0, from = 0, open = 0xFFFFFFFFu;
+  for (uint32_t i = i0 + lane; i < i1; i += 64) {
+    const Keys k = token_keys(a, s, i);
+    if (k.none()) {  // sees nothing: nothing is open to all
+      from = 0xFFFFFFFFu;
+      open = 0;
+      continue;
+    }
+    lo = min(lo, k.lo);
+    hi = max(hi, k.hi);
+    from = max(from, k.lo);
+    open = min(open, k.hi);
+  }
+  Union u{wave_min(lo), wave_max(hi), wave_max(from), wave_min(open)};
+  if (u.lo >= u.hi) u.lo = u.hi = 0;
+  return u;
+}
+
+__device__ inline void set_run(const SightArgs& a, Work& w, const Union& u, uint32_t run, uint32_t run_units) {
+  const uint32_t start = u.lo / a.align * a.align;
+  const uint64_t lo = start + (uint64_t)run * run_units * a.unit, hi = lo + (uint64_t)run_units * a.unit;
+  w.key0 = u.lo;
+  w.from = u.from;
+  w.open = u.open;
+  w.lo = same((uint32_t)min(lo, (uint64_t)0x7FFFFFFFu));
+  w.hi = same((uint32_t)min(hi, (uint64_t)u.hi));
+}
+
+// The item of a batch whose sequences are one tile each.
+__device__ inline Work work_of(const SightArgs& a, uint32_t block, uint32_t lane) {
+  Work w{};
+  w.item = divide(block, a.by_kv);
+  w.kv = block - w.item * a.kv_heads;
+  const uint32_t item = w.item;
+  const Item it = find_item(a, lane, [&](uint32_t first, uint32_t n, uint32_t) { return item - first < n; });
+  w.some = it.found;
+  if (block == 0 && it.bad) report(a.b, MORI_DEV_BAD_TOKENS);
+  if (!w.some) return w;
+  SeqNumbers x = read_sequence(a.b, it.b);
+  w.s = checked_sequence(a.b, SeqNumbers{same(x.lo), same(x.hi), same(x.len), same(x.p), same(x.first), same(x.last)});
+  // more rows than a tile has only where the batch brings more tokens than it may: padding
+  const uint32_t k = w.item - it.first, back = k / it.per_tile, run = k - back * it.per_tile;
+  const uint32_t tiles = (w.s.n * a.group + a.tile_rows - 1) / a.tile_rows;
+  w.per_tile = it.per_tile;
+  w.row0 = same((tiles - 1 - back) * a.tile_rows);
+  w.rows = min(a.tile_rows, w.s.n * a.group - w.row0);
+  Union u{0, 0, 0, 0};
+  if (!w.s.error) u = union_of(a, w.s, 0, w.s.n, lane);
+  set_run(a, w, u, run, it.run_units);
+  return w;
+}
+
+// A tile and its run among those written down.
+struct TileRun {
+  uint32_t tile, first, per_tile, run_units;  // first: its first item
+  bool found;
+};
+// `tile` for its items, or else the tile of `item`; the same for the whole wavefront.
+__device__ inline TileRun find_tile(const SightArgs& a, uint32_t lane, uint32_t item, uint32_t tile, bool by_item) {
+  const uint32_t k = (a.tiles + 63) / 64, t0 = lane * k;
+  const auto units = [&](uint32_t t) {
+    const uint2 s = a.span[t];
+    const uint32_t n = (s.y - s.x / a.align * a.align + a.unit - 1) / a.unit;
+    return s.x > s.y ? 0u : n ? n : 1u;  // an empty tile is an item too: its rows are 0
+  };
+  uint64_t total = 0;
+  for (uint32_t t = t0; t < min(t0 + k, a.tiles); ++t) total += units(t);
+  total = wave::sum(total);
+  TileRun r{};
+  r.run_units = (uint32_t)max((uint64_t)a.least, (total + a.slots - 1) / a.slots);
+  uint32_t mine = 0;
+  for (uint32_t t = t0; t < min(t0 + k, a.tiles); ++t) mine += (units(t) + r.run_units - 1) / r.run_units;
+  uint32_t first = wave::incl_add(mine) - mine, hit = 0xFFFFFFFFu, hit_first = 0, hit_per = 1;
+  for (uint32_t t = t0; t < min(t0 + k, a.tiles); ++t) {
+    const uint32_t n = (units(t) + r.run_units - 1) / r.run_units;
+    if (by_item ? item - first < n : t == tile && n) {
+      hit = t;
+      hit_first = first;
+      hit_per = n;
+    }
+    first += n;
+  }
+  const uint64_t who = __ballot(hit != 0xFFFFFFFFu);
+  r.found = who != 0;
+  if (!r.found) return r;
+  const int l = __ffsll((unsigned long long)who) - 1;
+  r.tile = (uint32_t)__builtin_amdgcn_readlane((int)hit, l);
+  r.first = (uint32_t)__builtin_amdgcn_readlane((int)hit_first, l);
+  r.per_tile = (uint32_t)__builtin_amdgcn_readlane((int)hit_per, l);
+  return r;
+}
+
+// The item of a batch whose tiles are written down.
+__device__ inline Work tile_work(const SightArgs& a, uint32_t block, uint32_t lane) {
+  Work w{};
+  w.item = divide(block, a.by_kv);
+  w.kv = block - w.item * a.kv_heads;
+  TileRun r{w.item, w.item, 1, 0x7FFFFFFFu, w.item < a.tiles};
+  if (a.splits) r = find_tile(a, lane, w.item, 0, true);
+  if (!r.found) return w;
+  const uint2 span = a.span[r.tile];
+  if (same(span.x) > same(span.y)) return w;
+  const uint4 t = a.tile[r.tile];
+  w.some = true;
+  const SeqNumbers x = read_sequence(a.b, same(t.z));
+  w.s = checked_sequence(a.b, SeqNumbers{same(x.lo), same(x.hi), same(x.len), same(x.p), same(x.first), same(x.last)});
+  w.row0 = same(t.w);
+  w.rows = min(a.tile_rows, w.s.n * a.group - w.row0);
+  w.per_tile = r.per_tile;
+  set_run(a, w, Union{same(span.x), same(span.y), same(t.x), same(t.y)}, w.item - r.first, r.run_units);
+  return w;
+}
+
+// tanh, where all of a wavefront's arguments are below 1, and anywhere.
+__device__ inline float tanh_small(float x) {
+  const float u = x * x;
+  float p = __builtin_fmaf(u, -0.003067060373723507f, 0.016743116080760956f);
+  p = __builtin_fmaf(u, p, -0.051605675369501114f);
+  p = __builtin_fmaf(u, p, 0.13281433284282684f);
+  p = __builtin_fmaf(u, p, -0.3332904279232025f);
+  return x * __builtin_fmaf(u, p, 0.9999994039535522f);
+}
+__device__ inline float tanh_any(float x) {
+  const float big = 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * 2.8853900817779268f) + 1.f);
+  return fabsf(x) < 1.f ? tanh_small(x) : big;
+}
+
+// Scores of one row (or, lane by lane, of several) in the softmax's units from the
+// products of queries and keys; key(i) is what the i-th one's key is ahead of `base`.
+template <int N, typename K>
+__device__ __forceinline__ void shape_scores(const SightArgs& a, float (&y)[N], float slope, int32_t base, K key) {
+  if (a.cap != 0) {
+    float big = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      y[i] *= a.cap_in;
+      big = fmaxf(big, fabsf(y[i]));
+    }
+    if (__any(big >= 1.f)) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) y[i] = a.cap * tanh_any(y[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) y[i] = a.cap * tanh_small(y[i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] *= a.c;
+  }
+  if (a.slopes) {
+    const float b = (float)base;
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = __builtin_fmaf(-slope, fabsf(b + (float)key(i)), y[i]);
+  }
+}
+// log2(e) * slope of a head.
+__device__ inline float slope_of(const SightArgs& a, uint32_t h) {
+  return a.slopes ? 1.4426950408889634f * a.slopes[h] : 0.f;
+}
+__device__ inline auto score_of(const SightArgs& a, const Work& w, uint32_t r, uint32_t h) {
+  const int32_t pos = w.s.position(divide(w.row0 + r, a.by_group));
+  return [&a, slope = slope_of(a, h), pos](float s, uint32_t key) {
+    float y = a.cap != 0 ? a.cap * tanh_any(s * a.cap_in) : s * a.c;
+    if (a.slopes) y = __builtin_fmaf(-slope, fabsf((float)((int32_t)key - pos)), y);
+    return y;
+  };
+}
+
+template <typename Args>
+struct IsSight {
+  static constexpr bool value = false;
+};
+template <>
+struct IsSight<SightArgs> {
+  static constexpr bool value = true;
+};
+
+}  // namespace mori

@@ -41,7 +41,8 @@ EXPORTS = ("mori_create", "mori_destroy", "mori_register", "mori_host_alloc", "m
            "mori_rank_partition", "mori_plan_wait", "mori_kv_swap_out", "mori_kv_swap_in", "mori_query",
            "mori_strerror", "mori_profile", "mori_profile_read", "mori_evict_workspace", "mori_evict_order",
            "mori_replica_admit", "mori_evict_order_noalloc", "mori_kv_append", "mori_kv_attend_workspace",
-           "mori_kv_attend", "mori_tables_grow_workspace", "mori_tables_grow", "mori_kv_append_axes")
+           "mori_kv_attend", "mori_tables_grow_workspace", "mori_tables_grow", "mori_kv_append_axes",
+           "mori_kv_attend_sight_workspace", "mori_kv_attend_sight")
 
 
 class mori_pool(C.Structure):
@@ -98,6 +99,11 @@ class mori_attend(C.Structure):
         ("scale", C.c_float), ("q", mori_rows), ("out", mori_rows), ("lse", C.c_void_p)]
 
 
+class mori_sight(C.Structure):
+    _fields_ = [("cap", C.c_float), ("window", C.c_uint32), ("slopes", C.c_void_p), ("first", C.c_void_p),
+                ("end", C.c_void_p)]
+
+
 class mori_plan(C.Structure):
     _fields_ = [(n, C.c_uint32) for n in (
         "num_programs", "m_gpu", "m_cpu", "n_out", "n_in", "n_drop_gpu", "n_drop_cpu", "n_admit_gpu",
@@ -143,6 +149,9 @@ def lib():
         L.mori_kv_append_axes.argtypes = [PP, U32, PT, C.POINTER(mori_append), C.POINTER(mori_axes), V, V]
         L.mori_kv_attend_workspace.argtypes = [PP, PT, C.POINTER(mori_attend), C.POINTER(U64)]
         L.mori_kv_attend.argtypes = [PP, U32, PT, C.POINTER(mori_attend), V, U64, V, V]
+        PA, PS = C.POINTER(mori_attend), C.POINTER(mori_sight)
+        L.mori_kv_attend_sight_workspace.argtypes = [PP, PT, PA, PS, C.POINTER(U64)]
+        L.mori_kv_attend_sight.argtypes = [PP, U32, PT, PA, PS, V, U64, V, V]
         L.mori_tables_grow_workspace.argtypes = [PP, C.POINTER(mori_growth), C.POINTER(U64)]
         L.mori_tables_grow.argtypes = [PP, C.POINTER(mori_growth), V, U64, V, V]
         L.mori_strerror.restype = C.c_char_p
@@ -258,6 +267,18 @@ def mori_kv_attend(pool: mori_pool, layer: int, tokens: mori_tokens, attend: mor
                    workspace_bytes: int, error: int = 0, stream: int = 0) -> int:
     return lib().mori_kv_attend(C.byref(pool), layer, C.byref(tokens), C.byref(attend), workspace or None,
                                 workspace_bytes, error or None, stream)
+
+
+def mori_kv_attend_sight_workspace(pool: mori_pool, tokens: mori_tokens, attend: mori_attend, sight: mori_sight):
+    b = C.c_uint64()
+    rc = lib().mori_kv_attend_sight_workspace(C.byref(pool), C.byref(tokens), C.byref(attend), C.byref(sight), C.byref(b))
+    return rc, b.value
+
+
+def mori_kv_attend_sight(pool: mori_pool, layer: int, tokens: mori_tokens, attend: mori_attend, sight: mori_sight,
+                         workspace: int, workspace_bytes: int, error: int = 0, stream: int = 0) -> int:
+    return lib().mori_kv_attend_sight(C.byref(pool), layer, C.byref(tokens), C.byref(attend), C.byref(sight),
+                                      workspace or None, workspace_bytes, error or None, stream)
 
 
 def mori_tables_grow_workspace(pool: mori_pool, growth: mori_growth):

@@ -1,0 +1,315 @@
+"""Attention with caps, biases by distance, windows and ranges, against the definition in
+64 bits.  Free pages, other layers and rows past a program's length hold NaN."""
+import numpy as np
+import pytest
+import torch
+
+import attend_ref as R
+import sight_ref as S
+from paper_2606_00866_amd import attention as A
+from paper_2606_00866_amd import mori as M
+from paper_2606_00866_amd.tiering import MoriError
+
+pytestmark = pytest.mark.gpu
+F16, BF16 = torch.float16, torch.bfloat16
+
+
+def queries(inst, H, scale=2.5, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(int(inst.n.sum()), H, inst.dim, generator=g) * scale).to(inst.dtype)
+
+
+def positions(inst):
+    return np.concatenate([np.arange(l - n, l) for n, l in zip(inst.n, inst.length)]).astype(np.int64)
+
+
+def documents(inst, mean, seed=1):
+    """Where each token's document begins."""
+    rng, out = np.random.default_rng(seed), []
+    for n, l in zip(inst.n.tolist(), inst.length.tolist()):
+        starts = np.concatenate([[0], np.cumsum(rng.integers(1, 2 * mean + 1, 2 + 4 * l // mean))])
+        pos = np.arange(l - n, l)
+        out.append(np.where(pos < 0, 0, starts[np.maximum(np.searchsorted(starts, pos, side="right") - 1, 0)]))
+    return np.concatenate(out).astype(np.int32)
+
+
+def slopes_of(H):
+    return np.exp2(-8.0 * np.arange(1, H + 1) / H).astype(np.float32)
+
+
+def dev(x):
+    return None if x is None else torch.from_numpy(np.ascontiguousarray(x)).cuda()
+
+
+def run(inst, q, scale, lse=True, **kw):
+    b = R.batch(inst)
+    out = torch.full((*q.shape,), float("nan"), dtype=q.dtype, device="cuda")
+    l = torch.full(q.shape[:2], float("nan"), device="cuda") if lse else None
+    k = {n: dev(x) if isinstance(x, np.ndarray) else x for n, x in kw.items()}
+    A.kv_attend(inst.pool.cuda(), inst.geom, inst.layer, b, q.cuda(), scale=scale, out=out, lse=l, **k)
+    b.check()
+    return out.double().cpu().numpy(), l.double().cpu().numpy() if lse else None
+
+
+def compare(inst, q, scale, **kw):
+    out, lse = run(inst, q, scale, **kw)
+    want, want_lse, bound, delta = S.attend(inst, q, scale, **kw)
+    bad = ~(np.abs(out - want) <= bound)
+    assert not bad.any(), (np.argwhere(bad)[:3], np.abs(out - want)[bad][:3], bound[bad][:3])
+    none = np.isneginf(want_lse)
+    assert (np.isneginf(lse) == none).all() and (out[none] == 0).all()
+    # the sum's error: every weight by its score's, the sum and the logarithm by 2^-16
+    assert (np.abs(lse - want_lse)[~none] <= (2 * delta + 2.0 ** -16 * (1 + np.abs(want_lse)))[~none]).all()
+
+
+SIGHTS = {
+    "cap": lambda inst, H: dict(cap=20.0),
+    "cap_below_scores": lambda inst, H: dict(cap=2.0),
+    "large_cap": lambda inst, H: dict(cap=30000.0),
+    "slopes": lambda inst, H: dict(slopes=slopes_of(H)),
+    "window": lambda inst, H: dict(window=37),
+    "window_of_one": lambda inst, H: dict(window=1),
+    "wide_window": lambda inst, H: dict(window=100000),
+    "documents": lambda inst, H: dict(first=documents(inst, 30)),
+    "long_documents": lambda inst, H: dict(first=documents(inst, 300)),
+    "prefix": lambda inst, H: dict(end=np.maximum(positions(inst) + 1, 50).astype(np.int32)),
+    "all_see_all": lambda inst, H: dict(end=np.full(int(inst.n.sum()), 1 << 30, np.int32)),
+    "everything": lambda inst, H: dict(cap=15.0, slopes=slopes_of(H), window=90, first=documents(inst, 200),
+                                       end=(positions(inst) + 1 + np.arange(int(inst.n.sum())) % 40).astype(np.int32)),
+}
+# n, length, kv, q heads, dim, bt: steps of 16 and 32 rows, tiles of 128, split and whole
+FORMS = {
+    "step": ([1] * 5, [1, 33, 300, 700, 64], 2, 8, 64, 16),
+    "step_long": ([1, 1], [5000, 1700], 1, 8, 128, 16),
+    "few": ([4, 1, 3], [4, 90, 400], 2, 8, 128, 16),
+    "few_32": ([4, 2], [60, 900], 1, 8, 64, 24),
+    "tile": ([70, 1, 33], [70, 400, 600], 2, 4, 128, 16),
+    "tile_64": ([50, 20], [700, 20], 1, 5, 64, 32),
+    "tile_odd_pages": ([40, 9], [300, 150], 1, 8, 128, 7),
+    "tile_odd_pages_64": ([60], [500], 2, 2, 64, 12),
+    "tile_many_heads": ([5, 2], [200, 90], 1, 160, 64, 16),
+    "prompt": ([260], [260], 1, 3, 128, 16),
+}
+
+
+@pytest.mark.parametrize("sight", SIGHTS)
+@pytest.mark.parametrize("form", FORMS)
+def test_against_definition(form, sight):
+    n, length, kv, H, dim, bt = FORMS[form]
+    dtype = F16 if len(form + sight) % 3 == 0 else BF16
+    inst = R.instance(len(form) * 31 + len(sight), n, length, kv=kv, dim=dim, dtype=dtype, bt=bt)
+    q = queries(inst, H, 8.0 if "cap" in sight else 2.5)
+    compare(inst, q, dim ** -0.5, **SIGHTS[sight](inst, H))
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("form", ["step", "few", "tile", "tile_odd_pages"])
+def test_a_sight_that_says_nothing(form, dtype):
+    """A window past every length: the plain call's result within the same bound, and a
+    call with ranges that are the causal ones gives the same bits."""
+    n, length, kv, H, dim, bt = FORMS[form]
+    inst = R.instance(77, n, length, kv=kv, dim=dim, dtype=dtype, bt=bt)
+    q = queries(inst, H)
+    compare(inst, q, dim ** -0.5, window=1 << 31)
+    a, la = run(inst, q, dim ** -0.5, window=1 << 31)
+    b, lb = run(inst, q, dim ** -0.5, first=np.full(q.shape[0], -5, np.int32), end=(positions(inst) + 1).astype(np.int32))
+    assert np.array_equal(a, b) and np.array_equal(la, lb)
+
+
+@pytest.mark.parametrize("form", ["step", "few", "tile"])
+def test_rows_that_see_nothing(form):
+    """Some tokens' ranges are empty, upside down or outside: zeros, and no others change."""
+    n, length, kv, H, dim, bt = FORMS[form]
+    inst = R.instance(78, n, length, kv=kv, dim=dim, bt=bt)
+    q = queries(inst, H)
+    T = q.shape[0]
+    first, end = np.zeros(T, np.int32), (positions(inst) + 1).astype(np.int32)
+    whole, _ = run(inst, q, 0.1, first=first, end=end)
+    f, e = first.copy(), end.copy()
+    f[0], e[0] = 5, 5
+    if T > 2:
+        f[1], e[1] = 2 ** 31 - 1, 2 ** 31 - 1
+        f[2], e[2] = 0, -2 ** 31
+    if T > 4:
+        f[4] = 100000
+    compare(inst, q, 0.1, first=f, end=e)
+    out, _ = run(inst, q, 0.1, first=f, end=e)
+    empty = [0] + ([1, 2] if T > 2 else []) + ([4] if T > 4 else [])
+    assert (out[empty] == 0).all()
+    if form == "step":
+        rest = np.setdiff1d(np.arange(T), empty)
+        assert np.array_equal(out[rest], whole[rest])
+    none = np.full(T, 1 << 30, np.int32)
+    out, lse = run(inst, q, 0.1, first=none)
+    assert (out == 0).all() and np.isneginf(lse).all()
+
+
+def test_padding():
+    """Tokens before position 0: zeros, whatever their ranges say."""
+    inst = R.instance(79, [8, 40], [3, 20], kv=2, dim=64)
+    q = queries(inst, 4)
+    for kw in (dict(window=2), dict(first=np.zeros(48, np.int32), end=np.full(48, 9, np.int32)), dict(cap=5.0)):
+        compare(inst, q, 0.125, **kw)
+
+
+def test_unseen_pages_need_not_be_there():
+    """Pages that no token's range reaches hold no page id: nothing is reported."""
+    for n, length, kv, H, dim, bt in (([1, 1], [900, 500], 2, 8, 64, 16), ([40], [2000], 1, 8, 128, 16),
+                                      ([40], [2000], 1, 8, 128, 12), ([40], [2000], 1, 8, 64, 12)):
+        inst = R.instance(80, n, length, kv=kv, dim=dim, bt=bt)
+        q = queries(inst, H)
+        want = run(inst, q, 0.1, window=50)[0]
+        for b in range(len(n)):
+            p = inst.prog[b]
+            first = max(0, length[b] - n[b] + 1 - 50)
+            inst.tbl[inst.tbl_off[p]:inst.tbl_off[p] + first // bt] = R.NONE
+            inst.tbl[inst.tbl_off[p] - (-length[b] // bt):inst.tbl_off[p + 1]] = R.NONE
+        assert np.array_equal(run(inst, q, 0.1, window=50)[0], want)
+        with pytest.raises(MoriError) as e:
+            run(inst, q, 0.1, window=2000)
+        assert e.value.detail == M.MORI_DEV_NOT_RESIDENT
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("form", ["step", "few", "tile", "tile_odd_pages", "prompt"])
+def test_what_a_row_does_not_see_does_not_reach_it(form, bad):
+    """Values and keys that are not finite, seen by some rows, by none, or by all."""
+    n, length, kv, H, dim, bt = FORMS[form]
+    for where, kw in (("before", dict(window=20)), ("after", dict(end=None)), ("between", dict(first=None))):
+        inst = R.instance(81, n, length, kv=kv, dim=dim, bt=bt)
+        q = queries(inst, H)
+        pos = positions(inst)
+        if where == "after":  # every token stops short of its own position by a few
+            kw = dict(end=(pos - 2).astype(np.int32))
+        if where == "between":
+            kw = dict(first=documents(inst, 17))
+        b = int(np.argmax(inst.length))
+        L = int(inst.length[b])
+        at = {"before": max(0, L - 21 - n[b] // 2), "after": L - 1, "between": L - n[b] // 2 - 1}[where]
+        page, row = inst.slot(b, at)
+        for plane in (0, 1):
+            inst.pool[inst.layer, plane, page, row, :, 3 + plane] = bad
+        out, _ = run(inst, q, 0.1, **kw)
+        t0, m = int(inst.seq_off[b]), n[b]
+        seen = np.zeros(q.shape[0], bool)
+        for i in range(m):
+            p = L - m + i
+            lo = max(0, p + 1 - 20) if where == "before" else int(kw["first"][t0 + i]) if where == "between" else 0
+            hi = int(kw["end"][t0 + i]) if where == "after" else p + 1
+            seen[t0 + i] = lo <= at < hi
+        assert not seen.all()
+        page, row = inst.slot(b, at)
+        for plane in (0, 1):
+            inst.pool[inst.layer, plane, page, row, :, 3 + plane] = 0
+        want, _, bound, _ = S.attend(inst, q, 0.1, **kw)
+        assert (np.abs(out - want) <= bound)[~seen].all(), (where, np.argwhere(~(np.abs(out - want) <= bound)[~seen])[:4])
+
+
+def test_capped_infinities():
+    """Infinite scores are the cap: what a key of 1000 gives (its score is 100, and tanh 20
+    is 1 in 32 bits), with the same weights everywhere."""
+    out = []
+    for value in (float("inf"), 1000.0):
+        inst = R.instance(82, [1, 30], [40, 60], kv=1, dim=64)
+        q = queries(inst, 8)
+        q[..., 5] = torch.where(q[..., 5] < 0, -1.0, 1.0).to(BF16)
+        for b, at in ((0, 7), (1, 10)):
+            page, row = inst.slot(b, at)
+            inst.pool[1, 0, page, row, 0, :] = 0
+            inst.pool[1, 0, page, row, 0, 5] = value
+        out.append(run(inst, q, 0.1, cap=5.0)[0])
+    assert np.array_equal(*out)
+    want, _, bound, _ = S.attend(inst, q, 0.1, cap=5.0)
+    assert (np.abs(out[0] - want) <= bound).all()
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.1, 1.0])
+def test_scales(scale):
+    inst = R.instance(83, [1, 40], [300, 90], kv=2, dim=64)
+    q = queries(inst, 4, 1.0)
+    for kw in (dict(cap=3.0), dict(slopes=np.array([0.5, -0.01, 0.0, 1e-8], np.float32)), dict(window=30)):
+        compare(inst, q, scale, **kw)
+
+
+@pytest.mark.parametrize("form", ["step_long", "tile", "few"])
+def test_repeats_and_workspaces(form):
+    """The same bits every time, with a workspace given for any sight, dirty from others."""
+    n, length, kv, H, dim, bt = FORMS[form]
+    inst = R.instance(84, n, length, kv=kv, dim=dim, bt=bt)
+    q, pool, b = queries(inst, H).cuda(), inst.pool.cuda(), R.batch(inst)
+    ws = A.kv_attend_workspace(inst.geom, b, q, sight=True)
+    ws.fill_(255)
+    first = dev(documents(inst, 100))
+    calls = [dict(cap=9.0), dict(window=64), dict(first=first), dict(slopes=dev(slopes_of(H)))]
+    one = [A.kv_attend(pool, inst.geom, 1, b, q, scale=0.1, **kw) for kw in calls]
+    for _ in range(3):
+        for kw, want in zip(calls, one):
+            assert torch.equal(A.kv_attend(pool, inst.geom, 1, b, q, scale=0.1, workspace=ws, **kw), want)
+    b.check()
+
+
+def test_graph_replays():
+    """Ranges, lengths and slopes are read at replay."""
+    inst = R.instance(85, [1, 20, 5], [200, 300, 50], kv=2, dim=64)
+    q, pool, b = queries(inst, 8).cuda(), inst.pool.cuda(), R.batch(inst)
+    ws = A.kv_attend_workspace(inst.geom, b, q, sight=True)
+    first, slopes = torch.zeros(26, dtype=torch.int32, device="cuda"), torch.zeros(8, device="cuda")
+    out = torch.empty_like(q)
+    call = lambda o, w: A.kv_attend(pool, inst.geom, 1, b, q, scale=0.1, out=o, workspace=w, first=first, slopes=slopes, cap=8.0)
+    call(out, ws)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out, ws)
+    other = torch.empty_like(ws)
+    for i in range(5):
+        first.copy_(dev(documents(inst, 20 + 10 * i, seed=i)))
+        slopes.copy_(dev(slopes_of(8) * i))
+        graph.replay()
+        want = torch.empty_like(q)
+        call(want, other)
+        torch.randn(10000, device="cuda").sum().item()
+        assert torch.equal(out, want)
+    b.check()
+
+
+def test_strided_queries_and_outputs():
+    inst = R.instance(86, [30, 1], [80, 200], kv=2, dim=64)
+    big = torch.randn(31, 12, 64).to(BF16)
+    o = torch.zeros(31, 8, 192, dtype=BF16, device="cuda")
+    b = R.batch(inst)
+    x = big.cuda()
+    A.kv_attend(inst.pool.cuda(), inst.geom, 1, b, x[:, 2:10], scale=0.2, out=o[:, :, 64:128], window=25)
+    want, _, bound, _ = S.attend(inst, big[:, 2:10], 0.2, window=25)
+    assert (np.abs(o[:, :, 64:128].double().cpu().numpy() - want) <= bound).all()
+    assert (o[:, :, :64] == 0).all() and (o[:, :, 128:] == 0).all()
+    b.check()
+
+
+def test_rows_behind_the_last_sequence():
+    """More tokens than the sequences have: those rows are left as they were."""
+    inst = R.instance(87, [40, 1], [80, 200], kv=2, dim=64)
+    for n in ([40, 1], [1, 1]):
+        inst.n = np.array(n)
+        inst.seq_off = np.concatenate([[0], np.cumsum(n)])
+        T = sum(n) + 6
+        b = R.batch(inst, tokens=T)
+        q = torch.randn(T, 4, 64, device="cuda").bfloat16()
+        o = torch.full((T, 4, 64), 7.0, device="cuda", dtype=BF16)
+        A.kv_attend(inst.pool.cuda(), inst.geom, 1, b, q, scale=0.2, out=o, cap=4.0, window=30)
+        b.check()
+        assert (o[-6:] == 7).all() and torch.isfinite(o).all()
+
+
+def test_bad_batches():
+    """Lengths past the bounds: the bit, zeros, and nothing read out of range."""
+    inst = R.instance(88, [6, 3], [80, 200], kv=2, dim=64)
+    inst.length[0] = 10 ** 6
+    q = queries(inst, 4)
+    for kw in (dict(window=10), dict(first=np.zeros(9, np.int32)), dict(end=np.full(9, 1 << 30, np.int32))):
+        b = R.batch(inst, max_kv=300)
+        k = {n: dev(x) if isinstance(x, np.ndarray) else x for n, x in kw.items()}
+        out = A.kv_attend(inst.pool.cuda(), inst.geom, 1, b, q.cuda(), scale=0.2, **k)
+        with pytest.raises(MoriError) as e:
+            b.check()
+        assert e.value.detail == M.MORI_DEV_BAD_TOKENS
+        assert (out[:6] == 0).all() and torch.isfinite(out).all() and (out[6:] != 0).any()
