@@ -27,7 +27,7 @@ __global__ __launch_bounds__(64 * NW) void attend_join_kernel(Args a, uint32_t s
   const uint32_t t = blockIdx.x / per_token, h0 = (blockIdx.x - t * per_token) * heads_wg + (WPH > 1 ? 0 : wv * some);
   Item it;
   bool lines = false;  // tiles are written down, with runs of their own
-  if constexpr (SIGHT) lines = a.span != nullptr;
+  if constexpr (SIGHT) lines = a.tile != nullptr;
   if (lines) it.b = find_sequence(a.b, t, lane);
   else it = find_item(a, lane, [&](uint32_t, uint32_t n, uint32_t b) {
     return n && a.b.seq_off[b] <= t && t < a.b.seq_off[b + 1];
@@ -41,24 +41,19 @@ __global__ __launch_bounds__(64 * NW) void attend_join_kernel(Args a, uint32_t s
   else none = s.position(t - s.t0) < 0;
   const uint32_t tiles = (n * a.group + a.tile_rows - 1) / a.tile_rows;
   const uint64_t step = (uint64_t)a.kv_heads * a.tile_rows;
-  uint32_t known = 0xFFFFFFFFu;  // the tile whose runs are known
   for (uint32_t h = h0; h < min(h0 + some, a.heads); ++h) {
     const uint32_t kv = divide(h, a.by_group), x = (t - t0) * a.group + (h - kv * a.group);
     const uint32_t tile = x / a.tile_rows;
-    uint64_t item = it.first;
+    uint64_t item = it.first + (uint64_t)(tiles - 1 - tile) * it.per_tile;
     if constexpr (SIGHT) {
       if (lines) {
-        if (tile != known) {
-          known = tile;
-          const TileRun r = find_tile(a, lane, 0, same(a.seq_tile[it.b]) + (tiles - 1 - tile), false);
-          it.first = r.first;
-          it.per_tile = r.found ? r.per_tile : 0;
-        }
+        const uint32_t i = same(a.seq_tile[it.b]) + (tiles - 1 - tile);
+        if (i >= a.tiles) continue;
+        item = same(a.tile[i].first);
+        it.per_tile = same(a.tile[i].runs);
         if (it.per_tile < 2) continue;
-        item = it.first;
       }
     }
-    if (!lines) item = it.first + (uint64_t)(tiles - 1 - tile) * it.per_tile;
     const uint32_t runs = it.per_tile;
     const uint32_t r0 = WPH > 1 ? (uint32_t)((uint64_t)runs * wv / NW) : 0;
     const uint32_t r1 = WPH > 1 ? (uint32_t)((uint64_t)runs * (wv + 1) / NW) : runs;
@@ -157,8 +152,10 @@ void launch_attend_join(const AttendArgs& a, bool f16, uint32_t value, hipStream
   else launch<BF16>(a, value, s);
 }
 void launch_attend_join(const SightArgs& a, bool f16, uint32_t value, hipStream_t s) {
-  if (f16) launch<F16>(a, value, s);
-  else launch<BF16>(a, value, s);
+  Sight<UNKNOWN> x;
+  static_cast<SightArgs&>(x) = a;
+  if (f16) launch<F16>(x, value, s);
+  else launch<BF16>(x, value, s);
 }
 
 }  // namespace mori

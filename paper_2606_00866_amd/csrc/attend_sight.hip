@@ -1,39 +1,190 @@
-// Writes down the tiles of a batch: which keys each one's rows see together and which all
-// of them see.  A wavefront a tile; a tile's tokens (128 rows at most) are two reads a
-// lane.  Without splits a tile is an item; with them the attention's wavefronts and the
-// join's scan these lines for theirs.
+// Writes down the tiles of a batch whose sequences have several, and their items.
+//
+// Without splits a tile is an item: a wavefront a tile, whose tokens (128 rows at most)
+// are two reads a lane; 5 us for 650 tiles.  With splits there are fewer than 2048 tiles,
+// and one workgroup does it all: it checks the sequences, takes the tiles' keys, chooses
+// the length of the runs and lists the items in order.
+//
+// The length of the runs.  An item's time is its steps and a fixed part of about three;
+// 512 of them run at a time (two workgroups a CU), 256 of them in two thirds of the time;
+// splitting at all costs the second kernel, about two steps, and every 88 items of split
+// tiles one step to write and join 64 KiB of partial sums each.  32 lengths from the
+// shortest allowed to 15 times that are tried, two a wavefront, and the one with the
+// least time is taken.
 #include "sight.h"
 
 namespace mori {
 namespace {
 
+// The keys of a tile that starts at row0.
+__device__ inline Union tile_union(const SightArgs& a, const Seq& s, uint32_t row0, uint32_t rows, uint32_t lane) {
+  if (s.error) return Union{0, 0, 0xFFFFFFFFu, 0};
+  return union_of(a, s, divide(row0, a.by_group), divide(row0 + rows - 1, a.by_group) + 1, lane);
+}
+
+__device__ inline uint32_t units_of(const SightArgs& a, uint32_t lo, uint32_t hi) {
+  const uint32_t n = (hi - lo / a.align * a.align + a.unit - 1) / a.unit;
+  return n ? n : 1u;  // an empty tile is an item too: its rows are 0
+}
+
 __global__ __launch_bounds__(256) void sight_tiles_kernel(SightArgs a) {
   const uint32_t lane = threadIdx.x & 63, tile = blockIdx.x * 4 + wave_index();
   if (tile >= a.tiles) return;
-  AttendArgs whole = a;  // a tile is one run here
-  whole.splits = 0;
+  AttendArgs whole = a;
   const Item it = find_item(whole, lane, [&](uint32_t first, uint32_t n, uint32_t) { return tile - first < n; });
   if (tile == 0 && it.bad && lane == 0) report(a.b, MORI_DEV_BAD_TOKENS);
+  uint4* const to = reinterpret_cast<uint4*>(a.tile + tile);
   if (!it.found) {
-    if (lane == 0) a.span[tile] = uint2{1, 0};
+    if (lane == 0) to[2] = uint4{0, 0, 0, 0};
     return;
   }
   const SeqNumbers x = read_sequence(a.b, it.b);
   const Seq s = checked_sequence(a.b, SeqNumbers{same(x.lo), same(x.hi), same(x.len), same(x.p), same(x.first), same(x.last)});
   const uint32_t tiles = (s.n * a.group + a.tile_rows - 1) / a.tile_rows, back = tile - it.first;
   const uint32_t row0 = (tiles - 1 - back) * a.tile_rows, rows = min(a.tile_rows, s.n * a.group - row0);
-  Union u{0, 0, 0, 0};
-  if (!s.error) u = union_of(a, s, divide(row0, a.by_group), divide(row0 + rows - 1, a.by_group) + 1, lane);
+  const Union u = tile_union(a, s, row0, rows, lane);
   if (lane) return;
-  a.span[tile] = uint2{u.lo, u.hi};
-  a.tile[tile] = uint4{u.from, u.open, it.b, row0};
-  if (back == 0) a.seq_tile[it.b] = it.first;
+  report(a.b, s.error);
+  to[0] = uint4{u.lo, u.hi, u.from, u.open};
+  to[1] = uint4{s.t0, s.n, s.len, s.tbl};
+  to[2] = uint4{row0, tile, 1, 0x7FFFFFFFu};
+}
+
+constexpr uint32_t NT = 1024, WAVES = NT / 64, MOST = 2048, K = MOST / NT;
+
+__device__ inline uint32_t scan_before(uint32_t v, uint32_t* s_wave, uint32_t* total) {
+  const uint32_t lane = threadIdx.x & 63, wv = threadIdx.x >> 6, in = wave::incl_add(v);
+  if (lane == 63) s_wave[wv] = in;
+  __syncthreads();
+  uint32_t before = in - v, all = 0;
+#pragma unroll
+  for (uint32_t i = 0; i < WAVES; ++i) {
+    const uint32_t x = s_wave[i];
+    before += i < wv ? x : 0;
+    all += x;
+  }
+  *total = all;
+  __syncthreads();
+  return before;
+}
+
+__global__ __launch_bounds__(NT) void sight_items_kernel(SightArgs a) {
+  __shared__ uint4 s_seq[MOST];                    // t0, n, len, tbl
+  __shared__ uint32_t s_tile0[MOST], s_units[MOST], s_row0[MOST];
+  __shared__ uint32_t s_wave[WAVES], s_run[WAVES];
+  __shared__ float s_cost[WAVES];
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wv = wave_index();
+  // sequences: there are fewer of them than tiles may be
+  uint32_t mine = 0, err = 0, have[K];
+#pragma unroll
+  for (uint32_t k = 0; k < K; ++k) {
+    const uint32_t b = K * tid + k;
+    have[k] = 0;
+    if (b >= a.b.B) continue;
+    const Seq s = checked_sequence(a.b, read_sequence(a.b, b));
+    err |= s.error;
+    s_seq[b] = uint4{s.t0, s.n, s.len, s.tbl};  // len 0 where something is wrong: padding
+    have[k] = (s.n * a.group + a.tile_rows - 1) / a.tile_rows;
+    mine += have[k];
+  }
+  err = wave::all_or(err);
+  if (lane == 0) report(a.b, err);
+  uint32_t tiles;
+  uint32_t at = scan_before(mine, s_wave, &tiles);
+  tiles = min(tiles, a.tiles);  // more only where sequences overlap
+#pragma unroll
+  for (uint32_t k = 0; k < K; ++k) {
+    const uint32_t b = K * tid + k;
+    if (b < a.b.B) {
+      s_tile0[b] = at;
+      a.seq_tile[b] = at;
+    }
+    at += have[k];
+  }
+  __syncthreads();
+  // tiles, a wavefront each
+  for (uint32_t tile = wv; tile < tiles; tile += WAVES) {
+    uint32_t lo = 0, hi = a.b.B - 1;  // the last sequence whose first tile is not behind this one
+    while (lo < hi) {
+      const uint32_t mid = (lo + hi + 1) / 2;
+      if (same(s_tile0[mid]) <= tile) lo = mid;
+      else hi = mid - 1;
+    }
+    const uint4 q = s_seq[lo];
+    Seq s{};
+    s.t0 = same(q.x);
+    s.n = same(q.y);
+    s.len = same(q.z);
+    const uint32_t of = (s.n * a.group + a.tile_rows - 1) / a.tile_rows;
+    const uint32_t row0 = (of - 1 - (tile - same(s_tile0[lo]))) * a.tile_rows;
+    const Union u = tile_union(a, s, row0, min(a.tile_rows, s.n * a.group - row0), lane);
+    if (lane == 0) {
+      uint4* const to = reinterpret_cast<uint4*>(a.tile + tile);
+      to[0] = uint4{u.lo, u.hi, u.from, u.open};
+      to[1] = q;
+      s_units[tile] = units_of(a, u.lo, u.hi);
+      s_row0[tile] = row0;
+    }
+  }
+  __syncthreads();
+  // the length of the runs
+  uint32_t units[K], total;
+#pragma unroll
+  for (uint32_t k = 0; k < K; ++k) {
+    const uint32_t t = K * tid + k;
+    units[k] = t < tiles ? s_units[t] : 0;
+  }
+  scan_before(units[0] + units[1], s_wave, &total);
+  const uint32_t least = max(a.least, (total + a.slots - 1) / a.slots);
+  float best = 3.0e38f;
+  uint32_t run = least;
+  for (uint32_t j = 2 * wv; j < 2 * wv + 2; ++j) {
+    const uint32_t c = (uint32_t)((float)least * __builtin_amdgcn_exp2f(0.125f * (float)j) + 0.999f);
+    uint32_t n = 0;
+    for (uint32_t t = lane; t < tiles; t += 64) n += (s_units[t] + c - 1) / c;
+    n = wave::sum(n);
+    const uint32_t groups = n * a.kv_heads, rest = groups % 512;
+    const float rounds = (float)(groups / 512) + (rest == 0 ? 0.f : rest <= 256 ? 0.65f : 1.f);
+    const float cost = rounds * (float)(c + 3) + (n > tiles ? 2.f + (float)groups / 88.f : 0.f);
+    if (cost < best) {
+      best = cost;
+      run = c;
+    }
+  }
+  if (lane == 0) {
+    s_cost[wv] = best;
+    s_run[wv] = run;
+  }
+  __syncthreads();
+  best = s_cost[0];
+  run = s_run[0];
+  for (uint32_t i = 1; i < WAVES; ++i)
+    if (s_cost[i] < best) {
+      best = s_cost[i];
+      run = s_run[i];
+    }
+  // items
+  uint32_t runs[K], items;
+#pragma unroll
+  for (uint32_t k = 0; k < K; ++k) runs[k] = (units[k] + run - 1) / run;
+  at = scan_before(runs[0] + runs[1], s_wave, &items);
+#pragma unroll
+  for (uint32_t k = 0; k < K; ++k) {
+    const uint32_t t = K * tid + k;
+    if (t < tiles) {
+      reinterpret_cast<uint4*>(a.tile + t)[2] = uint4{s_row0[t], at, runs[k], run};
+      for (uint32_t i = at; i < min(at + runs[k], a.items); ++i) a.list[i] = t;
+    }
+    at += runs[k];
+  }
+  for (uint32_t i = items + tid; i < a.items; i += NT) a.list[i] = NO_TILE;
 }
 
 }  // namespace
 
 void launch_sight_tiles(const SightArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(sight_tiles_kernel, dim3((a.tiles + 3) / 4), dim3(256), 0, s, a);
+  if (a.splits) hipLaunchKernelGGL(sight_items_kernel, dim3(1), dim3(NT), 0, s, a);
+  else hipLaunchKernelGGL(sight_tiles_kernel, dim3((a.tiles + 3) / 4), dim3(256), 0, s, a);
 }
 
 }  // namespace mori

@@ -35,6 +35,7 @@ constexpr uint32_t NW = 4, STEP = 32;
 template <typename DT, int D, int NB, typename Args>
 __global__ __launch_bounds__(64 * NW) void attend_step_kernel(Args a) {
   constexpr bool SIGHT = IsSight<Args>::value;
+  constexpr int FORM = IsSight<Args>::FORM;
   constexpr int KS = D / 32;       // matrix steps over the head's elements
   constexpr int E = D / 16;        // value elements of a lane: 4 or 8
   constexpr int VW = E / 2;        // their 32-bit words
@@ -139,7 +140,7 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(Args a) {
           float y[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) y[i] = s[nb][i / 4][i % 4];
-          shape_scores(a, y, slope[nb], (int32_t)(k0 + 4 * g) - pos[nb], [](int i) { return 16 * (i / 4) + i % 4; });
+          shape_scores<FORM>(a, y, ref_of(top[nb]), slope[nb], (int32_t)(k0 + 4 * g) - pos[nb], [](int i) { return 16 * (i / 4) + i % 4; });
 #pragma unroll
           for (int i = 0; i < 8; ++i) s[nb][i / 4][i % 4] = y[i];
         }
@@ -155,9 +156,15 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(Args a) {
         float m = s[nb][0][0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) m = fmaxf(m, s[nb][i / 4][i % 4]);
-        m = (SIGHT ? 1.f : a.c) * max_over_16(max_over_32(m));
+        if constexpr (SIGHT) m = max_over_16(max_over_32(m)) + ref_of(top[nb]);
+        else m = a.c * max_over_16(max_over_32(m));
         if (__any(risen<DT>(m, top[nb]))) {
           const float t = follow<DT>(m, top[nb]), keep = __builtin_amdgcn_exp2f(top[nb] - t);
+          if constexpr (SIGHT) {
+            const float further = ref_of(t) - ref_of(top[nb]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[nb][i / 4][i % 4] -= further;
+          }
           top[nb] = t;
           sum[nb] *= keep;
 #pragma unroll
@@ -166,7 +173,7 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(Args a) {
         float f[8], part = 0;  // of this step: one by one, small weights would be lost in a large sum
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          f[i] = __builtin_amdgcn_exp2f(SIGHT ? s[nb][i / 4][i % 4] - top[nb]
+          f[i] = __builtin_amdgcn_exp2f(SIGHT ? s[nb][i / 4][i % 4]
                                               : __builtin_fmaf(s[nb][i / 4][i % 4], a.c, -top[nb]));
           part += f[i];
         }
@@ -285,6 +292,10 @@ void launch(const Args& a, bool f16, uint32_t dim, hipStream_t s) {
 }  // namespace
 
 void launch_attend_step(const AttendArgs& a, bool f16, uint32_t dim, hipStream_t s) { launch(a, f16, dim, s); }
-void launch_attend_step(const SightArgs& a, bool f16, uint32_t dim, hipStream_t s) { launch(a, f16, dim, s); }
+void launch_attend_step(const SightArgs& a, bool f16, uint32_t dim, hipStream_t s) {
+  Sight<UNKNOWN> x;  // bound by bytes: one kernel for every form
+  static_cast<SightArgs&>(x) = a;
+  launch(x, f16, dim, s);
+}
 
 }  // namespace mori

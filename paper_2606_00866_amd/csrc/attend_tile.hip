@@ -121,6 +121,8 @@ __device__ __forceinline__ void step(const Args& a, const Work& w, Tile<D, PAGED
                                      uint32_t tid, uint32_t wv) {
   typedef Tile<D, PAGED> T;
   constexpr bool SIGHT = IsSight<Args>::value;
+  constexpr int FORM = IsSight<Args>::FORM;
+  constexpr bool SHAPED = FORM != 0;  // scores are more than products with the scale
   constexpr uint32_t NT = T::NT, ROW = T::ROW, LD = T::LD;
   constexpr int KS = T::KS, DB = T::DB;
   const uint32_t lane = tid & 63, n = lane & 31, h = lane >> 5;
@@ -155,11 +157,11 @@ __device__ __forceinline__ void step(const Args& a, const Work& w, Tile<D, PAGED
       if (k % T::BETWEEN == 0) x.fetch(a, w, next, then_k, then_v, tid, wv, k / T::BETWEEN);
     }
     uint32_t p[16];
-    if constexpr (SIGHT) {
+    if constexpr (SHAPED) {
       float y[32];
 #pragma unroll
       for (int i = 0; i < 32; ++i) y[i] = s[i / 16][i % 16];
-      shape_scores(a, y, x.slope, (int32_t)(k0 + 4 * h) - x.pos,
+      shape_scores<FORM>(a, y, ref_of(x.top), x.slope, (int32_t)(k0 + 4 * h) - x.pos,
                    [](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4; });
 #pragma unroll
       for (int i = 0; i < 32; ++i) s[i / 16][i % 16] = y[i];
@@ -176,9 +178,15 @@ __device__ __forceinline__ void step(const Args& a, const Work& w, Tile<D, PAGED
     float m = s[0][0];
 #pragma unroll
     for (int i = 1; i < 32; ++i) m = fmaxf(m, s[i / 16][i % 16]);
-    m = (SIGHT ? 1.f : a.c) * max_over_32(m);
+    if constexpr (SHAPED) m = max_over_32(m) + ref_of(x.top);
+    else m = a.c * max_over_32(m);
     if (__any(risen<DT>(m, x.top))) {
       const float t = follow<DT>(m, x.top), keep = __builtin_amdgcn_exp2f(x.top - t);
+      if constexpr (SHAPED) {
+        const float further = ref_of(t) - ref_of(x.top);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) s[i / 16][i % 16] -= further;
+      }
       x.top = t;
       x.sum *= keep;
 #pragma unroll
@@ -188,8 +196,8 @@ __device__ __forceinline__ void step(const Args& a, const Work& w, Tile<D, PAGED
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const float y0 = s[i / 8][2 * i % 16], y1 = s[i / 8][2 * i % 16 + 1];
-      const float f0 = __builtin_amdgcn_exp2f(SIGHT ? y0 - x.top : __builtin_fmaf(y0, a.c, -x.top));
-      const float f1 = __builtin_amdgcn_exp2f(SIGHT ? y1 - x.top : __builtin_fmaf(y1, a.c, -x.top));
+      const float f0 = __builtin_amdgcn_exp2f(SHAPED ? y0 : __builtin_fmaf(y0, a.c, -x.top));
+      const float f1 = __builtin_amdgcn_exp2f(SHAPED ? y1 : __builtin_fmaf(y1, a.c, -x.top));
       part += f0 + f1;
       p[i] = pair_of<DT>(f0, f1);
     }
@@ -223,7 +231,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tile_kernel(Args a) {
   const uint32_t tid = threadIdx.x, lane = tid & 63, wv = wave_index();
   const uint32_t n = lane & 31, h = lane >> 5;
   Work w;
-  if constexpr (SIGHT) w = tile_work(a, blockIdx.x, lane);
+  if constexpr (SIGHT) w = tile_work(a, blockIdx.x);
   else w = work_of(a, blockIdx.x, lane);
   if (!w.some) return;
   T x;
@@ -334,6 +342,8 @@ void launch(const Args& a, bool f16, uint32_t dim, hipStream_t s) {
 }  // namespace
 
 void launch_attend_tile(const AttendArgs& a, bool f16, uint32_t dim, hipStream_t s) { launch(a, f16, dim, s); }
-void launch_attend_tile(const SightArgs& a, bool f16, uint32_t dim, hipStream_t s) { launch(a, f16, dim, s); }
+void launch_attend_tile(const SightArgs& a, bool f16, uint32_t dim, hipStream_t s) {
+  with_form(a, [&](const auto& x) { launch(x, f16, dim, s); });
+}
 
 }  // namespace mori

@@ -19,7 +19,7 @@ struct Plan {
   SightArgs a;
   uint32_t dim, value;
   bool f16, step, latent;
-  uint64_t ml_at, span_at, tile_at, seq_at, bytes;  // workspace
+  uint64_t ml_at, tile_at, list_at, seq_at, bytes;  // workspace
 };
 
 // Host check of what the call and its workspace size take, and the schedule.
@@ -73,6 +73,10 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
       a.cap = sight->cap * 1.4426950408889634f;
       a.cap_in = at->scale == 0 ? 1.f : std::fabs(at->scale) / sight->cap;
       if (!std::isfinite(a.cap) || !std::isfinite(a.cap_in) || a.cap == 0) return false;
+      constexpr double P[6] = {0.9999994039535522,    -0.3332904279232025, 0.13281433284282684,
+                               -0.051605675369501114, 0.016743116080760956, -0.003067060373723507};
+      for (int k = 0; k < 6; ++k) a.p[k] = (float)(P[k] * a.cap);
+      a.exact = sight->cap > 64;
     }
     a.slopes = sight->slopes;
     a.window = sight->window;
@@ -104,11 +108,11 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
   a.items = (uint32_t)items;
   const uint64_t n = a.splits ? items * a.kv_heads * a.tile_rows : 0;
   p.ml_at = n * p.value * sizeof(float);
-  p.span_at = p.bytes = p.ml_at + n * sizeof(float2);
+  p.bytes = p.ml_at + n * sizeof(float2);
   if (sight && !p.step) {
-    p.span_at = (p.span_at + 15) / 16 * 16;
-    p.tile_at = p.span_at + (tiles + 1) / 2 * 16;
-    p.seq_at = p.tile_at + tiles * sizeof(uint4);
+    p.tile_at = (p.bytes + 15) / 16 * 16;
+    p.list_at = p.tile_at + tiles * sizeof(SightTile);
+    p.seq_at = p.list_at + (a.splits ? items * sizeof(uint32_t) : 0);
     p.bytes = p.seq_at + (uint64_t)a.b.B * sizeof(uint32_t);
     a.tiles = (uint32_t)tiles;
   }
@@ -146,8 +150,8 @@ int attend_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, 
   };
   if (sight) {
     if (!p.step) {
-      a.span = reinterpret_cast<uint2*>(ws + p.span_at);
-      a.tile = reinterpret_cast<uint4*>(ws + p.tile_at);
+      a.tile = reinterpret_cast<SightTile*>(ws + p.tile_at);
+      a.list = reinterpret_cast<uint32_t*>(ws + p.list_at);
       a.seq_tile = reinterpret_cast<uint32_t*>(ws + p.seq_at);
       launch_sight_tiles(a, s);
     }

@@ -13,14 +13,18 @@
 // Items.  As in attend.h, but a tile's keys are those its rows see, so a window over a
 // long context gives as many items as the window has work for.  Batches whose sequences
 // are one tile each (decode steps) find that from the lengths and ranges themselves;
-// the others have the tiles' ranges written down by a small kernel first, since every
-// workgroup would read all tokens' ranges otherwise.
+// the others have their tiles and items written down by a small kernel first
+// (attend_sight.hip), since every workgroup would read all tokens' ranges otherwise.
 //
 // tanh.  With all scores of a step and wavefront below the cap, tanh x is x P(x^2), P of
 // six terms with a relative error of 7e-7 (a minimax fit on [0, 1]); else 1 - 2 / (e^2x
-// + 1) where |x| >= 1.  The polynomial costs seven full-rate instructions, the other form
-// two at a quarter of the rate and three more; small scores keep their relative accuracy
-// whatever the cap.
+// + 1).  The polynomial costs seven full-rate instructions, the other form two at a
+// quarter of the rate and three more.  The latter's error is 2^-22 of the cap, which for
+// caps up to 64 is 2^-16 of a score's unit; above that small scores keep to the polynomial.
+//
+// Reference.  Scores are taken relative to where the maximum was last followed in the
+// instruction that finishes them, so neither caps nor biases cost another one for it; a
+// row that has seen nothing yet has the reference 0.
 #pragma once
 #include "attend.h"
 
@@ -28,15 +32,33 @@ namespace mori {
 
 struct SightArgs : AttendArgs {
   float cap, cap_in;   // log2(e) * cap; |scale| / cap.  0: none
+  float p[6];          // cap * P's coefficients
+  uint32_t exact;      // the cap is above 64
   const float* slopes;
   uint32_t window;     // 0: none
   const int32_t *first, *end;
   // tiles as written down (no array: a sequence is a tile)
   uint32_t tiles;      // bound on their number
   uint32_t align;      // a tile's keys are taken from a multiple of this on
-  uint2* span;         // [tiles] keys lo .. hi - 1 of its rows; lo > hi: no tile
-  uint4* tile;         // [tiles] from, open, sequence, first row
+  struct SightTile* tile;  // [tiles]
+  uint32_t* list;      // [items] an item's tile; without splits it is the item itself
   uint32_t* seq_tile;  // [B] a sequence's first one
+};
+constexpr uint32_t NO_TILE = 0xFFFFFFFFu;
+
+// What a kernel knows of a sight when it is compiled.
+constexpr int CAPPED = 1, BIASED = 2, UNKNOWN = 4;
+template <int F>
+struct Sight : SightArgs {
+  static constexpr int FORM = F;
+};
+
+// A tile of rows, 48 bytes.
+struct SightTile {
+  uint32_t lo, hi, from, open;    // keys that its rows see together, and all of them
+  uint32_t t0, n, len, tbl;       // of its sequence (Seq)
+  uint32_t row0, first, runs;     // its first row, its first item and their number (0: no tile)
+  uint32_t run_units;
 };
 
 // Keys of token i of a sequence.
@@ -143,109 +165,77 @@ __device__ inline Work work_of(const SightArgs& a, uint32_t block, uint32_t lane
   return w;
 }
 
-// A tile and its run among those written down.
-struct TileRun {
-  uint32_t tile, first, per_tile, run_units;  // first: its first item
-  bool found;
-};
-// `tile` for its items, or else the tile of `item`; the same for the whole wavefront.
-__device__ inline TileRun find_tile(const SightArgs& a, uint32_t lane, uint32_t item, uint32_t tile, bool by_item) {
-  const uint32_t k = (a.tiles + 63) / 64, t0 = lane * k;
-  const auto units = [&](uint32_t t) {
-    const uint2 s = a.span[t];
-    const uint32_t n = (s.y - s.x / a.align * a.align + a.unit - 1) / a.unit;
-    return s.x > s.y ? 0u : n ? n : 1u;  // an empty tile is an item too: its rows are 0
-  };
-  uint64_t total = 0;
-  for (uint32_t t = t0; t < min(t0 + k, a.tiles); ++t) total += units(t);
-  total = wave::sum(total);
-  TileRun r{};
-  r.run_units = (uint32_t)max((uint64_t)a.least, (total + a.slots - 1) / a.slots);
-  uint32_t mine = 0;
-  for (uint32_t t = t0; t < min(t0 + k, a.tiles); ++t) mine += (units(t) + r.run_units - 1) / r.run_units;
-  uint32_t first = wave::incl_add(mine) - mine, hit = 0xFFFFFFFFu, hit_first = 0, hit_per = 1;
-  for (uint32_t t = t0; t < min(t0 + k, a.tiles); ++t) {
-    const uint32_t n = (units(t) + r.run_units - 1) / r.run_units;
-    if (by_item ? item - first < n : t == tile && n) {
-      hit = t;
-      hit_first = first;
-      hit_per = n;
-    }
-    first += n;
-  }
-  const uint64_t who = __ballot(hit != 0xFFFFFFFFu);
-  r.found = who != 0;
-  if (!r.found) return r;
-  const int l = __ffsll((unsigned long long)who) - 1;
-  r.tile = (uint32_t)__builtin_amdgcn_readlane((int)hit, l);
-  r.first = (uint32_t)__builtin_amdgcn_readlane((int)hit_first, l);
-  r.per_tile = (uint32_t)__builtin_amdgcn_readlane((int)hit_per, l);
-  return r;
-}
-
 // The item of a batch whose tiles are written down.
-__device__ inline Work tile_work(const SightArgs& a, uint32_t block, uint32_t lane) {
+__device__ inline Work tile_work(const SightArgs& a, uint32_t block) {
   Work w{};
   w.item = divide(block, a.by_kv);
   w.kv = block - w.item * a.kv_heads;
-  TileRun r{w.item, w.item, 1, 0x7FFFFFFFu, w.item < a.tiles};
-  if (a.splits) r = find_tile(a, lane, w.item, 0, true);
-  if (!r.found) return w;
-  const uint2 span = a.span[r.tile];
-  if (same(span.x) > same(span.y)) return w;
-  const uint4 t = a.tile[r.tile];
+  const uint32_t tile = a.splits ? same(a.list[w.item]) : w.item;
+  if (tile >= a.tiles) return w;
+  const uint4* const at = reinterpret_cast<const uint4*>(a.tile + tile);
+  const uint4 x = at[0], y = at[1], z = at[2];
+  w.per_tile = same(z.z);
+  if (!w.per_tile) return w;
   w.some = true;
-  const SeqNumbers x = read_sequence(a.b, same(t.z));
-  w.s = checked_sequence(a.b, SeqNumbers{same(x.lo), same(x.hi), same(x.len), same(x.p), same(x.first), same(x.last)});
-  w.row0 = same(t.w);
+  w.s.t0 = same(y.x);
+  w.s.n = same(y.y);
+  w.s.len = same(y.z);
+  w.s.tbl = same(y.w);
+  w.s.named = true;
+  w.row0 = same(z.x);
   w.rows = min(a.tile_rows, w.s.n * a.group - w.row0);
-  w.per_tile = r.per_tile;
-  set_run(a, w, Union{same(span.x), same(span.y), same(t.x), same(t.y)}, w.item - r.first, r.run_units);
+  set_run(a, w, Union{same(x.x), same(x.y), same(x.z), same(x.w)}, w.item - same(z.y), same(z.w));
   return w;
 }
 
-// tanh, where all of a wavefront's arguments are below 1, and anywhere.
-__device__ inline float tanh_small(float x) {
+// cap * tanh(x) - ref, where all of a wavefront's arguments are below 1, and anywhere.
+__device__ inline float capped_small(const SightArgs& a, float x, float ref) {
   const float u = x * x;
-  float p = __builtin_fmaf(u, -0.003067060373723507f, 0.016743116080760956f);
-  p = __builtin_fmaf(u, p, -0.051605675369501114f);
-  p = __builtin_fmaf(u, p, 0.13281433284282684f);
-  p = __builtin_fmaf(u, p, -0.3332904279232025f);
-  return x * __builtin_fmaf(u, p, 0.9999994039535522f);
+  float p = __builtin_fmaf(u, a.p[5], a.p[4]);
+#pragma unroll
+  for (int k = 3; k >= 0; --k) p = __builtin_fmaf(u, p, a.p[k]);
+  return __builtin_fmaf(x, p, -ref);
 }
-__device__ inline float tanh_any(float x) {
-  const float big = 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * 2.8853900817779268f) + 1.f);
-  return fabsf(x) < 1.f ? tanh_small(x) : big;
+__device__ inline float capped_any(const SightArgs& a, float x, float ref) {
+  const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * 2.8853900817779268f) + 1.f);
+  return __builtin_fmaf(-2.f * a.cap, r, a.cap - ref);
 }
 
-// Scores of one row (or, lane by lane, of several) in the softmax's units from the
-// products of queries and keys; key(i) is what the i-th one's key is ahead of `base`.
-template <int N, typename K>
-__device__ __forceinline__ void shape_scores(const SightArgs& a, float (&y)[N], float slope, int32_t base, K key) {
-  if (a.cap != 0) {
+// Scores of one row (or, lane by lane, of several) in the softmax's units and less `ref`,
+// from the products of queries and keys; key(i) is what the i-th one's key is ahead of
+// `base`, which counts from the row's position.
+template <int FORM, int N, typename K>
+__device__ __forceinline__ void shape_scores(const SightArgs& a, float (&y)[N], float ref, float slope, int32_t base,
+                                             K key) {
+  if (FORM == UNKNOWN ? a.cap != 0 : FORM & CAPPED) {
     float big = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       y[i] *= a.cap_in;
       big = fmaxf(big, fabsf(y[i]));
     }
-    if (__any(big >= 1.f)) {
+    if (!__any(big >= 1.f)) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) y[i] = a.cap * tanh_any(y[i]);
+      for (int i = 0; i < N; ++i) y[i] = capped_small(a, y[i], ref);
+    } else if (!a.exact) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) y[i] = capped_any(a, y[i], ref);
     } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i) y[i] = a.cap * tanh_small(y[i]);
+      for (int i = 0; i < N; ++i) y[i] = fabsf(y[i]) < 1.f ? capped_small(a, y[i], ref) : capped_any(a, y[i], ref);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i) y[i] *= a.c;
+    for (int i = 0; i < N; ++i) y[i] = __builtin_fmaf(y[i], a.c, -ref);
   }
-  if (a.slopes) {
+  if (FORM == UNKNOWN ? a.slopes != nullptr : FORM & BIASED) {
     const float b = (float)base;
 #pragma unroll
     for (int i = 0; i < N; ++i) y[i] = __builtin_fmaf(-slope, fabsf(b + (float)key(i)), y[i]);
   }
 }
+// The reference of a row whose maximum was last followed at `top`.
+__device__ inline float ref_of(float top) { return top == NO_TOP ? 0.f : top; }
 // log2(e) * slope of a head.
 __device__ inline float slope_of(const SightArgs& a, uint32_t h) {
   return a.slopes ? 1.4426950408889634f * a.slopes[h] : 0.f;
@@ -253,7 +243,11 @@ __device__ inline float slope_of(const SightArgs& a, uint32_t h) {
 __device__ inline auto score_of(const SightArgs& a, const Work& w, uint32_t r, uint32_t h) {
   const int32_t pos = w.s.position(divide(w.row0 + r, a.by_group));
   return [&a, slope = slope_of(a, h), pos](float s, uint32_t key) {
-    float y = a.cap != 0 ? a.cap * tanh_any(s * a.cap_in) : s * a.c;
+    float y = s * a.c;
+    if (a.cap != 0) {
+      y = s * a.cap_in;
+      y = fabsf(y) < 1.f ? capped_small(a, y, 0.f) : capped_any(a, y, 0.f);
+    }
     if (a.slopes) y = __builtin_fmaf(-slope, fabsf((float)((int32_t)key - pos)), y);
     return y;
   };
@@ -262,10 +256,25 @@ __device__ inline auto score_of(const SightArgs& a, const Work& w, uint32_t r, u
 template <typename Args>
 struct IsSight {
   static constexpr bool value = false;
+  static constexpr int FORM = 0;
 };
-template <>
-struct IsSight<SightArgs> {
+template <int F>
+struct IsSight<Sight<F>> {
   static constexpr bool value = true;
+  static constexpr int FORM = F;
 };
+
+// The sight in the form that says what it does.
+template <typename L>
+inline void with_form(const SightArgs& a, L launch) {
+  const auto as = [&](auto form) {
+    static_cast<SightArgs&>(form) = a;
+    launch(form);
+  };
+  if (a.cap != 0 && a.slopes) as(Sight<CAPPED | BIASED>{});
+  else if (a.cap != 0) as(Sight<CAPPED>{});
+  else if (a.slopes) as(Sight<BIASED>{});
+  else as(Sight<0>{});
+}
 
 }  // namespace mori
