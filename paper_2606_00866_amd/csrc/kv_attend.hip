@@ -72,7 +72,8 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
     if (sight->cap > 0) {
       a.cap = sight->cap * 1.4426950408889634f;
       a.cap_in = at->scale == 0 ? 1.f : std::fabs(at->scale) / sight->cap;
-      if (!std::isfinite(a.cap) || !std::isfinite(a.cap_in) || a.cap == 0) return false;
+      if (!std::isfinite(a.cap) || !std::isfinite(4.f * a.cap_in) || a.cap == 0) return false;
+      a.cap_exp = 2.8853900817779268f * a.cap_in;
       constexpr double P[6] = {0.9999994039535522,    -0.3332904279232025, 0.13281433284282684,
                                -0.051605675369501114, 0.016743116080760956, -0.003067060373723507};
       for (int k = 0; k < 6; ++k) a.p[k] = (float)(P[k] * a.cap);

@@ -16,11 +16,12 @@
 // the others have their tiles and items written down by a small kernel first
 // (attend_sight.hip), since every workgroup would read all tokens' ranges otherwise.
 //
-// tanh.  With all scores of a step and wavefront below the cap, tanh x is x P(x^2), P of
-// six terms with a relative error of 7e-7 (a minimax fit on [0, 1]); else 1 - 2 / (e^2x
-// + 1).  The polynomial costs seven full-rate instructions, the other form two at a
-// quarter of the rate and three more.  The latter's error is 2^-22 of the cap, which for
-// caps up to 64 is 2^-16 of a score's unit; above that small scores keep to the polynomial.
+// tanh.  cap * tanh(x) = cap - 2 cap / (e^2x + 1): an exponential, a reciprocal and three
+// more instructions, with an error of 2^-22 of the cap.  For caps up to 64 that is 2^-16
+// of a score's unit.  Above, scores below the cap take x P(x^2) instead, P of six terms
+// with a relative error of 7e-7 (a minimax fit on [0, 1]), so they keep their relative
+// accuracy whatever the cap.  (The polynomial alone, where all of a step's scores are
+// small, is no faster: prompts of 20000 tokens 1656 us, 1592 with the other form.)
 //
 // Reference.  Scores are taken relative to where the maximum was last followed in the
 // instruction that finishes them, so neither caps nor biases cost another one for it; a
@@ -32,6 +33,7 @@ namespace mori {
 
 struct SightArgs : AttendArgs {
   float cap, cap_in;   // log2(e) * cap; |scale| / cap.  0: none
+  float cap_exp;       // 2 log2(e) * cap_in
   float p[6];          // cap * P's coefficients
   uint32_t exact;      // the cap is above 64
   const float* slopes;
@@ -188,17 +190,18 @@ __device__ inline Work tile_work(const SightArgs& a, uint32_t block) {
   return w;
 }
 
-// cap * tanh(x) - ref, where all of a wavefront's arguments are below 1, and anywhere.
-__device__ inline float capped_small(const SightArgs& a, float x, float ref) {
-  const float u = x * x;
+// cap * tanh(scale * s / cap) - ref from a product s, with an error of 2^-22 of the cap
+// and with one of 2^-20 of the score.
+__device__ inline float capped_any(const SightArgs& a, float s, float ref) {
+  const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s * a.cap_exp) + 1.f);
+  return __builtin_fmaf(-2.f * a.cap, r, a.cap - ref);
+}
+__device__ inline float capped_exact(const SightArgs& a, float s, float ref) {
+  const float x = s * a.cap_in, u = x * x;
   float p = __builtin_fmaf(u, a.p[5], a.p[4]);
 #pragma unroll
   for (int k = 3; k >= 0; --k) p = __builtin_fmaf(u, p, a.p[k]);
-  return __builtin_fmaf(x, p, -ref);
-}
-__device__ inline float capped_any(const SightArgs& a, float x, float ref) {
-  const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * 2.8853900817779268f) + 1.f);
-  return __builtin_fmaf(-2.f * a.cap, r, a.cap - ref);
+  return fabsf(x) < 1.f ? __builtin_fmaf(x, p, -ref) : capped_any(a, s, ref);
 }
 
 // Scores of one row (or, lane by lane, of several) in the softmax's units and less `ref`,
@@ -208,21 +211,12 @@ template <int FORM, int N, typename K>
 __device__ __forceinline__ void shape_scores(const SightArgs& a, float (&y)[N], float ref, float slope, int32_t base,
                                              K key) {
   if (FORM == UNKNOWN ? a.cap != 0 : FORM & CAPPED) {
-    float big = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      y[i] *= a.cap_in;
-      big = fmaxf(big, fabsf(y[i]));
-    }
-    if (!__any(big >= 1.f)) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) y[i] = capped_small(a, y[i], ref);
-    } else if (!a.exact) {
+    if (!a.exact) {
 #pragma unroll
       for (int i = 0; i < N; ++i) y[i] = capped_any(a, y[i], ref);
     } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i) y[i] = fabsf(y[i]) < 1.f ? capped_small(a, y[i], ref) : capped_any(a, y[i], ref);
+      for (int i = 0; i < N; ++i) y[i] = capped_exact(a, y[i], ref);
     }
   } else {
 #pragma unroll
@@ -245,8 +239,7 @@ __device__ inline auto score_of(const SightArgs& a, const Work& w, uint32_t r, u
   return [&a, slope = slope_of(a, h), pos](float s, uint32_t key) {
     float y = s * a.c;
     if (a.cap != 0) {
-      y = s * a.cap_in;
-      y = fabsf(y) < 1.f ? capped_small(a, y, 0.f) : capped_any(a, y, 0.f);
+      y = a.exact ? capped_exact(a, s, 0.f) : capped_any(a, s, 0.f);
     }
     if (a.slopes) y = __builtin_fmaf(-slope, fabsf((float)((int32_t)key - pos)), y);
     return y;

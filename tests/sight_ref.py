@@ -33,14 +33,15 @@ def attend(inst, q, scale, cap=None, slopes=None, window=None, first=None, end=N
             for h in range(H):
                 kk, vv = k[lo:hi, h // G], v[lo:hi, h // G]
                 s = kk @ q[t, h] * scale
-                # as in attend_ref; a cap does not stretch differences, its tanh is off by at most 2^-20 of the
-                # score (a polynomial's 7e-7 and six roundings, or three instructions' and four roundings' error
-                # next to 1) and the product with the cap by a rounding; a bias adds two roundings of itself and
-                # one of the sum
+                # as in attend_ref; a cap does not stretch differences.  Its tanh as 1 - 2 r, r = 1 / (e + 1): r is
+                # off by the exponential's and the reciprocal's 2^-23, the argument's rounding (2x 2^-24 of e) and
+                # the sum's, together below 2 r (1 - r) (2^-23 + x 2^-23) + 2 r 2^-23 + 2^-24 < 2^-22 of the cap;
+                # above a cap of 64 by 2^-20 of the score (a polynomial's 7e-7 and roundings, or the above next to
+                # a tanh of 0.76 at least).  A bias adds two roundings of itself and one of the sum
                 d = (D + 3) * 2.0 ** -23 * (np.abs(kk) @ np.abs(q[t, h])).max() * abs(scale)
                 if cap is not None:
                     s = cap * np.tanh(s / cap)
-                    d += 2.0 ** -20 * np.abs(s).max()
+                    d += 2.0 ** -20 * np.abs(s).max() + (cap * 2.0 ** -22 if cap <= 64 else 0)
                 if slopes is not None:
                     far = float(slopes[h]) * np.abs(pos - np.arange(lo, hi))
                     s = s - far
