@@ -31,6 +31,7 @@ namespace mori {
 namespace {
 
 constexpr uint32_t STEP = 64, NW = 4;
+constexpr int V_AHEAD = 4;  // values read ahead of their products
 // A wavefront's rows and its place in the loads.
 template <int D, bool PAGED>
 struct Tile {
@@ -146,6 +147,7 @@ __device__ __forceinline__ void step(const Args& a, const Work& w, Tile<D, PAGED
     f32x16 s[2];
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0;
+    __builtin_amdgcn_s_setprio(1);  // the products go first where both wavefronts of a SIMD could
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
 #pragma unroll
@@ -156,6 +158,18 @@ __device__ __forceinline__ void step(const Args& a, const Work& w, Tile<D, PAGED
       // the next step's loads, a few at a time: issued at once they hold the wavefront up
       if (k % T::BETWEEN == 0) x.fetch(a, w, next, then_k, then_v, tid, wv, k / T::BETWEEN);
     }
+    __builtin_amdgcn_s_setprio(0);
+    x.find(a, w, k0 + 2 * STEP, tid);  // behind the last use of what was found before, well ahead of the wait
+    // the first values on the way behind the weights
+    const auto value = [&](int i) {  // of 16 keys, 32 elements
+      const uint8_t* at = vs + 16 * (i / DB) * ROW + (((4 * (i % DB) + vc) ^ vx) << 4);
+      const u32x2 lo = read_tr(at), hi = read_tr(at + 8 * ROW);
+      return u32x4{lo[0], lo[1], hi[0], hi[1]};
+    };
+    u32x4 v[V_AHEAD];
+#pragma unroll
+    for (int i = 0; i < V_AHEAD; ++i) v[i] = value(i);
+    __builtin_amdgcn_sched_barrier(0);
     uint32_t p[16];
     if constexpr (SHAPED) {
       float y[32];
@@ -202,20 +216,21 @@ __device__ __forceinline__ void step(const Args& a, const Work& w, Tile<D, PAGED
       p[i] = pair_of<DT>(f0, f1);
     }
     x.sum += part;
+    __builtin_amdgcn_s_setprio(1);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-#pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        const uint8_t* at = vs + 16 * t * ROW + (((4 * d + vc) ^ vx) << 4);
-        const u32x2 lo = read_tr(at), hi = read_tr(at + 8 * ROW);
-        const u32x4 v = {lo[0], lo[1], hi[0], hi[1]};
-        x.o[d] = mfma_32x32x16(DT(), v, u32x4{p[4 * t], p[4 * t + 1], p[4 * t + 2], p[4 * t + 3]}, x.o[d]);
-      }
+    for (int i = 0; i < 4 * DB; ++i) {
+      const int t = i / DB, d = i % DB;
+      x.o[d] = mfma_32x32x16(DT(), v[i % V_AHEAD], u32x4{p[4 * t], p[4 * t + 1], p[4 * t + 2], p[4 * t + 3]}, x.o[d]);
+      if (i + V_AHEAD < 4 * DB) v[i % V_AHEAD] = value(i + V_AHEAD);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
   }
   if (!here) {
 #pragma unroll
     for (uint32_t i = 0; i < LD; ++i) x.fetch(a, w, next, then_k, then_v, tid, wv, i);
+    x.find(a, w, k0 + 2 * STEP, tid);
   }
 }
 
@@ -277,7 +292,6 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tile_kernel(Args a) {
       if (k0 + STEP > w.hi) drop_tail<T>(w, now_v, k0, tid);
       if (SIGHT && k0 < w.key0) drop_head<T>(w, now_v, k0, tid);
       step<DT>(a, w, x, now_k, now_v, then_k, then_v, k0, tid, wv);
-      x.find(a, w, k0 + 2 * STEP, tid);
       wait_loads();
       __syncthreads();
     };

@@ -101,6 +101,10 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
   // workgroup's a key head: 256 programs behind 500 keys, one of them behind 65536, 866 us
   // against 186; a prompt of 8192 with one such program 2220 against 862.
   a.splits = most > a.least * a.unit && tiles * a.kv_heads < 2048;
+  // With a sight, steps of few keys are not split either: one sequence of 500 keys, 8 key
+  // heads of 128, 11.8 us, 16.4 with splits and their second launch; of 1000 keys 15.9, 16.2;
+  // of 2000 keys 24.5, 16.1.
+  if (sight && p.step && most <= 1024) a.splits = 0;
   // runs have `least` units or more, so short contexts give fewer items than slots
   const uint64_t runs = tiles * ((most + a.unit - 1) / a.unit) / a.least;
   const uint64_t items = tiles + (a.splits ? std::min<uint64_t>(a.slots, runs + 1) : 0);

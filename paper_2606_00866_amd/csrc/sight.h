@@ -149,12 +149,22 @@ __device__ inline Work work_of(const SightArgs& a, uint32_t block, uint32_t lane
   w.item = divide(block, a.by_kv);
   w.kv = block - w.item * a.kv_heads;
   const uint32_t item = w.item;
+  // batches of up to 64: every lane has its sequence's numbers on the way while the item is found
+  const bool few = a.b.B <= 64;
+  SeqNumbers x{};
+  if (few && lane < a.b.B) x = read_sequence(a.b, lane);
   const Item it = find_item(a, lane, [&](uint32_t first, uint32_t n, uint32_t) { return item - first < n; });
   w.some = it.found;
   if (block == 0 && it.bad) report(a.b, MORI_DEV_BAD_TOKENS);
   if (!w.some) return w;
-  SeqNumbers x = read_sequence(a.b, it.b);
-  w.s = checked_sequence(a.b, SeqNumbers{same(x.lo), same(x.hi), same(x.len), same(x.p), same(x.first), same(x.last)});
+  if (few) {
+    const auto of = [&](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, (int)it.b); };
+    x = SeqNumbers{of(x.lo), of(x.hi), of(x.len), of(x.p), of(x.first), of(x.last)};
+  } else {
+    x = read_sequence(a.b, it.b);
+    x = SeqNumbers{same(x.lo), same(x.hi), same(x.len), same(x.p), same(x.first), same(x.last)};
+  }
+  w.s = checked_sequence(a.b, x);
   // more rows than a tile has only where the batch brings more tokens than it may: padding
   const uint32_t k = w.item - it.first, back = k / it.per_tile, run = k - back * it.per_tile;
   const uint32_t tiles = (w.s.n * a.group + a.tile_rows - 1) / a.tile_rows;
