@@ -1,0 +1,182 @@
+"""The operators together, as a step uses them: programs of a TierPool grow by pages of
+its free map, their new tokens are appended with positions of three axes, and attend with
+a cap, a window and ranges -- beside the same tokens on a plain copy of every program's
+keys and values -- while plans move programs out and back in between the steps."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2606_00866_amd import attention as A
+from paper_2606_00866_amd import mori as M
+from paper_2606_00866_amd.tiering import MoriError, TierPool
+from workload import Geometry
+
+pytestmark = pytest.mark.gpu
+
+KV, HEADS, DIM, BT = 2, 4, 64, 16
+SECTIONS = (12, 10, 10)
+
+
+def tier_pool(nblk, num_blocks, layers=2, room=400):
+    """Every program on the GPU, pages from the end of the pool; a table with room to grow."""
+    off = np.concatenate([[0], np.cumsum(nblk)]).astype(np.uint32)
+    total = int(off[-1])
+    ids = np.random.default_rng(3).permutation(num_blocks).astype(np.uint32)
+    free = np.ones(num_blocks, np.uint8)
+    free[ids[:total]] = 0
+    g = Geometry(layers, 2, BT, KV * DIM * 2, num_blocks)
+    tp = TierPool(g, off, ids[:total].copy(), np.zeros(len(nblk), np.uint8), free, arena_bytes=64 << 20)
+    tp.reserve(total + room)
+    return tp
+
+
+class Plain:
+    """Keys and values of every program, appended row by row."""
+
+    def __init__(self, programs, layers):
+        self.k = [[torch.zeros(0, KV, DIM, device="cuda") for _ in range(programs)] for _ in range(layers)]
+        self.v = [[torch.zeros(0, KV, DIM, device="cuda") for _ in range(programs)] for _ in range(layers)]
+
+    def step(self, layer, prog, new, q, k, v, scale, cap, window, slopes):
+        out, t = torch.empty_like(q, dtype=torch.float64), 0
+        for p, n in zip(prog, new):
+            s = slice(t, t + n)
+            self.k[layer][p] = torch.cat([self.k[layer][p], k[s].float()])
+            self.v[layer][p] = torch.cat([self.v[layer][p], v[s].float()])
+            kk, vv = self.k[layer][p].double(), self.v[layer][p].double()
+            L = kk.shape[0]
+            pos, at = torch.arange(L - n, L, device="cuda"), torch.arange(L, device="cuda")
+            kk, vv = (x.repeat_interleave(HEADS // KV, 1).permute(1, 2, 0).contiguous() for x in (kk, vv))
+            x = torch.stack([q[s, h].double() @ kk[h] for h in range(HEADS)]) * scale
+            x = cap * torch.tanh(x / cap) - slopes.double()[:, None, None] * (pos[:, None] - at).abs()
+            x = x.masked_fill((at > pos[:, None]) | (at <= pos[:, None] - window), -float("inf"))
+            w = torch.softmax(x, -1)
+            out[s] = torch.stack([w[h] @ vv[h].t() for h in range(HEADS)], 1)
+            t += n
+        return out
+
+
+def turned(x, at, rope):
+    axis = torch.tensor(A.pair_axes(SECTIONS, "turns"), device="cuda")
+    row = at.long()[axis].t()
+    m = DIM // 2
+    c, s = (rope.double()[row, torch.arange(m, device="cuda") + o][:, None] for o in (0, m))
+    y = x.double()
+    return torch.cat([y[..., :m] * c - y[..., m:] * s, y[..., m:] * c + y[..., :m] * s], -1).to(x.dtype)
+
+
+def close(out, want):
+    """Queries and keys are the same 16-bit numbers but where a rotation's rounding falls on
+    the other side (a 16-bit step of one operand in few places: 2^-8 of a score's terms),
+    weights and results are rounded to 16 bits: 2^-8 each of values up to about 4."""
+    return ((out.double() - want).abs() <= 2.0 ** -5).all()
+
+
+def test_steps_over_a_pool_whose_programs_move_and_grow():
+    P, layers, rng = 10, 2, np.random.default_rng(5)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    nblk = np.array([1] * P)
+    tp = tier_pool(nblk, 260)
+    plain = Plain(P, layers)
+    held = torch.zeros(P, dtype=torch.int32, device="cuda")
+    length = np.zeros(P, np.int64)
+    rope, slopes = A.rope_table(4000, DIM), torch.tensor([0.3, 0.05, 0.01, 0.0], device="cuda")
+    block = tp.geom.block_bytes
+    moved = 0
+    try:
+        for step in range(12):
+            here = np.flatnonzero(tp.state()[1] == M.MORI_TIER_GPU)
+            prog = rng.permutation(here)[:max(1, len(here) - 1)]
+            new = np.where(length[prog] == 0, rng.integers(5, 90, len(prog)), rng.choice([1, 1, 1, 40], len(prog)))
+            T = int(new.sum())
+            dev = lambda a: torch.from_numpy(np.ascontiguousarray(a, np.int32)).cuda()
+            g = A.TokenGrowth.of(tp, held, dev(new), dev(prog), num_tokens=T + 3, max_new=100, max_kv=2000)
+            b = g.run()
+            x = torch.randn(T + 3, HEADS + 2 * KV, DIM, device="cuda", generator=gen).bfloat16()
+            at = torch.randint(0, 4000, (3, T + 3), device="cuda", dtype=torch.int32, generator=gen)
+            for layer in range(layers):
+                q, k, v = x[:, :HEADS], x[:, HEADS:HEADS + KV], x[:, HEADS + KV:]
+                r = A.kv_append(tp.pool, tp.geom, layer, b, k, v, q=q, q_out=torch.zeros_like(q), rope=rope, positions=at,
+                                sections=SECTIONS, order="turns")
+                o = A.kv_attend(tp.pool, tp.geom, layer, b, r, scale=0.2, cap=6.0, window=70, slopes=slopes)
+                want = plain.step(layer, prog, new, turned(q[:T], at[:, :T], rope), turned(k[:T], at[:, :T], rope), v[:T], 0.2,
+                                  6.0, 70, slopes)
+                assert close(o[:T], want)
+            b.check()
+            length[prog] += new
+            assert (held.cpu().numpy() == length).all()
+            # slots name the rows that were written
+            slot = g.slots[:T]
+            rows = tp.pool.view(torch.bfloat16).view(layers, 2, tp.geom.num_blocks * BT, KV, DIM)
+            assert torch.equal(rows[1, 1, slot], x[:T, HEADS + KV:]) and (g.slots[T:] == -1).all()
+            # a plan over the grown tables: it accepts them, pages are neither lost nor owned twice
+            idle = torch.from_numpy(rng.random(P).astype(np.float32)).cuda()
+            sizes = np.diff(tp.tbl_off.cpu().numpy())
+            assert (sizes * BT >= length).all()
+            plan = tp.step(gpu_bytes=int(sizes.sum() * 0.7) * block, cpu_bytes=int(sizes.sum()) * block,
+                           idleness=idle, flags=M.MORI_F_IDLENESS_GIVEN)
+            moved += plan.n_in + plan.n_out
+            assert plan.n_drop_gpu == plan.n_drop_cpu == 0 and (tp.nblk == sizes).all()
+        assert moved > 20 and int(tp.nblk.max()) > 6
+        # and a program off the GPU is not grown
+        away = np.flatnonzero(tp.state()[1] != M.MORI_TIER_GPU)[:1]
+        before = [x.clone() for x in (tp.tbl_off, tp.tbl, tp.free_map, held)]
+        g = A.TokenGrowth.of(tp, held, dev([1]), dev(away), num_tokens=1, max_new=1, max_kv=4000)
+        with pytest.raises(MoriError) as e:
+            g.run().check()
+        assert e.value.detail == M.MORI_DEV_NOT_RESIDENT
+        assert all(torch.equal(x, y) for x, y in zip(before, (tp.tbl_off, tp.tbl, tp.free_map, held)))
+    finally:
+        tp.close()
+
+
+def test_a_captured_step_replays_while_programs_grow():
+    """Growth, append and attention in one graph: 70 decode steps over block borders, each
+    compared with the same calls made one by one on a second pool."""
+    P, layer, steps = 6, 1, 70
+    pools = [tier_pool(np.array([1] * P), 100) for _ in range(2)]
+    pools[1].pool.copy_(pools[0].pool)
+    rope, slopes = A.rope_table(4000, DIM), torch.tensor([0.3, 0.05, 0.01, 0.0], device="cuda")
+    held = [torch.zeros(P, dtype=torch.int32, device="cuda") for _ in pools]
+    prog = torch.tensor([4, 0, 3, 5], dtype=torch.int32, device="cuda")
+    new = torch.ones(4, dtype=torch.int32, device="cuda")
+    x = torch.zeros(4, HEADS + 2 * KV, DIM, dtype=torch.bfloat16, device="cuda")
+    at = torch.zeros(3, 4, dtype=torch.int32, device="cuda")
+    out = [torch.zeros(4, HEADS, DIM, dtype=torch.bfloat16, device="cuda") for _ in pools]
+    growth = [A.TokenGrowth.of(tp, h, new, prog, num_tokens=4, max_new=1, max_kv=500) for tp, h in zip(pools, held)]
+    work = [A.kv_attend_workspace(tp.geom, g.batch, out[0], sight=True) for tp, g in zip(pools, growth)]
+    r = [torch.zeros_like(o) for o in out]
+
+    def step(i):
+        tp, b = pools[i], growth[i].run()
+        q, k, v = x[:, :HEADS], x[:, HEADS:HEADS + KV], x[:, HEADS + KV:]
+        A.kv_append(tp.pool, tp.geom, layer, b, k, v, q=q, q_out=r[i], rope=rope, positions=at, sections=SECTIONS)
+        A.kv_attend(tp.pool, tp.geom, layer, b, r[i], scale=0.2, out=out[i], workspace=work[i], cap=6.0, slopes=slopes,
+                    window=60)
+
+    try:
+        new.zero_()
+        for i in (0, 1):  # nothing new: warms up without a change
+            step(i)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step(0)
+        for n in range(steps):
+            new.fill_(1) if n % 9 else new.copy_(torch.tensor([1, 0, 1, 0], dtype=torch.int32))
+            x.normal_()
+            at.random_(0, 4000)
+            graph.replay()
+            step(1)
+            live = new.nonzero().flatten()
+            rows = torch.arange(int(new.sum()), device="cuda")
+            assert torch.equal(out[0][rows], out[1][rows]) and torch.isfinite(out[0][rows]).all(), n
+            assert live.numel() in (2, 4)
+        for g in growth:
+            g.batch.check()
+        a, b = (tp.state() for tp in pools)
+        assert all((u == w).all() for u, w in zip(a, b))
+        off = pools[0].tbl_off.cpu().numpy()
+        assert (np.diff(off)[[4, 0, 3, 5]] >= [5, 4, 5, 4]).all() and (a[2].sum() == 100 - off[-1])
+    finally:
+        for tp in pools:
+            tp.close()
