@@ -221,6 +221,7 @@ class TokenGrowth:
         _need(0 < P <= M.MORI_MAX_PROGRAMS and 0 < B <= M.MORI_MAX_PROGRAMS and (program is not None or B <= P),
               "TokenGrowth: programs or sequences out of range")
         _need(0 <= num_tokens < 1 << 31, "TokenGrowth: bounds out of range")
+        _need(dev.type == "cuda", "TokenGrowth: its tensors are on a GPU")
         _need(_apart(to, (tbl_off, tbl, free_map, held), [x for x in (new_tokens, program, tier) if x is not None]),
               "TokenGrowth: into is the tensors themselves or some that overlap no others")
         self.slots = torch.empty(num_tokens, dtype=torch.int64, device=dev)
@@ -242,6 +243,7 @@ class TokenGrowth:
         # other streams' calls keep all of it from reuse
         self.batch._keep += (tbl_off, tbl, free_map, held, new_tokens, tier, *to[2:], self.slots, self.positions,
                              self._workspace)
+        self._tier_pool, self._tbl = None, tbl
         self._written = (*to, self.batch.seq_off, self.batch.kv_len, self.slots, self.positions)
 
     @classmethod
@@ -250,12 +252,16 @@ class TokenGrowth:
         """Of a ``TierPool``'s programs, in place; those on the GPU grow.  Make room in the
         table first (``TierPool.reserve``), and run it when a step's swaps have ended."""
         tier_pool.grows = True  # its sizes are read back before the next swaps
-        return cls(tier_pool.geom, tier_pool.tbl_off, tier_pool.tbl, tier_pool.free_map, held, new_tokens, program,
-                   tier=tier_pool.tier, num_tokens=num_tokens, max_new=max_new, max_kv=max_kv)
+        growth = cls(tier_pool.geom, tier_pool.tbl_off, tier_pool.tbl, tier_pool.free_map, held, new_tokens, program,
+                     tier=tier_pool.tier, num_tokens=num_tokens, max_new=max_new, max_kv=max_kv)
+        growth._tier_pool = tier_pool
+        return growth
 
     def run(self, stream=None) -> TokenBatch:
         """Calls that may overlap, on other streams, need a growth each (and tables)."""
         batch = self.batch
+        if self._tier_pool is not None and self._tier_pool.tbl is not self._tbl:
+            raise MoriError("TokenGrowth: the pool's table has moved (reserve) since this was made", M.MORI_EINVAL)
         if _current_device() != batch.index:  # launches go to the current device
             with torch.cuda.device(batch.index):
                 return self.run(stream)
@@ -397,9 +403,9 @@ def pair_axes(sections, order: str = "blocks") -> list:
     if order not in ORDERS or not 0 < len(sections) <= M.MORI_MAX_AXES or any(int(n) != n or n < 0 for n in sections):
         raise MoriError("kv_append: up to four sections, order 'blocks' or 'turns'", M.MORI_EINVAL)
     if order == "blocks":
-        return [a for a, n in enumerate(sections) for _ in range(n)]
+        return [a for a, n in enumerate(sections) for _ in range(int(n))]
     A = len(sections)
-    axes = [i % A if i // A < sections[i % A] else 0 for i in range(sum(sections))]
+    axes = [i % A if i // A < sections[i % A] else 0 for i in range(int(sum(sections)))]
     if any(axes.count(a) != n for a, n in enumerate(sections)):
         raise MoriError(f"kv_append: sections {tuple(sections)} do not fit in turns", M.MORI_EINVAL)
     return axes
@@ -408,7 +414,7 @@ def pair_axes(sections, order: str = "blocks") -> list:
 @functools.lru_cache(maxsize=64)  # the same few in every layer
 def _sections(sections: tuple, order: str):
     """Their pairs and the library's form of them, if they fit."""
-    return len(pair_axes(sections, order)), (C.c_uint32 * M.MORI_MAX_AXES)(*sections)
+    return len(pair_axes(sections, order)), (C.c_uint32 * M.MORI_MAX_AXES)(*map(int, sections))
 
 
 def _attend_desc(geom, q: torch.Tensor, scale: float | None) -> M.mori_attend:
@@ -432,7 +438,7 @@ def _sight(geom, batch: TokenBatch, heads: int, cap, slopes, window, first, end)
         if x is not None and not (x.dtype == dtype and x.shape == (n,) and x.is_contiguous() and x.device == batch.device):
             raise MoriError(f"kv_attend: {name} is a contiguous {dtype} [{n}] on the batch's device", M.MORI_EINVAL)
     ptr = lambda x: x.data_ptr() or None if x is not None else None
-    return M.mori_sight(cap or 0.0, window or 0, ptr(slopes), ptr(first), ptr(end))
+    return M.mori_sight(float(cap or 0.0), int(window or 0), ptr(slopes), ptr(first), ptr(end))
 
 
 def _empty_pool(geom) -> M.mori_pool:

@@ -64,6 +64,32 @@ CASES = {
 
 
 @pytest.mark.parametrize("in_place", [False, True])
+def test_large_pools(in_place):
+    """More pages than 2^19: larger tiles.  Pages are taken on both sides of tile borders, and
+    the last tile is a part of one."""
+    s = R.instance(21, 50, 40, (500, 4000), bt=4, held=300, spare_pages=0)
+    used = s.free.size
+    pages = (1 << 19) + 4096 + 777
+    free = np.zeros(pages, np.uint8)
+    at = np.sort(np.random.default_rng(2).permutation(np.arange(used, pages))[:s.extra["grown"] + 9])
+    free[at] = 1
+    free[-3:] = 1
+    s.free, s.geom.num_blocks = free, pages
+    g = growth(s, in_place)
+    g.run()
+    same(arrays(g), R.grow(s))
+    g.batch.check()
+
+
+def test_no_tokens():
+    s = R.instance(22, 9, 4, 0, pad=0)
+    g = growth(s, True)
+    assert g.slots.numel() == g.positions.numel() == 0
+    g.run()
+    same(arrays(g), R.grow(s))
+
+
+@pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("name", CASES)
 def test_against_definition(name, in_place):
     programs, seqs, new, kw = CASES[name]

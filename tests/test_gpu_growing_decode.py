@@ -118,6 +118,11 @@ def test_steps_over_a_pool_whose_programs_move_and_grow():
             moved += plan.n_in + plan.n_out
             assert plan.n_drop_gpu == plan.n_drop_cpu == 0 and (tp.nblk == sizes).all()
         assert moved > 20 and int(tp.nblk.max()) > 6
+        # a growth made before the table moved is refused
+        tp.reserve(tp.tbl_len + 50)
+        with pytest.raises(MoriError) as e:
+            g.run()
+        assert e.value.code == M.MORI_EINVAL
         # and a program off the GPU is not grown
         away = np.flatnonzero(tp.state()[1] != M.MORI_TIER_GPU)[:1]
         before = [x.clone() for x in (tp.tbl_off, tp.tbl, tp.free_map, held)]

@@ -69,6 +69,7 @@ SIGHTS = {
     "slopes": lambda inst, H: dict(slopes=slopes_of(H)),
     "window": lambda inst, H: dict(window=37),
     "window_of_one": lambda inst, H: dict(window=1),
+    "window_of_2000": lambda inst, H: dict(window=2000),
     "wide_window": lambda inst, H: dict(window=100000),
     "documents": lambda inst, H: dict(first=documents(inst, 30)),
     "long_documents": lambda inst, H: dict(first=documents(inst, 300)),
@@ -89,6 +90,10 @@ FORMS = {
     "tile_odd_pages_64": ([60], [500], 2, 2, 64, 12),
     "tile_many_heads": ([5, 2], [200, 90], 1, 160, 64, 16),
     "prompt": ([260], [260], 1, 3, 128, 16),
+    "tile_long": ([40, 3], [4700, 2300], 1, 4, 128, 16),
+    "step_many": ([1] * 130, list(range(1, 131)), 1, 4, 64, 16),
+    "few_many": ([1 + i % 3 for i in range(70)], [3 + 5 * i for i in range(70)], 1, 4, 64, 16),
+    "tile_many": ([1] * 40 + [45] + [1] * 40, [2 + 3 * i for i in range(40)] + [1700] + [90] * 40, 2, 4, 64, 16),
 }
 
 
@@ -203,6 +208,52 @@ def test_what_a_row_does_not_see_does_not_reach_it(form, bad):
             inst.pool[inst.layer, plane, page, row, :, 3 + plane] = 0
         want, _, bound, _ = S.attend(inst, q, 0.1, **kw)
         assert (np.abs(out - want) <= bound)[~seen].all(), (where, np.argwhere(~(np.abs(out - want) <= bound)[~seen])[:4])
+
+
+@pytest.mark.parametrize("window", range(5, 13))
+@pytest.mark.parametrize("dim", [64, 128])
+def test_first_key_inside_a_load(window, dim):
+    """The tiles' kernel loads a page's rows a few at a time: those before the first key that
+    is seen hold NaN, and so does what is behind the program's last row."""
+    inst = R.instance(90, [1], [301], kv=1, dim=dim)
+    for at in range(301 - window):
+        page, row = inst.slot(0, at)
+        inst.pool[1, :, page, row] = float("nan")
+    compare(inst, queries(inst, 40), 0.1, window=window)
+    compare(inst, queries(inst, 40), 0.1, first=np.array([301 - window], np.int32), slopes=slopes_of(40))
+
+
+def test_more_tiles_than_are_split():
+    """Enough tiles to fill the chip: each is one item, as the tiles' lines have them."""
+    inst = R.instance(91, [900, 20, 700], [900, 400, 1500], kv=16, dim=64, bt=16)
+    q = queries(inst, 48)
+    assert (inst.n.sum() * 3 // 128 + 3) * 16 < 2048  # split: the other side of the rule, by the bits
+    a = run(inst, q, 0.1, window=300)
+    big = R.instance(91, [900, 20, 700] * 4, [900, 400, 1500] * 4, kv=16, dim=64, bt=16)
+    big.pool = big.pool * 0
+    assert (big.n.sum() * 3 // 128 + 12) * 16 >= 2048
+    for b in range(12):  # the same programs four times
+        for p in (0, 1):
+            j = np.arange(int(big.length[b]))
+            pages = big.tbl[big.tbl_off[big.prog[b]] + j // 16]
+            big.pool[1, p, torch.from_numpy(pages), torch.from_numpy(j % 16)] = torch.from_numpy(inst.rows(p, b % 3, j.size)).bfloat16()
+    out, lse = run(big, q.repeat(4, 1, 1), 0.1, window=300)
+    T = q.shape[0]
+    for i in range(4):
+        # the two sum runs in other places: a rounding of the weights and of the result
+        assert (np.abs(out[i * T:(i + 1) * T] - a[0]) <= 2.0 ** -7 * np.abs(a[0]) + 2.0 ** -8).all()
+        assert np.allclose(lse[i * T:(i + 1) * T], a[1], atol=1e-4)
+    t = np.array([0, 1, 31, 32, 899, 905, 950, 1619])
+    for b, rows in ((0, t[t < 900]), (1, [900 + 5]), (2, [920 + 30, 1619])):
+        L, n, k = int(inst.length[b]), int(inst.n[b]), [inst.rows(p, b, int(inst.length[b])) for p in (0, 1)]
+        for r in rows:
+            pos = L - n + int(r) - int(inst.seq_off[b])
+            lo = max(0, pos - 299)
+            for h in (0, 47):
+                s = k[0][lo:pos + 1, h // 3] @ q[r, h].double().numpy() * 0.1
+                w = np.exp(s - s.max())
+                want = w @ k[1][lo:pos + 1, h // 3] / w.sum()
+                assert (np.abs(out[int(r), h] - want) <= 2.0 ** -6).all()
 
 
 def test_capped_infinities():
