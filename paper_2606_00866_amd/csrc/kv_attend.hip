@@ -101,10 +101,14 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
   // workgroup's a key head: 256 programs behind 500 keys, one of them behind 65536, 866 us
   // against 186; a prompt of 8192 with one such program 2220 against 862.
   a.splits = most > a.least * a.unit && tiles * a.kv_heads < 2048;
-  // With a sight, steps of few keys are not split either: one sequence of 500 keys, 8 key
-  // heads of 128, 11.8 us, 16.4 with splits and their second launch; of 1000 keys 15.9, 16.2;
-  // of 2000 keys 24.5, 16.1.
-  if (sight && p.step && most <= 1024) a.splits = 0;
+  // With a sight, steps of few keys are not split either; where the sequences alone give
+  // every CU a workgroup, that holds for more keys.  A workgroup takes 8 us for 1000 keys of
+  // two planes of 256 B (a CU reads no faster), the second launch 5 us.  Whole and split, key
+  // heads of 128, 8 of them: one sequence of 500 keys 10.8 and 14.3 us, of 1000 15.1 and
+  // 14.6, of 2000 23.7 and 14.7; 8 sequences of about 500 (up to 1100) 17.4 and 14.3; 32 of
+  // about 500 21.7 and 32.1, of 1000 39.1 and 45.2, of 2000 (up to 5000) 82.0 and 74.6; 64 of
+  // 500 31.2 and 37.9, of 1000 (up to 3000) 67.3 and 60.1.
+  if (sight && p.step && most <= (tiles * a.kv_heads < 256 ? 768 : 2048)) a.splits = 0;
   // runs have `least` units or more, so short contexts give fewer items than slots
   const uint64_t runs = tiles * ((most + a.unit - 1) / a.unit) / a.least;
   const uint64_t items = tiles + (a.splits ? std::min<uint64_t>(a.slots, runs + 1) : 0);

@@ -8,8 +8,9 @@
 //   seq_off = exclusive scan over b of n_b,  kv_len_b = held'_p = held_p + n_b
 //   slot_t  = page of t's block * block_tokens + its row,  position_t = held_p + i
 //
-// Two launches, bound by their latency and dependent reads: a byte of the free map per
-// page, an entry of the tables in and out, 12 bytes a token.
+// One or two launches, bound by their latency and dependent reads: a byte of the free map
+// per page, an entry of the tables in and out, 12 bytes a token.
+//   grow_small   everything, in one workgroup, for small pools and batches
 //   grow_count   one workgroup checks and scans the sequences and programs; the others
 //                count free pages, 512 at a time, and, where the tables grow in place,
 //                copy the old entries aside
@@ -396,6 +397,15 @@ __device__ void place_tokens(const GrowArgs& a, const Head& h, bool ok, uint32_t
   if (a.positions) a.positions[t] = at;
 }
 
+// What the batch and the programs are afterwards, by thread x of all.
+__device__ inline void store_batch(const GrowArgs& a, const Head& h, bool ok, uint32_t x) {
+  if (x == 0 && !h.error && !ok && a.error) atomicOr(a.error, MORI_DEV_NOSPC);
+  if (x <= a.B) a.seq_off[x] = ok ? a.tok[x] : 0;
+  if (x < a.B) a.kv_len[x] = ok ? a.len[x] : 0;
+  if (x < a.P && (ok || a.held_to != a.held)) a.held_to[x] = ok ? a.held_new[x] : a.held[x];
+  if (x <= a.P && h.sound) a.tbl_off_to[x] = ok ? a.new_off[x] : a.old_off[x];
+}
+
 template <int N>
 __global__ __launch_bounds__(NT) void grow_assign_kernel(GrowArgs a, uint32_t movers, uint32_t placers) {
   __shared__ uint32_t s_before[NT / 64], s_total[NT / 64];
@@ -439,13 +449,100 @@ __global__ __launch_bounds__(NT) void grow_assign_kernel(GrowArgs a, uint32_t mo
     if (lane == 0 && err && a.error) atomicOr(a.error, err);
     return;
   }
-  i -= placers;
-  if (i == 0 && tid == 0 && !h.error && !ok && a.error) atomicOr(a.error, MORI_DEV_NOSPC);
-  const uint32_t x = i * NT + tid;
-  if (x <= a.B) a.seq_off[x] = ok ? a.tok[x] : 0;
-  if (x < a.B) a.kv_len[x] = ok ? a.len[x] : 0;
-  if (x < a.P && (ok || a.held_to != a.held)) a.held_to[x] = ok ? a.held_new[x] : a.held[x];
-  if (x <= a.P && h.sound) a.tbl_off_to[x] = ok ? a.new_off[x] : a.old_off[x];
+  store_batch(a, h, ok, (i - placers) * NT + tid);
+}
+
+// All of it in one workgroup, where a pool and a batch are small (16 pages, 8 entries, 4
+// tokens and a program a thread at most): one launch, no workspace.  What the scan finds
+// and the grown table lie in LDS, and tokens find their pages there whether their blocks
+// are new or old.  Everything is read before the first barrier, so in place is as good.
+// A pool of 600 pages, 8 programs that take a token each: 8.6 us a call with two launches.
+template <int W>
+__global__ __launch_bounds__(W) void grow_small_kernel(GrowArgs a) {
+  constexpr uint32_t E = 8;
+  __shared__ uint32_t s_wave[W / 64], s_tbl[E * W], s_page[E * W];
+  __shared__ uint32_t s_old_off[W + 1], s_new_off[W + 1], s_held[W], s_tok[W + 1], s_ahead[W + 1], s_len[W], s_prog[W];
+  __shared__ Head s_head;
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  Pages<16> x;
+  const uint64_t page0 = 16ull * tid;
+  x.load(a.free_map, a.num_blocks, page0);
+  uint32_t entry[E];
+#pragma unroll
+  for (uint32_t k = 0; k < E; ++k) entry[k] = k * W + tid < a.tbl_len ? a.tbl[k * W + tid] : 0;
+  a.head = &s_head;
+  a.old_off = s_old_off;
+  a.new_off = s_new_off;
+  a.held_new = s_held;
+  a.tok = s_tok;
+  a.ahead = s_ahead;
+  a.len = s_len;
+  a.prog = s_prog;
+  scan_batch<W, 1>(a);
+  const uint32_t mine = x.count(), in = wave::incl_add(mine);
+  if (lane == 63) s_wave[wv] = in;
+  __syncthreads();
+  uint32_t r = in - mine, total = 0;  // index among the free pages
+#pragma unroll 4
+  for (uint32_t i = 0; i < W / 64; ++i) {
+    if (i < wv) r += s_wave[i];
+    total += s_wave[i];
+  }
+  const Head h = s_head;
+  const bool ok = !h.error && total >= h.more;
+  const uint32_t more = ok ? h.more : 0;
+#pragma unroll
+  for (uint32_t k = 0; k < E; ++k) {
+    uint32_t e = k * W + tid;
+    if (e >= h.entries) continue;
+    if (more) {  // else they stay where they are
+      const uint32_t p = last_not_above(s_old_off, 0, a.P - 1, e);
+      e = s_new_off[p] + (e - s_old_off[p]);  // below tbl_len
+    }
+    s_tbl[e] = entry[k];
+    if (more || !a.in_place) a.tbl_to[e] = entry[k];
+  }
+  const bool taken = r < more && mine;
+#pragma unroll
+  for (uint32_t i = 0; i < 16; ++i) {
+    const uint32_t byte = 0xFFu << (8 * (i % 4));
+    if (x.w[i / 4] & byte) {
+      if (r < more) {  // no more than the grown table's entries
+        s_page[r] = (uint32_t)page0 + i;
+        x.w[i / 4] &= ~byte;
+      }
+      ++r;
+    }
+  }
+  if (taken || a.free_to != a.free_map) x.store(a.free_to, a.num_blocks, page0);
+  store_batch(a, h, ok, tid);
+  if (tid == 0) store_batch(a, h, ok, W);  // one more of each offset than programs and sequences
+  if (more) {
+    __syncthreads();
+    for (uint32_t i = tid; i < more; i += W) {
+      const uint32_t b = last_not_above(s_ahead, 0, a.B - 1, i), p = s_prog[b];
+      const uint32_t e = s_new_off[p] + (s_old_off[p + 1] - s_old_off[p]) + (i - s_ahead[b]);
+      s_tbl[e] = a.tbl_to[e] = s_page[i];
+    }
+  }
+  if (!a.slots && !a.positions) return;
+  __syncthreads();
+  uint32_t err = 0;
+  for (uint32_t t = tid; t < a.T; t += W) {
+    int64_t slot = -1;
+    int32_t at = -1;
+    if (ok && t < h.tokens) {
+      const uint32_t b = last_not_above(s_tok, 0, a.B - 1, t), p = s_prog[b];
+      const uint32_t pos = s_len[b] - (s_tok[b + 1] - t), block = divide(pos, a.by_bt);
+      const uint32_t page = s_tbl[s_new_off[p] + block];
+      at = (int32_t)pos;
+      if (page < a.num_blocks) slot = (int64_t)((uint64_t)page * a.bt + (pos - block * a.bt));
+      else err |= page == MORI_NO_PAGE ? MORI_DEV_NOT_RESIDENT : MORI_DEV_PAGE_RANGE;
+    }
+    if (a.slots) a.slots[t] = slot;
+    if (a.positions) a.positions[t] = at;
+  }
+  if (err && a.error) atomicOr(a.error, err);
 }
 
 struct Layout {
@@ -546,6 +643,14 @@ extern "C" int mori_tables_grow(const mori_pool* pool, const mori_growth* growth
   a.error = error;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const uint32_t most = std::max(a.P, a.B);
+  const auto fits = [&](uint32_t w) {
+    return most <= w && a.num_blocks <= 16 * w && a.tbl_len <= 8 * w && a.T <= 4 * w;
+  };
+  if (fits(1024)) {
+    if (fits(256)) hipLaunchKernelGGL(grow_small_kernel<256>, dim3(1), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(grow_small_kernel<1024>, dim3(1), dim3(1024), 0, s, a);
+    return hipGetLastError() == hipSuccess ? MORI_OK : MORI_EHIP;
+  }
   const auto count = [&](auto kernel, uint32_t threads) {
     const uint64_t pages = 16ull * threads;
     hipLaunchKernelGGL(kernel, dim3(1 + a.copies + (uint32_t)((a.num_blocks + pages - 1) / pages)), dim3(threads), 0, s, a);

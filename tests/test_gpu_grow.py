@@ -60,6 +60,17 @@ CASES = {
     "tiles": (300, 200, (1, 400), dict(held=900, spare_pages=13000)),
     "pages_from_the_end": (200, 100, (1, 300), dict(held=2000, spare_pages=0, free_first=True)),
     "taken_over_tiles": (30, 30, (2000, 4000), dict(bt=4, held=50, spare_pages=3)),
+    # on both sides of what one workgroup takes: pages, entries, tokens, programs
+    "small_programs": (1024, 1024, (0, 4), dict(bt=4, held=12, spare_pages=900)),
+    "programs_above": (1025, 40, (0, 4), dict(bt=4, held=12)),
+    "programs_257": (257, 257, 1, dict(bt=4, held=12)),
+    "some_256": (256, 256, (0, 3), dict(bt=4, held=8, spare_blocks=1)),
+    "pages_4096": (30, 20, (0, 40), dict(held=50, spare_pages=4000)),
+    "pages_above": (30, 20, (0, 40), dict(held=50, spare_pages=16390)),
+    "entries_above": (40, 20, (0, 40), dict(held=50, room=8192)),
+    "tokens_above": (8, 8, 500, dict(held=50, pad=97)),
+    "tokens_4096": (8, 8, 500, dict(held=50, pad=96)),
+    "large_step": (200, 100, 1, dict(held=500, spare_pages=17000)),
 }
 
 
@@ -157,11 +168,12 @@ def refusals():
             "tokens": (None, M.MORI_DEV_BAD_TOKENS, dict(num_tokens=500))}
 
 
+@pytest.mark.parametrize("pages", [40, 17000])  # one workgroup's pool, and a larger one
 @pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("name", refusals())
-def test_what_does_not_fit_changes_nothing(name, in_place):
+def test_what_does_not_fit_changes_nothing(name, in_place, pages):
     spoil, bits, bounds = refusals()[name]
-    s = R.instance(5, 25, 12, (60, 90), held=100, spare_blocks=0)
+    s = R.instance(5, 25, 12, (60, 90), held=100, spare_blocks=0, spare_pages=pages)
     s.new[5] = 90
     if spoil:
         if name == "pages":  # one page fewer than needed; with all of them it fits
@@ -179,10 +191,11 @@ def test_what_does_not_fit_changes_nothing(name, in_place):
     assert e.value.detail == bits
 
 
+@pytest.mark.parametrize("pages", [40, 17000])
 @pytest.mark.parametrize("bad", ["start", "falls", "long"])
-def test_bad_offsets(bad):
+def test_bad_offsets(bad, pages):
     """In place nothing is written; the batch is empty."""
-    s = R.instance(6, 25, 12, (1, 9))
+    s = R.instance(6, 25, 12, (1, 9), spare_pages=pages)
     if bad == "start":
         s.tbl_off[0] = 1
     elif bad == "falls":
@@ -197,9 +210,10 @@ def test_bad_offsets(bad):
     assert e.value.detail & M.MORI_DEV_BAD_TBL_OFF
 
 
-def test_exactly_enough():
+@pytest.mark.parametrize("pad", [5, 5000])
+def test_exactly_enough(pad):
     for spare in (0, 1):
-        s = R.instance(8, 25, 12, (60, 90), held=100, spare_blocks=0, spare_pages=spare, room=spare)
+        s = R.instance(8, 25, 12, (60, 90), held=100, spare_blocks=0, spare_pages=spare, room=spare, pad=pad)
         g = growth(s, True)
         g.run()
         same(arrays(g), R.grow(s))
@@ -207,9 +221,10 @@ def test_exactly_enough():
 
 
 @pytest.mark.parametrize("page,bit", [(-1, M.MORI_DEV_NOT_RESIDENT), (10 ** 6, M.MORI_DEV_PAGE_RANGE)])
-def test_old_block_without_page(page, bit):
+@pytest.mark.parametrize("pad", [5, 5000])
+def test_old_block_without_page(page, bit, pad):
     """The token's slot is -1; the rest stands."""
-    s = R.instance(9, 10, 10, 3, held=60, spare_blocks=2, off_gpu=0.0)
+    s = R.instance(9, 10, 10, 3, held=60, spare_blocks=2, off_gpu=0.0, pad=pad)
     p = int(s.prog[4])
     s.held[p] = 20
     s.tbl_off[p + 1:] += max(0, 3 - int(s.tbl_off[p + 1] - s.tbl_off[p]))
