@@ -217,9 +217,12 @@ __device__ inline float capped_exact(const SightArgs& a, float s, float ref) {
 // Scores of one row (or, lane by lane, of several) in the softmax's units and less `ref`,
 // from the products of queries and keys; key(i) is what the i-th one's key is ahead of
 // `base`, which counts from the row's position.
+// On one side of the rows' positions a bias is a straight line, and a constant for each
+// key and one for the step take the place of the distance.
 template <int FORM, int N, typename K>
 __device__ __forceinline__ void shape_scores(const SightArgs& a, float (&y)[N], float ref, float slope, int32_t base,
                                              K key) {
+  const bool biased = FORM == UNKNOWN ? a.slopes != nullptr : FORM & BIASED;
   if (FORM == UNKNOWN ? a.cap != 0 : FORM & CAPPED) {
     if (!a.exact) {
 #pragma unroll
@@ -229,10 +232,19 @@ __device__ __forceinline__ void shape_scores(const SightArgs& a, float (&y)[N], 
       for (int i = 0; i < N; ++i) y[i] = capped_exact(a, y[i], ref);
     }
   } else {
+    if (FORM == BIASED) {
+      const bool behind = __all(base <= -key(N - 1)), ahead = __all(base >= 0);
+      if (behind || ahead) {
+        const float s = behind ? slope : -slope, b = __builtin_fmaf(s, (float)base, -ref);
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] = __builtin_fmaf(y[i], a.c, __builtin_fmaf(s, (float)key(i), b));
+        return;
+      }
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) y[i] = __builtin_fmaf(y[i], a.c, -ref);
   }
-  if (FORM == UNKNOWN ? a.slopes != nullptr : FORM & BIASED) {
+  if (biased) {
     const float b = (float)base;
 #pragma unroll
     for (int i = 0; i < N; ++i) y[i] = __builtin_fmaf(-slope, fabsf(b + (float)key(i)), y[i]);
