@@ -104,23 +104,36 @@ struct Pages {
   }
 };
 
+// Exclusive scans over i = k W + thread of values v[k], after the wavefronts' sums of every
+// k have met in LDS: `part` has K * WAVES of them, in that order.
+template <int K, int WAVES>
+__device__ inline void scan_parts(const uint32_t* part, const uint32_t (&incl)[K], const uint32_t (&v)[K], uint32_t lane,
+                                  uint32_t wv, uint32_t (&before)[K], uint32_t* total) {
+  static_assert(K * WAVES <= 64, "a wavefront scans them");
+  const uint32_t x = lane < K * WAVES ? part[lane] : 0, in = wave::incl_add(x);
+#pragma unroll
+  for (int k = 0; k < K; ++k) before[k] = (uint32_t)__shfl((int)(in - x), (int)(k * WAVES + wv)) + incl[k] - v[k];
+  *total = wave::lane63(in);
+}
+
 // The batch and the programs: checks, scans, and what grow_assign reads of them.  One
-// workgroup of W threads, K neighbouring programs and sequences each: every read of global
-// memory is under way before the first barrier, the rest is in LDS and three barriers long.
-// Sums are of 64 bits, so none wraps unseen; where something does not fit, what is written
-// here is not used.
+// workgroup of W threads, thread t with the programs and sequences t, W + t, ...: every read
+// of global memory is under way before the first barrier, the rest is in LDS and three
+// barriers long.  Totals are of 64 bits, so none wraps unseen; where something does not
+// fit, what is written here is not used.
 template <int W, int K>
 __device__ void scan_batch(const GrowArgs& a) {
   constexpr uint32_t WAVES = W / 64, NONE = 0xFFFFFFFFu, CLAIMED = 0xFFFFFFFEu;
   __shared__ uint32_t s_more[W * K], s_len[W * K], s_held[W * K], s_blocks[W * K];  // by program
   __shared__ uint8_t s_tier[W * K];
-  __shared__ uint64_t s_n[WAVES], s_m[WAVES], s_e[WAVES];
+  __shared__ uint64_t s_total[WAVES][3];
+  __shared__ uint32_t s_part[3][K * WAVES];
   __shared__ uint32_t s_error[WAVES], s_bad[WAVES];
   const uint32_t tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   uint32_t lo[K], blocks[K], held[K], n[K], prog[K], bad = 0, err = 0;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    const uint32_t p = K * tid + k;
+    const uint32_t p = k * W + tid;
     prog[k] = p < a.B ? a.program ? a.program[p] : p : NONE;
     n[k] = p < a.B ? a.new_tokens[p] : 0;
     lo[k] = blocks[k] = held[k] = 0;
@@ -139,45 +152,53 @@ __device__ void scan_batch(const GrowArgs& a) {
   bad = __ballot(bad) != 0;
   if (lane == 0) s_bad[wv] = bad;
   __syncthreads();
-  uint32_t more[K], len[K];
-  uint64_t v = 0, m = 0;
+  uint32_t more[K], len[K], n_in[K], m_in[K];
+  uint64_t n_sum = 0, m_sum = 0;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const uint32_t p = prog[k], x = n[k];
     more[k] = len[k] = n[k] = 0;
-    if (K * tid + k >= a.B) continue;
-    if (p >= a.P || atomicCAS(&s_more[p], NONE, CLAIMED) != NONE) {  // no program, or one that is here already
-      err |= MORI_DEV_BAD_TOKENS;
-      continue;
+    if (k * W + tid < a.B) {
+      if (p >= a.P || atomicCAS(&s_more[p], NONE, CLAIMED) != NONE) {  // no program, or one that is here already
+        err |= MORI_DEV_BAD_TOKENS;
+      } else {
+        const uint32_t h = s_held[p], have = s_blocks[p];
+        if (s_tier[p] != MORI_TIER_GPU) err |= MORI_DEV_NOT_RESIDENT;
+        if (x > a.max_new || (uint64_t)h + x > a.max_kv || h > (uint64_t)have * a.bt) {
+          err |= MORI_DEV_BAD_TOKENS;
+        } else {
+          n[k] = x;
+          len[k] = h + x;  // with the rounding below 2^31
+          const uint32_t need = divide(len[k] + a.bt - 1, a.by_bt);
+          more[k] = need > have ? need - have : 0;
+          s_more[p] = more[k];
+          s_len[p] = len[k];
+        }
+      }
     }
-    const uint32_t h = s_held[p], have = s_blocks[p];
-    if (s_tier[p] != MORI_TIER_GPU) err |= MORI_DEV_NOT_RESIDENT;
-    if (x > a.max_new || (uint64_t)h + x > a.max_kv || h > (uint64_t)have * a.bt) {
-      err |= MORI_DEV_BAD_TOKENS;
-      continue;
+    n_in[k] = wave::incl_add(n[k]);
+    m_in[k] = wave::incl_add(more[k]);
+    if (lane == 63) {
+      s_part[0][k * WAVES + wv] = n_in[k];
+      s_part[1][k * WAVES + wv] = m_in[k];
     }
-    n[k] = x;
-    len[k] = h + x;  // with the rounding below 2^31
-    const uint32_t need = divide(len[k] + a.bt - 1, a.by_bt);
-    more[k] = need > have ? need - have : 0;
-    s_more[p] = more[k];
-    s_len[p] = len[k];
-    v += x;
-    m += more[k];
+    n_sum += n[k];
+    m_sum += more[k];
   }
-  const uint64_t v_in = wave::incl_add(v), m_in = wave::incl_add(m);
+  n_sum = wave::sum(n_sum);
+  m_sum = wave::sum(m_sum);
   err = wave::all_or(err);
-  if (lane == 63) {
-    s_n[wv] = v_in;
-    s_m[wv] = m_in;
+  if (lane == 0) {
+    s_total[wv][0] = n_sum;
+    s_total[wv][1] = m_sum;
     s_error[wv] = err;
   }
   __syncthreads();
-  uint64_t e = 0;
-  uint32_t grown[K];
+  uint64_t e_sum = 0;
+  uint32_t grown[K], e_in[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    const uint32_t p = K * tid + k;
+    const uint32_t p = k * W + tid;
     grown[k] = 0;
     if (p < a.P) {
       const uint32_t x = s_more[p];
@@ -185,56 +206,46 @@ __device__ void scan_batch(const GrowArgs& a) {
       grown[k] = blocks[k] + (takes ? x : 0);
       a.held_new[p] = takes ? s_len[p] : held[k];
     }
-    e += grown[k];
+    e_in[k] = wave::incl_add(grown[k]);
+    if (lane == 63) s_part[2][k * WAVES + wv] = e_in[k];
+    e_sum += grown[k];
   }
-  const uint64_t e_in = wave::incl_add(e);
-  if (lane == 63) s_e[wv] = e_in;
+  e_sum = wave::sum(e_sum);
+  if (lane == 0) s_total[wv][2] = e_sum;
   __syncthreads();
-  v = v_in - v;
-  m = m_in - m;
-  e = e_in - e;
-  uint64_t v_all = 0, m_all = 0, e_all = 0;
-  bad = 0;
-#pragma unroll 2
-  for (uint32_t i = 0; i < WAVES; ++i) {
-    if (i < wv) {
-      v += s_n[i];
-      m += s_m[i];
-      e += s_e[i];
-    }
-    v_all += s_n[i];
-    m_all += s_m[i];
-    e_all += s_e[i];
-    err |= s_error[i];
-    bad |= s_bad[i];
-  }
-  if (v_all > a.T) err |= MORI_DEV_BAD_TOKENS;
+  uint32_t tok[K], ahead[K], off[K], t_all, m_all, e_all;
+  scan_parts<K, WAVES>(s_part[0], n_in, n, lane, wv, tok, &t_all);
+  scan_parts<K, WAVES>(s_part[1], m_in, more, lane, wv, ahead, &m_all);
+  scan_parts<K, WAVES>(s_part[2], e_in, grown, lane, wv, off, &e_all);
+  uint64_t sums[3];  // in full
+#pragma unroll
+  for (int j = 0; j < 3; ++j) sums[j] = wave::sum(lane < WAVES ? s_total[lane][j] : (uint64_t)0);
+  err = wave::all_or(lane < WAVES ? s_error[lane] : 0u);
+  bad = wave::all_or(lane < WAVES ? s_bad[lane] : 0u);
+  if (sums[0] > a.T) err |= MORI_DEV_BAD_TOKENS;
   if (bad) err |= MORI_DEV_BAD_TBL_OFF;
-  else if (m_all > a.num_blocks || e_all > a.tbl_len) err |= MORI_DEV_NOSPC;
+  else if (sums[1] > a.num_blocks || sums[2] > a.tbl_len) err |= MORI_DEV_NOSPC;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    const uint32_t i = K * tid + k;
+    const uint32_t i = k * W + tid;
     if (i < a.B) {
-      a.tok[i] = (uint32_t)v;
-      a.ahead[i] = (uint32_t)m;
+      a.tok[i] = tok[k];
+      a.ahead[i] = ahead[k];
       a.len[i] = len[k];
       a.prog[i] = prog[k];
     }
-    v += n[k];
-    m += more[k];
     if (i < a.P) {
-      a.new_off[i] = (uint32_t)e;
+      a.new_off[i] = off[k];
       a.old_off[i] = lo[k];
       if (i == a.P - 1) {
-        a.new_off[a.P] = (uint32_t)e + grown[k];
+        a.new_off[a.P] = e_all;
         a.old_off[a.P] = lo[k] + blocks[k];
-        *a.head = Head{err, (uint32_t)m_all, (uint32_t)v_all, bad ? 0 : lo[k] + blocks[k], !bad};
-        a.tok[a.B] = (uint32_t)v_all;
-        a.ahead[a.B] = (uint32_t)m_all;
+        *a.head = Head{err, m_all, t_all, bad ? 0 : lo[k] + blocks[k], !bad};
+        a.tok[a.B] = t_all;
+        a.ahead[a.B] = m_all;
         if (err && a.error) atomicOr(a.error, err);
       }
     }
-    e += grown[k];
   }
 }
 
