@@ -23,7 +23,7 @@ __device__ inline Union tile_union(const SightArgs& a, const Seq& s, uint32_t ro
 }
 
 __device__ inline uint32_t units_of(const SightArgs& a, uint32_t lo, uint32_t hi) {
-  const uint32_t n = (hi - lo / a.align * a.align + a.unit - 1) / a.unit;
+  const uint32_t n = (hi - (lo & ~(a.align - 1)) + a.unit - 1) >> a.unit_log;
   return n ? n : 1u;  // an empty tile is an item too: its rows are 0
 }
 

@@ -83,6 +83,7 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
     a.window = sight->window;
     a.first = sight->first;
     a.end = sight->end;
+    a.unit_log = p.step ? 7 : 6;
     a.align = p.step || a.b.bt % (512 / p.dim) ? 1 : 512 / p.dim;  // rows that a wavefront loads at once from a page
     if (a.window && !a.end) most = std::min<uint64_t>(most, (uint64_t)a.window + a.b.max_new);
     most += a.align;

@@ -41,7 +41,8 @@ struct SightArgs : AttendArgs {
   const int32_t *first, *end;
   // tiles as written down (no array: a sequence is a tile)
   uint32_t tiles;      // bound on their number
-  uint32_t align;      // a tile's keys are taken from a multiple of this on
+  uint32_t align;      // a tile's keys are taken from a multiple of this power of two on
+  uint32_t unit_log;
   struct SightTile* tile;  // [tiles]
   uint32_t* list;      // [items] an item's tile; without splits it is the item itself
   uint32_t* seq_tile;  // [B] a sequence's first one
@@ -78,16 +79,24 @@ __device__ inline Keys row_keys(const SightArgs& a, const Work& w, uint32_t r) {
   return token_keys(a, w.s, divide(w.row0 + r, a.by_group));
 }
 
-// A sequence as one tile, for the scan over the sequences.
+// A sequence as one tile, for the scan over the sequences.  More rows than a tile has
+// only where it brings more tokens than it may: padding.
 __device__ inline Share share_of(const SightArgs& a, uint32_t b) {
-  Share s = share_of(static_cast<const AttendArgs&>(a), b);
-  if (s.bad || !s.n) return s;
-  s.units = 1;
+  Share s{0, 1, 0, false};
   Seq q{};
   q.t0 = a.b.seq_off[b];
-  q.n = s.n;
+  const uint32_t end = a.b.seq_off[b + 1];
   q.len = a.b.kv_len[b];
-  if (q.n > a.b.max_new || q.len > a.b.max_kv) return s;
+  s.bad = q.t0 > end || end > a.b.T;
+  if (s.bad) return s;
+  s.n = q.n = end - q.t0;
+  if (!q.n) return s;
+  s.tiles = 1;
+  if (q.n > a.b.max_new) {
+    s.tiles = (s.n * a.group + a.tile_rows - 1) / a.tile_rows;
+    return s;
+  }
+  if (q.len > a.b.max_kv) return s;
   uint32_t lo = 0xFFFFFFFFu, hi = 0;
   if (!a.first && !a.end) {  // the first token's and the last one's
     lo = token_keys(a, q, q.len < q.n ? q.n - q.len : 0).lo;
@@ -100,7 +109,7 @@ __device__ inline Share share_of(const SightArgs& a, uint32_t b) {
       hi = max(hi, k.hi);
     }
   }
-  if (hi > lo) s.units = (hi - lo + a.unit - 1) / a.unit;
+  if (hi > lo) s.units = (hi - lo + a.unit - 1) >> a.unit_log;
   return s;
 }
 
@@ -115,6 +124,11 @@ struct Union {
   uint32_t lo, hi, from, open;
 };
 __device__ inline Union union_of(const SightArgs& a, const Seq& s, uint32_t i0, uint32_t i1, uint32_t lane) {
+  if (i1 - i0 == 1) {
+    const Keys k = token_keys(a, s, i0);
+    if (k.none()) return Union{0, 0, 0xFFFFFFFFu, 0};
+    return Union{k.lo, k.hi, k.lo, k.hi};
+  }
   uint32_t lo = 0xFFFFFFFFu, hi = 0, from = 0, open = 0xFFFFFFFFu;
   for (uint32_t i = i0 + lane; i < i1; i += 64) {
     const Keys k = token_keys(a, s, i);
@@ -134,11 +148,11 @@ __device__ inline Union union_of(const SightArgs& a, const Seq& s, uint32_t i0, 
 }
 
 __device__ inline void set_run(const SightArgs& a, Work& w, const Union& u, uint32_t run, uint32_t run_units) {
-  const uint32_t start = u.lo / a.align * a.align;
+  const uint32_t start = u.lo & ~(a.align - 1);
   const uint64_t lo = start + (uint64_t)run * run_units * a.unit, hi = lo + (uint64_t)run_units * a.unit;
-  w.key0 = u.lo;
-  w.from = u.from;
-  w.open = u.open;
+  w.key0 = same(u.lo);
+  w.from = same(u.from);
+  w.open = same(u.open);
   w.lo = same((uint32_t)min(lo, (uint64_t)0x7FFFFFFFu));
   w.hi = same((uint32_t)min(hi, (uint64_t)u.hi));
 }
@@ -165,11 +179,13 @@ __device__ inline Work work_of(const SightArgs& a, uint32_t block, uint32_t lane
     x = SeqNumbers{same(x.lo), same(x.hi), same(x.len), same(x.p), same(x.first), same(x.last)};
   }
   w.s = checked_sequence(a.b, x);
-  // more rows than a tile has only where the batch brings more tokens than it may: padding
-  const uint32_t k = w.item - it.first, back = k / it.per_tile, run = k - back * it.per_tile;
-  const uint32_t tiles = (w.s.n * a.group + a.tile_rows - 1) / a.tile_rows;
+  uint32_t run = w.item - it.first;
+  if (w.s.n > a.b.max_new) {
+    const uint32_t back = run / it.per_tile, tiles = (w.s.n * a.group + a.tile_rows - 1) / a.tile_rows;
+    run -= back * it.per_tile;
+    w.row0 = same((tiles - 1 - back) * a.tile_rows);
+  }
   w.per_tile = it.per_tile;
-  w.row0 = same((tiles - 1 - back) * a.tile_rows);
   w.rows = min(a.tile_rows, w.s.n * a.group - w.row0);
   Union u{0, 0, 0, 0};
   if (!w.s.error) u = union_of(a, w.s, 0, w.s.n, lane);
