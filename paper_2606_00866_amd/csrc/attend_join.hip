@@ -27,7 +27,10 @@ __global__ __launch_bounds__(64 * NW) void attend_join_kernel(Args a, uint32_t s
   const uint32_t t = blockIdx.x / per_token, h0 = (blockIdx.x - t * per_token) * heads_wg + (WPH > 1 ? 0 : wv * some);
   Item it;
   bool lines = false;  // tiles are written down, with runs of their own
-  if constexpr (SIGHT) lines = a.tile != nullptr;
+  if constexpr (SIGHT) {
+    lines = a.tile != nullptr;
+    if (lines && !same(a.seq_tile[a.b.B])) return;  // no tile was split
+  }
   if (lines) it.b = find_sequence(a.b, t, lane);
   else it = find_item(a, lane, [&](uint32_t, uint32_t n, uint32_t b) {
     return n && a.b.seq_off[b] <= t && t < a.b.seq_off[b + 1];

@@ -178,6 +178,7 @@ __global__ __launch_bounds__(NT) void sight_items_kernel(SightArgs a) {
     at += runs[k];
   }
   for (uint32_t i = items + tid; i < a.items; i += NT) a.list[i] = NO_TILE;
+  if (tid == 0) a.seq_tile[a.b.B] = items > tiles;
 }
 
 }  // namespace

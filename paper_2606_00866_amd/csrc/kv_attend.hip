@@ -123,7 +123,7 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
     p.tile_at = (p.bytes + 15) / 16 * 16;
     p.list_at = p.tile_at + tiles * sizeof(SightTile);
     p.seq_at = p.list_at + (a.splits ? items * sizeof(uint32_t) : 0);
-    p.bytes = p.seq_at + (uint64_t)a.b.B * sizeof(uint32_t);
+    p.bytes = p.seq_at + ((uint64_t)a.b.B + 1) * sizeof(uint32_t);
     a.tiles = (uint32_t)tiles;
   }
   return true;
