@@ -25,6 +25,10 @@
 // 128; with 17 to 32 rows 292, one wavefront a SIMD).  One sequence of 65502 keys, one key
 // head (34 MB): 17 us with the join, 2 TB/s: finding the item, two rounds of dependent
 // reads (table, keys) and the second launch.  Eight sequences of 760 keys: 10 us.
+//
+// With a sight (sight.h) one form serves caps, biases, windows and ranges: it is the bytes
+// that bound it.  64 sequences that see 4096 keys each (1.07 GB): 200 us, 5.4 TB/s.  One
+// sequence of 65502 keys with a bias: 18.3 us, eight of 760 with a cap 11.9.
 #include "sight.h"
 
 namespace mori {

@@ -18,7 +18,9 @@
 //
 // Bound by bytes: prompt chunks of five programs (16587 tokens, 32 query and 8 key
 // heads of 128; 416 MB) take 77 us, 5.4 TB/s; a decode step of eight agents (4 key
-// heads of 64) 3.7 us, where the launch and two dependent reads are the time.
+// heads of 64) 3.7 us, where the launch and two dependent reads are the time.  With three
+// axes 77 and 3.9 us; axes in turns over 2 key and 16 query heads (73 MB) 17.1 us, 28.2
+// where every unit gathered its own.
 #include "float16.h"
 #include "tokens.h"
 

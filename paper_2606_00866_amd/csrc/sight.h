@@ -21,7 +21,7 @@
 // of a score's unit.  Above, scores below the cap take x P(x^2) instead, P of six terms
 // with a relative error of 7e-7 (a minimax fit on [0, 1]), so they keep their relative
 // accuracy whatever the cap.  (The polynomial alone, where all of a step's scores are
-// small, is no faster: prompts of 20000 tokens 1656 us, 1592 with the other form.)
+// small, is no faster: prompts of 20600 tokens 1656 us, 1592 with the other form.)
 //
 // Reference.  Scores are taken relative to where the maximum was last followed in the
 // instruction that finishes them, so neither caps nor biases cost another one for it; a

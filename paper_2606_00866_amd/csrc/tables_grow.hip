@@ -9,7 +9,9 @@
 //   slot_t  = page of t's block * block_tokens + its row,  position_t = held_p + i
 //
 // One or two launches, bound by their latency and dependent reads: a byte of the free map
-// per page, an entry of the tables in and out, 12 bytes a token.
+// per page, an entry of the tables in and out, 12 bytes a token.  A step of 8 programs
+// (600 pages) takes 6.1 us, of 400 of 1024 (300 000 pages) 10.9, of 3000 of 4096 16.6;
+// chunks of 24 of 64 programs (60 000 tokens, 4000 pages) 9.
 //   grow_small   everything, in one workgroup, for small pools and batches
 //   grow_count   one workgroup checks and scans the sequences and programs; the others
 //                count free pages, 512 at a time, and, where the tables grow in place,
@@ -27,7 +29,10 @@ namespace mori {
 namespace {
 
 constexpr uint32_t NT = 256;
-constexpr uint32_t COUNTED = 512;   // pages of a count: the smallest tile
+// Pages of a count: the smallest tile.  A tile's workgroup also writes the slots of all
+// tokens in its pages: with 4096 pages a tile chunks of 60 000 tokens took 28 us there,
+// with 512 5.5.
+constexpr uint32_t COUNTED = 512;
 constexpr uint32_t ENTRIES = 1024;  // table entries of a workgroup
 constexpr uint32_t MOST = MORI_MAX_PROGRAMS;
 
@@ -80,11 +85,13 @@ struct Pages {
       }
       return;
     }
+    uint8_t x[N];  // all reads at once, of the last page where there is none
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = map[page + i < num_blocks ? page + i : num_blocks - 1u];
 #pragma unroll
     for (int i = 0; i < W; ++i) w[i] = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (page + i < num_blocks) w[i / 4] |= (uint32_t)map[page + i] << (8 * (i % 4));
+    for (int i = 0; i < N; ++i) w[i / 4] |= page + i < num_blocks ? (uint32_t)x[i] << (8 * (i % 4)) : 0u;
   }
   __device__ __forceinline__ void store(uint8_t* map, uint32_t num_blocks, uint64_t page) const {
     if (page + N <= num_blocks) {
@@ -93,8 +100,23 @@ struct Pages {
       return;
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (page + i < num_blocks) map[page + i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
+    for (int i = 0; i < W; ++i) {
+#pragma unroll 1
+      for (int j = 0; j < 4 && 4 * i + j < N; ++j)
+        if (page + 4 * i + j < num_blocks) map[page + 4 * i + j] = (uint8_t)(w[i] >> (8 * j));
+    }
+  }
+  // Takes free pages out, the first one as the r-th, while r is below `end`: to(r, its index here).
+  template <typename F>
+  __device__ __forceinline__ void take(uint32_t r, uint32_t end, F to) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      for (uint32_t bits = set_bytes(w[i]); bits && r < end; bits &= bits - 1, ++r) {
+        const uint32_t j = (uint32_t)__builtin_ctz(bits) / 8;
+        to(r, 4 * i + j);
+        w[i] &= ~(0xFFu << (8 * j));
+      }
+    }
   }
   __device__ __forceinline__ uint32_t count() const {
     uint32_t n = 0;
@@ -289,8 +311,10 @@ __device__ inline uint32_t wave_last_not_above(const uint32_t* x, uint32_t n, ui
     step = (step + 63) / 64;
   }
 }
-// The same by a thread between two indexes.
-__device__ inline uint32_t last_not_above(const uint32_t* x, uint32_t lo, uint32_t hi, uint32_t v) {
+// The same by a thread between two indexes.  X: a pointer, or an array in LDS, which stays
+// one to the compiler so.
+template <typename X>
+__device__ __forceinline__ uint32_t last_not_above(const X& x, uint32_t lo, uint32_t hi, uint32_t v) {
   while (lo < hi) {
     const uint32_t mid = (lo + hi + 1) / 2;
     if (x[mid] <= v) lo = mid;
@@ -328,17 +352,7 @@ __device__ void assign_tile(const GrowArgs& a, const Head& h, bool ok, uint32_t 
       count += s_wave[i];
     }
     count = min(count, more - base);
-#pragma unroll
-    for (uint32_t i = 0; i < N; ++i) {
-      const uint32_t byte = 0xFFu << (8 * (i % 4));
-      if (x.w[i / 4] & byte) {
-        if (r < count) {
-          s_taken[r].page = (uint32_t)page0 + i;
-          x.w[i / 4] &= ~byte;
-        }
-        ++r;
-      }
-    }
+    x.take(r, count, [&](uint32_t at, uint32_t i) { s_taken[at].page = (uint32_t)page0 + i; });
     __syncthreads();
     for (uint32_t i = tid; i < count; i += NT) {
       // sequences that take none share their number with the next: the last of them takes it
@@ -467,7 +481,8 @@ __global__ __launch_bounds__(NT) void grow_assign_kernel(GrowArgs a, uint32_t mo
 // tokens and a program a thread at most): one launch, no workspace.  What the scan finds
 // and the grown table lie in LDS, and tokens find their pages there whether their blocks
 // are new or old.  Everything is read before the first barrier, so in place is as good.
-// A pool of 600 pages, 8 programs that take a token each: 8.6 us a call with two launches.
+// A pool of 600 pages, 8 programs that take a token each: 6.1 us a call (64 threads; 6.5
+// with 256), 8.7 with the two launches, which in a graph take 5.6.
 template <int W>
 __global__ __launch_bounds__(W) void grow_small_kernel(GrowArgs a) {
   constexpr uint32_t E = 8;
@@ -478,9 +493,9 @@ __global__ __launch_bounds__(W) void grow_small_kernel(GrowArgs a) {
   Pages<16> x;
   const uint64_t page0 = 16ull * tid;
   x.load(a.free_map, a.num_blocks, page0);
-  uint32_t entry[E];
+  uint32_t entry[E];  // neighbours
 #pragma unroll
-  for (uint32_t k = 0; k < E; ++k) entry[k] = k * W + tid < a.tbl_len ? a.tbl[k * W + tid] : 0;
+  for (uint32_t k = 0; k < E; ++k) entry[k] = E * tid + k < a.tbl_len ? a.tbl[E * tid + k] : 0;
   a.head = &s_head;
   a.old_off = s_old_off;
   a.new_off = s_new_off;
@@ -502,42 +517,43 @@ __global__ __launch_bounds__(W) void grow_small_kernel(GrowArgs a) {
   const Head h = s_head;
   const bool ok = !h.error && total >= h.more;
   const uint32_t more = ok ? h.more : 0;
-#pragma unroll
-  for (uint32_t k = 0; k < E; ++k) {
-    uint32_t e = k * W + tid;
-    if (e >= h.entries) continue;
-    if (more) {  // else they stay where they are
-      const uint32_t p = last_not_above(s_old_off, 0, a.P - 1, e);
-      e = s_new_off[p] + (e - s_old_off[p]);  // below tbl_len
+  if (E * tid < h.entries) {
+    uint32_t p = 0, end = 0xFFFFFFFFu, up = 0;  // how far an entry moves: it stays where nothing is taken
+    if (more) {
+      p = last_not_above(s_old_off, 0, a.P - 1, E * tid);
+      end = s_old_off[p + 1];
+      up = s_new_off[p] - s_old_off[p];
     }
-    s_tbl[e] = entry[k];
-    if (more || !a.in_place) a.tbl_to[e] = entry[k];
+#pragma unroll
+    for (uint32_t k = 0; k < E; ++k) {
+      const uint32_t e = E * tid + k;
+      if (e >= h.entries) break;
+      while (e >= end) {
+        ++p;
+        end = s_old_off[p + 1];
+        up = s_new_off[p] - s_old_off[p];
+      }
+      s_tbl[e + up] = entry[k];  // below tbl_len
+    }
   }
   const bool taken = r < more && mine;
-#pragma unroll
-  for (uint32_t i = 0; i < 16; ++i) {
-    const uint32_t byte = 0xFFu << (8 * (i % 4));
-    if (x.w[i / 4] & byte) {
-      if (r < more) {  // no more than the grown table's entries
-        s_page[r] = (uint32_t)page0 + i;
-        x.w[i / 4] &= ~byte;
-      }
-      ++r;
-    }
-  }
-  if (taken || a.free_to != a.free_map) x.store(a.free_to, a.num_blocks, page0);
-  store_batch(a, h, ok, tid);
-  if (tid == 0) store_batch(a, h, ok, W);  // one more of each offset than programs and sequences
+  x.take(r, more, [&](uint32_t at, uint32_t i) { s_page[at] = (uint32_t)page0 + i; });  // no more than entries
   if (more) {
     __syncthreads();
     for (uint32_t i = tid; i < more; i += W) {
       const uint32_t b = last_not_above(s_ahead, 0, a.B - 1, i), p = s_prog[b];
-      const uint32_t e = s_new_off[p] + (s_old_off[p + 1] - s_old_off[p]) + (i - s_ahead[b]);
-      s_tbl[e] = a.tbl_to[e] = s_page[i];
+      s_tbl[s_new_off[p] + (s_old_off[p + 1] - s_old_off[p]) + (i - s_ahead[b])] = s_page[i];
     }
   }
-  if (!a.slots && !a.positions) return;
   __syncthreads();
+  // every store from here on: a barrier behind one would wait for it
+  if (more || !a.in_place) {
+    for (uint32_t e = tid; e < h.entries + more; e += W) a.tbl_to[e] = s_tbl[e];
+  }
+  if (taken || a.free_to != a.free_map) x.store(a.free_to, a.num_blocks, page0);
+  store_batch(a, h, ok, tid);
+  if (tid == 0) store_batch(a, h, ok, W);  // one more of each offset than programs and sequences
+  if (!a.slots && !a.positions) return;
   uint32_t err = 0;
   for (uint32_t t = tid; t < a.T; t += W) {
     int64_t slot = -1;
@@ -658,7 +674,8 @@ extern "C" int mori_tables_grow(const mori_pool* pool, const mori_growth* growth
     return most <= w && a.num_blocks <= 16 * w && a.tbl_len <= 8 * w && a.T <= 4 * w;
   };
   if (fits(1024)) {
-    if (fits(256)) hipLaunchKernelGGL(grow_small_kernel<256>, dim3(1), dim3(256), 0, s, a);
+    if (fits(64)) hipLaunchKernelGGL(grow_small_kernel<64>, dim3(1), dim3(64), 0, s, a);
+    else if (fits(256)) hipLaunchKernelGGL(grow_small_kernel<256>, dim3(1), dim3(256), 0, s, a);
     else hipLaunchKernelGGL(grow_small_kernel<1024>, dim3(1), dim3(1024), 0, s, a);
     return hipGetLastError() == hipSuccess ? MORI_OK : MORI_EHIP;
   }

@@ -60,7 +60,14 @@ CASES = {
     "tiles": (300, 200, (1, 400), dict(held=900, spare_pages=13000)),
     "pages_from_the_end": (200, 100, (1, 300), dict(held=2000, spare_pages=0, free_first=True)),
     "taken_over_tiles": (30, 30, (2000, 4000), dict(bt=4, held=50, spare_pages=3)),
-    # on both sides of what one workgroup takes: pages, entries, tokens, programs
+    # on both sides of what a workgroup of 64, 256 and 1024 threads takes: pages, entries, tokens, programs
+    "pages_1024": (10, 8, (0, 40), dict(held=50, spare_pages=980)),
+    "pages_1030": (10, 8, (0, 40), dict(held=50, spare_pages=1020)),
+    "entries_512": (20, 8, (0, 20), dict(held=50, room=520)),
+    "tokens_256": (8, 8, 30, dict(held=50, pad=16)),
+    "tokens_257": (8, 8, 30, dict(held=50, pad=17)),
+    "programs_65": (65, 30, (0, 5), dict(held=20)),
+    "pages_17": (2, 1, 40, dict(held=20, spare_pages=9)),
     "small_programs": (1024, 1024, (0, 4), dict(bt=4, held=12, spare_pages=900)),
     "programs_above": (1025, 40, (0, 4), dict(bt=4, held=12)),
     "programs_257": (257, 257, 1, dict(bt=4, held=12)),
