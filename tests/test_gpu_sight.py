@@ -364,3 +364,84 @@ def test_bad_batches():
             b.check()
         assert e.value.detail == M.MORI_DEV_BAD_TOKENS
         assert (out[:6] == 0).all() and torch.isfinite(out).all() and (out[6:] != 0).any()
+
+
+@pytest.mark.parametrize("form", ["step_long", "few_many", "tile_long", "tile_many"])
+def test_workspace_is_what_is_used(form):
+    """Exactly the size asked for, with bytes behind it that stay as they are."""
+    n, length, kv, H, dim, bt = FORMS[form]
+    inst = R.instance(95, n, length, kv=kv, dim=dim, bt=bt)
+    q, pool, b = queries(inst, H).cuda(), inst.pool.cuda(), R.batch(inst)
+    size = A.kv_attend_workspace(inst.geom, b, q, sight=True).numel()
+    guarded = torch.full((size + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    for kw in (dict(cap=5.0), dict(window=900), dict(first=dev(documents(inst, 500)))):
+        A.kv_attend(pool, inst.geom, 1, b, q, scale=0.1, workspace=guarded[:size], **kw)
+        assert (guarded[size:] == 0x5A).all()
+    b.check()
+
+
+@pytest.mark.parametrize("n,H", [(40, 8), (1, 8)])
+def test_overlapping_sequences_stay_inside_the_workspace(n, H):
+    """Offsets that name tokens twice give more tiles and items than there is room for: the
+    fault is reported, what is written stays in bounds."""
+    inst = R.instance(96, [n] * 9, [3000] * 9, kv=1, dim=128)
+    inst.seq_off = np.array([0, n, 0, n, 0, n, 0, n, 0, n])
+    b = R.batch(inst, tokens=n)
+    q = torch.randn(n, H, 128).to(BF16).cuda()
+    size = A.kv_attend_workspace(inst.geom, b, q, sight=True).numel()
+    guarded = torch.full((size + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    for kw in (dict(cap=5.0), dict(window=2500), dict(end=torch.full((n,), 3000, dtype=torch.int32, device="cuda"))):
+        A.kv_attend(inst.pool.cuda(), inst.geom, 1, b, q, scale=0.1, workspace=guarded[:size], **kw)
+        torch.cuda.synchronize()
+        assert int(b.error.item()) == M.MORI_DEV_BAD_TOKENS
+        assert (guarded[size:] == 0x5A).all()
+
+
+def test_overlap_of_calls():
+    """Two calls of one batch on two streams, a workspace each, at once and again."""
+    inst = R.instance(97, [60, 1, 1], [2000, 900, 1500], kv=2, dim=64)
+    q, pool, b = queries(inst, 8).cuda(), inst.pool.cuda(), R.batch(inst)
+    first = dev(documents(inst, 300))
+    kws = [dict(window=700, cap=9.0), dict(first=first, slopes=dev(slopes_of(8)))]
+    want = [A.kv_attend(pool, inst.geom, 1, b, q, scale=0.1, **kw) for kw in kws]
+    ws = [A.kv_attend_workspace(inst.geom, b, q, sight=True) for _ in kws]
+    out = [torch.empty_like(w) for w in want]
+    streams = [torch.cuda.Stream() for _ in kws]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, kw, w, o in zip(streams, kws, ws, out):
+            A.kv_attend(pool, inst.geom, 1, b, q, scale=0.1, workspace=w, out=o, stream=s, **kw)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for o, w in zip(out, want))
+    b.check()
+
+
+def test_pages_behind_four_gigabytes():
+    """A pool whose planes pass 2^32 bytes, the programs' pages at its end: the same bits as
+    over a small one, appended with axes and attended to with a sight."""
+    layers, bt, dim, blocks = 1, 16, 128, (1 << 20) + 3000
+    for n, length, H in (([1, 3], [300, 900], 4), ([50, 20], [600, 300], 4)):
+        inst = R.instance(98, n, length, kv=1, dim=dim, bt=bt, layers=1, layer=0)
+        T = sum(n)
+        x = torch.randn(T, H + 2, dim, device="cuda").bfloat16()
+        at = torch.randint(0, 500, (3, T), device="cuda", dtype=torch.int32)
+        rope, kw = A.rope_table(500, dim), dict(scale=0.1, cap=7.0, window=250, slopes=dev(slopes_of(H)))
+        out = []
+        for large in (False, True):
+            if large:
+                small = inst.pool
+                inst.geom = R.Geom(layers, 2, bt, dim * 2, blocks)
+                pool = torch.empty(1, 2, blocks, bt, 1, dim, dtype=BF16, device="cuda")
+                shift = blocks - small.shape[2]
+                pool[:, :, shift:] = small.cuda()
+                inst.tbl = inst.tbl + shift
+            else:
+                pool = inst.pool.cuda()
+            b = R.batch(inst)
+            q = A.kv_append(pool, inst.geom, 0, b, x[:, H:H + 1], x[:, H + 1:], q=x[:, :H], rope=rope, positions=at,
+                            sections=(16, 24, 24))
+            out.append(A.kv_attend(pool, inst.geom, 0, b, q, **kw))
+            b.check()
+        assert torch.equal(*out) and torch.isfinite(out[0]).all()
+        del pool
+        torch.cuda.empty_cache()
