@@ -13,6 +13,8 @@
 // least time is taken.  Four chunks (1700 tokens, 8 key heads) with a window of 4096 are
 // left whole so, 456 workgroups of 65 steps: 155 us, 235 where 1536 workgroups were aimed
 // at (three rounds and a bit, and 31 us of joins).  The kernel itself takes 8.9 us there.
+#include <cstdlib>
+
 #include "sight.h"
 
 namespace mori {
@@ -32,7 +34,8 @@ __device__ inline uint32_t units_of(const SightArgs& a, uint32_t lo, uint32_t hi
 __global__ __launch_bounds__(256) void sight_tiles_kernel(SightArgs a) {
   const uint32_t lane = threadIdx.x & 63, tile = blockIdx.x * 4 + wave_index();
   if (tile >= a.tiles) return;
-  AttendArgs whole = a;
+  AttendArgs whole = a;  // a tile is one run here
+  whole.splits = 0;
   const Item it = find_item(whole, lane, [&](uint32_t first, uint32_t n, uint32_t) { return tile - first < n; });
   if (tile == 0 && it.bad && lane == 0) report(a.b, MORI_DEV_BAD_TOKENS);
   uint4* const to = reinterpret_cast<uint4*>(a.tile + tile);
@@ -50,8 +53,11 @@ __global__ __launch_bounds__(256) void sight_tiles_kernel(SightArgs a) {
   to[0] = uint4{u.lo, u.hi, u.from, u.open};
   to[1] = uint4{s.t0, s.n, s.len, s.tbl};
   to[2] = uint4{row0, tile, 1, 0x7FFFFFFFu};
+  if (a.splits && back == 0) a.seq_tile[it.b] = it.first;
 }
 
+
+static const uint32_t FEW = getenv("FEW") ? atoi(getenv("FEW")) : 64;
 constexpr uint32_t NT = 1024, WAVES = NT / 64, MOST = 2048, K = MOST / NT;
 
 __device__ inline uint32_t scan_before(uint32_t v, uint32_t* s_wave, uint32_t* total) {
@@ -70,11 +76,10 @@ __device__ inline uint32_t scan_before(uint32_t v, uint32_t* s_wave, uint32_t* t
   return before;
 }
 
-__global__ __launch_bounds__(NT) void sight_items_kernel(SightArgs a) {
+// The tiles by this workgroup, their units and first rows in LDS; their number.
+__device__ inline uint32_t write_tiles(const SightArgs& a, uint32_t* s_units, uint32_t* s_row0, uint32_t* s_wave) {
   __shared__ uint4 s_seq[MOST];                    // t0, n, len, tbl
-  __shared__ uint32_t s_tile0[MOST], s_units[MOST], s_row0[MOST];
-  __shared__ uint32_t s_wave[WAVES], s_run[WAVES];
-  __shared__ float s_cost[WAVES];
+  __shared__ uint32_t s_tile0[MOST];
   const uint32_t tid = threadIdx.x, lane = tid & 63, wv = wave_index();
   // sequences: there are fewer of them than tiles may be
   uint32_t mine = 0, err = 0, have[K];
@@ -128,7 +133,33 @@ __global__ __launch_bounds__(NT) void sight_items_kernel(SightArgs a) {
       s_row0[tile] = row0;
     }
   }
-  __syncthreads();
+  return tiles;
+}
+
+// READY: the tiles are written down already.
+template <bool READY>
+__global__ __launch_bounds__(NT) void sight_items_kernel(SightArgs a) {
+  __shared__ uint32_t s_units[MOST], s_row0[MOST], s_wave[WAVES], s_run[WAVES];
+  __shared__ float s_cost[WAVES];
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wv = wave_index();
+  uint32_t tiles;
+  if constexpr (READY) {
+    uint32_t mine = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < K; ++k) {
+      const uint32_t t = K * tid + k;
+      if (t >= a.tiles) continue;
+      const uint4* const at = reinterpret_cast<const uint4*>(a.tile + t);
+      const uint4 x = at[0], z = at[2];
+      s_units[t] = z.z ? units_of(a, x.x, x.y) : 0;
+      s_row0[t] = z.x;
+      mine += z.z;
+    }
+    scan_before(mine, s_wave, &tiles);
+  } else {
+    tiles = write_tiles(a, s_units, s_row0, s_wave);
+    __syncthreads();
+  }
   // the length of the runs
   uint32_t units[K], total;
 #pragma unroll
@@ -169,7 +200,7 @@ __global__ __launch_bounds__(NT) void sight_items_kernel(SightArgs a) {
   uint32_t runs[K], items;
 #pragma unroll
   for (uint32_t k = 0; k < K; ++k) runs[k] = (units[k] + run - 1) / run;
-  at = scan_before(runs[0] + runs[1], s_wave, &items);
+  uint32_t at = scan_before(runs[0] + runs[1], s_wave, &items);
 #pragma unroll
   for (uint32_t k = 0; k < K; ++k) {
     const uint32_t t = K * tid + k;
@@ -186,8 +217,12 @@ __global__ __launch_bounds__(NT) void sight_items_kernel(SightArgs a) {
 }  // namespace
 
 void launch_sight_tiles(const SightArgs& a, hipStream_t s) {
-  if (a.splits) hipLaunchKernelGGL(sight_items_kernel, dim3(1), dim3(NT), 0, s, a);
-  else hipLaunchKernelGGL(sight_tiles_kernel, dim3((a.tiles + 3) / 4), dim3(256), 0, s, a);
+  if (a.splits && a.tiles <= FEW) {
+    hipLaunchKernelGGL(sight_items_kernel<false>, dim3(1), dim3(NT), 0, s, a);
+    return;
+  }
+  hipLaunchKernelGGL(sight_tiles_kernel, dim3((a.tiles + 3) / 4), dim3(256), 0, s, a);
+  if (a.splits) hipLaunchKernelGGL(sight_items_kernel<true>, dim3(1), dim3(NT), 0, s, a);
 }
 
 }  // namespace mori
