@@ -457,5 +457,6 @@ void launch_attend_latent(const AttendArgs& a, bool f16, hipStream_t s);
 void launch_attend_join(const AttendArgs& a, bool f16, uint32_t value, hipStream_t s);
 void launch_attend_join(const SightArgs& a, bool f16, uint32_t value, hipStream_t s);
 void launch_sight_tiles(const SightArgs& a, hipStream_t s);
+void launch_sight_join(const SightArgs& a, bool f16, uint32_t dim, hipStream_t s);
 
 }  // namespace mori

@@ -18,48 +18,30 @@ namespace {
 // are on the way at once), else a wavefront takes `some` heads of a token.
 template <typename DT, int DV, int NW, int WPH, typename Args>
 __global__ __launch_bounds__(64 * NW) void attend_join_kernel(Args a, uint32_t some) {
-  constexpr bool SIGHT = IsSight<Args>::value;
   constexpr int W = DV / 64;                // elements of a lane
   typedef float vec __attribute__((ext_vector_type(W)));
   __shared__ float s_y[WPH > 1 ? NW : 1][DV], s_l[NW];
   const uint32_t lane = threadIdx.x & 63, wv = wave_index();
   const uint32_t heads_wg = WPH > 1 ? 1 : NW * some, per_token = (a.heads + heads_wg - 1) / heads_wg;
   const uint32_t t = blockIdx.x / per_token, h0 = (blockIdx.x - t * per_token) * heads_wg + (WPH > 1 ? 0 : wv * some);
-  Item it;
-  bool lines = false;  // tiles are written down, with runs of their own
-  if constexpr (SIGHT) {
-    lines = a.tile != nullptr;
-    if (lines && !same(a.seq_tile[a.b.B])) return;  // no tile was split
-  }
-  if (lines) it.b = find_sequence(a.b, t, lane);
-  else it = find_item(a, lane, [&](uint32_t, uint32_t n, uint32_t b) {
+  const Item it = find_item(a, lane, [&](uint32_t, uint32_t n, uint32_t b) {
     return n && a.b.seq_off[b] <= t && t < a.b.seq_off[b + 1];
   });
-  if (!lines && (!it.found || it.per_tile < 2)) return;
-  const uint32_t t0 = same(a.b.seq_off[it.b]), t1 = same(a.b.seq_off[it.b + 1]), n = t1 - t0;
-  if (lines && (t0 > t || t >= t1 || t1 > a.b.T)) return;
+  if (!it.found || it.per_tile < 2) return;
+  const uint32_t t0 = same(a.b.seq_off[it.b]), n = same(a.b.seq_off[it.b + 1]) - t0;
   const Seq s = sequence(a.b, it.b);
   bool none;
-  if constexpr (SIGHT) none = token_keys(a, s, t - s.t0).none();
+  if constexpr (IsSight<Args>::value) none = token_keys(a, s, t - s.t0).none();
   else none = s.position(t - s.t0) < 0;
   const uint32_t tiles = (n * a.group + a.tile_rows - 1) / a.tile_rows;
   const uint64_t step = (uint64_t)a.kv_heads * a.tile_rows;
+  const uint32_t runs = it.per_tile;
+  const uint32_t r0 = WPH > 1 ? (uint32_t)((uint64_t)runs * wv / NW) : 0;
+  const uint32_t r1 = WPH > 1 ? (uint32_t)((uint64_t)runs * (wv + 1) / NW) : runs;
   for (uint32_t h = h0; h < min(h0 + some, a.heads); ++h) {
     const uint32_t kv = divide(h, a.by_group), x = (t - t0) * a.group + (h - kv * a.group);
     const uint32_t tile = x / a.tile_rows;
-    uint64_t item = it.first + (uint64_t)(tiles - 1 - tile) * it.per_tile;
-    if constexpr (SIGHT) {
-      if (lines) {
-        const uint32_t i = same(a.seq_tile[it.b]) + (tiles - 1 - tile);
-        if (i >= a.tiles) continue;
-        item = same(a.tile[i].first);
-        it.per_tile = same(a.tile[i].runs);
-        if (it.per_tile < 2) continue;
-      }
-    }
-    const uint32_t runs = it.per_tile;
-    const uint32_t r0 = WPH > 1 ? (uint32_t)((uint64_t)runs * wv / NW) : 0;
-    const uint32_t r1 = WPH > 1 ? (uint32_t)((uint64_t)runs * (wv + 1) / NW) : runs;
+    const uint64_t item = it.first + (uint64_t)(tiles - 1 - tile) * it.per_tile;
     if (item + it.per_tile > a.items) continue;  // sequences that overlap: more items than tokens give, which were not run
     const uint64_t at0 = (item * a.kv_heads + kv) * a.tile_rows + (x - tile * a.tile_rows);
 

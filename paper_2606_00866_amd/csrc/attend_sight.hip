@@ -2,8 +2,9 @@
 //
 // Without splits a tile is an item: a wavefront a tile, whose tokens (128 rows at most)
 // are two reads a lane; 5 us for 650 tiles.  With splits there are fewer than 2048 tiles,
-// and one workgroup does it all: it checks the sequences, takes the tiles' keys, chooses
-// the length of the runs and lists the items in order.
+// and one workgroup more chooses the length of the runs and lists the items in order.
+// Where there are few tiles it does the first part too: it checks the sequences and takes
+// the tiles' keys.
 //
 // The length of the runs.  An item's time is its steps and a fixed part of about three;
 // 512 of them run at a time (two workgroups a CU), 256 of them in two thirds of the time;
@@ -13,8 +14,6 @@
 // least time is taken.  Four chunks (1700 tokens, 8 key heads) with a window of 4096 are
 // left whole so, 456 workgroups of 65 steps: 155 us, 235 where 1536 workgroups were aimed
 // at (three rounds and a bit, and 31 us of joins).  The kernel itself takes 8.9 us there.
-#include <cstdlib>
-
 #include "sight.h"
 
 namespace mori {
@@ -53,11 +52,13 @@ __global__ __launch_bounds__(256) void sight_tiles_kernel(SightArgs a) {
   to[0] = uint4{u.lo, u.hi, u.from, u.open};
   to[1] = uint4{s.t0, s.n, s.len, s.tbl};
   to[2] = uint4{row0, tile, 1, 0x7FFFFFFFu};
-  if (a.splits && back == 0) a.seq_tile[it.b] = it.first;
 }
 
-
-static const uint32_t FEW = getenv("FEW") ? atoi(getenv("FEW")) : 64;
+// Up to so many tiles one workgroup does it all: 27.4 us for four sequences of nine tokens
+// with a window and 50.7 for two of 300 so, 28.3 and 52.3 with two kernels.  Above, the tiles
+// are taken by a kernel of their own: documents in 36 sequences 197 us so, 246 with one
+// workgroup; 3 long and 17 short ones 271 and 305.
+constexpr uint32_t FEW = 64;
 constexpr uint32_t NT = 1024, WAVES = NT / 64, MOST = 2048, K = MOST / NT;
 
 __device__ inline uint32_t scan_before(uint32_t v, uint32_t* s_wave, uint32_t* total) {
@@ -104,7 +105,6 @@ __device__ inline uint32_t write_tiles(const SightArgs& a, uint32_t* s_units, ui
     const uint32_t b = K * tid + k;
     if (b < a.b.B) {
       s_tile0[b] = at;
-      a.seq_tile[b] = at;
     }
     at += have[k];
   }
@@ -207,14 +207,103 @@ __global__ __launch_bounds__(NT) void sight_items_kernel(SightArgs a) {
     if (t < tiles) {
       reinterpret_cast<uint4*>(a.tile + t)[2] = uint4{s_row0[t], at, runs[k], run};
       for (uint32_t i = at; i < min(at + runs[k], a.items); ++i) a.list[i] = t;
+    } else if (!READY && t < a.tiles) {
+      reinterpret_cast<uint4*>(a.tile + t)[2] = uint4{0, 0, 0, 0};
     }
     at += runs[k];
   }
   for (uint32_t i = items + tid; i < a.items; i += NT) a.list[i] = NO_TILE;
-  if (tid == 0) a.seq_tile[a.b.B] = items > tiles;
+  if (tid == 0) *a.split = items > tiles;
+}
+
+// Joins the partial sums of the tiles that were split, in run order (as attend_join, but by
+// tiles, each of which has runs of its own): a wavefront takes four rows of a tile and a
+// key head, whose maxima and sums are on the way together.  Tiles of one run are left at
+// once, after one read, and all are where none was split.  Bound by the partial sums' way
+// through memory, and by the launch where few are split: 25 us for 3 long and 17 short
+// sequences with documents, 55 where each token looked for its sequence and tile first;
+// 15 and 30 us for 35000 rows of 64; 3.9 us where none is split.
+constexpr uint32_t JOIN_ROWS = 16;  // of a workgroup
+template <typename DT, int D>
+__global__ __launch_bounds__(256) void sight_join_kernel(SightArgs a) {
+  constexpr int W = D / 64, ROWS = JOIN_ROWS / 4;
+  typedef float vec __attribute__((ext_vector_type(W)));
+  if (!same(*a.split)) return;
+  const uint32_t lane = threadIdx.x & 63, wv = wave_index();
+  const uint32_t parts = a.tile_rows / JOIN_ROWS, y = blockIdx.x / parts, part = blockIdx.x - y * parts;
+  const uint32_t tile = divide(y, a.by_kv);
+  Work w{};
+  w.kv = y - tile * a.kv_heads;
+  const uint4* const at = reinterpret_cast<const uint4*>(a.tile + tile);
+  const uint4 q = at[1], z = at[2];
+  const uint32_t runs = same(z.z), first = same(z.y);
+  if (runs < 2 || (uint64_t)first + runs > a.items) return;  // more items than there is room for: not run
+  w.s.t0 = same(q.x);
+  w.s.n = same(q.y);
+  w.s.len = same(q.z);
+  w.row0 = same(z.x);
+  w.rows = min(a.tile_rows, w.s.n * a.group - w.row0);
+  const uint32_t r0 = part * JOIN_ROWS + wv * ROWS;
+  if (r0 >= w.rows) return;
+  const uint64_t step = (uint64_t)a.kv_heads * a.tile_rows, at0 = ((uint64_t)first * a.kv_heads + w.kv) * a.tile_rows + r0;
+  float2 ml[ROWS];
+  Keys keys[ROWS];
+#pragma unroll
+  for (uint32_t i = 0; i < ROWS; ++i) {
+    ml[i] = lane < runs ? a.part_ml[at0 + i + lane * step] : float2{NO_TOP, 0};
+    keys[i] = row_keys(a, w, r0 + i);
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < ROWS; ++i) {
+    if (r0 + i >= w.rows) break;
+    float top = ml[i].x;
+    for (uint32_t k = lane + 64; k < runs; k += 64) top = fmaxf(top, a.part_ml[at0 + i + k * step].x);
+    top = max_over_16(max_over_32(top));
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+    float l = 0;
+    vec o = 0;
+    for (uint32_t k0 = 0; k0 < runs; k0 += 64) {
+      const uint32_t m = min(64u, runs - k0);
+      if (k0) ml[i] = lane < m ? a.part_ml[at0 + i + (k0 + lane) * step] : float2{NO_TOP, 0};
+      const float f = ml[i].x == NO_TOP ? 0.f : __builtin_amdgcn_exp2f(ml[i].x - top);
+      l += f * ml[i].y;
+      const uint64_t skip = __ballot(ml[i].x == NO_TOP);
+      constexpr uint32_t U = 4;
+      for (uint32_t k = 0; k < m; k += U) {
+        vec v[U];
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u)  // past the last run it is read again
+          v[u] = *reinterpret_cast<const vec*>(a.part + (at0 + i + (k0 + min(k + u, m - 1)) * step) * D + W * lane);
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+          if (k + u >= m || (skip >> (k + u) & 1)) continue;  // a run without keys
+          o += v[u] * bits<float>((uint32_t)__builtin_amdgcn_readlane((int)bits<uint32_t>(f), (int)(k + u)));
+        }
+      }
+    }
+    l = sum_over_16(sum_over_32(l));
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) l += __shfl_xor(l, d);
+    const float inv = 1.f / l;
+    const RowAt row = row_at(a, w, r0 + i);
+    const bool none = keys[i].none();
+    typename DT::scalar* const out =
+        reinterpret_cast<typename DT::scalar*>(a.out.data + row.t * a.out.token + row.h * a.out.head) + W * lane;
+#pragma unroll
+    for (int d = 0; d < W; ++d) out[d] = (typename DT::scalar)(none ? 0.f : o[d] * inv);
+    if (lane == 0) store_lse(a, row, top, l, none);
+  }
 }
 
 }  // namespace
+
+void launch_sight_join(const SightArgs& a, bool f16, uint32_t dim, hipStream_t s) {
+  const dim3 grid(a.tiles * a.kv_heads * (a.tile_rows / JOIN_ROWS));
+  const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a); };
+  if (f16) dim == 64 ? launch(sight_join_kernel<F16, 64>) : launch(sight_join_kernel<F16, 128>);
+  else dim == 64 ? launch(sight_join_kernel<BF16, 64>) : launch(sight_join_kernel<BF16, 128>);
+}
 
 void launch_sight_tiles(const SightArgs& a, hipStream_t s) {
   if (a.splits && a.tiles <= FEW) {

@@ -19,7 +19,7 @@ struct Plan {
   SightArgs a;
   uint32_t dim, value;
   bool f16, step, latent;
-  uint64_t ml_at, tile_at, list_at, seq_at, bytes;  // workspace
+  uint64_t ml_at, tile_at, list_at, split_at, bytes;  // workspace
 };
 
 // Host check of what the call and its workspace size take, and the schedule.
@@ -122,8 +122,8 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
   if (sight && !p.step) {
     p.tile_at = (p.bytes + 15) / 16 * 16;
     p.list_at = p.tile_at + tiles * sizeof(SightTile);
-    p.seq_at = p.list_at + (a.splits ? items * sizeof(uint32_t) : 0);
-    p.bytes = p.seq_at + ((uint64_t)a.b.B + 1) * sizeof(uint32_t);
+    p.split_at = p.list_at + (a.splits ? items * sizeof(uint32_t) : 0);
+    p.bytes = p.split_at + sizeof(uint32_t);
     a.tiles = (uint32_t)tiles;
   }
   return true;
@@ -158,13 +158,14 @@ int attend_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, 
     else launch_attend_tile(args, p.f16, p.dim, s);
     if (a.splits) launch_attend_join(args, p.f16, p.value, s);
   };
-  if (sight) {
-    if (!p.step) {
-      a.tile = reinterpret_cast<SightTile*>(ws + p.tile_at);
-      a.list = reinterpret_cast<uint32_t*>(ws + p.list_at);
-      a.seq_tile = reinterpret_cast<uint32_t*>(ws + p.seq_at);
-      launch_sight_tiles(a, s);
-    }
+  if (sight && !p.step) {
+    a.tile = reinterpret_cast<SightTile*>(ws + p.tile_at);
+    a.list = reinterpret_cast<uint32_t*>(ws + p.list_at);
+    a.split = reinterpret_cast<uint32_t*>(ws + p.split_at);
+    launch_sight_tiles(a, s);
+    launch_attend_tile(a, p.f16, p.dim, s);
+    if (a.splits) launch_sight_join(a, p.f16, p.dim, s);
+  } else if (sight) {
     run(a);
   } else if (p.latent) {
     launch_attend_latent(a, p.f16, s);

@@ -45,7 +45,7 @@ struct SightArgs : AttendArgs {
   uint32_t unit_log;
   struct SightTile* tile;  // [tiles]
   uint32_t* list;      // [items] an item's tile; without splits it is the item itself
-  uint32_t* seq_tile;  // [B + 1] a sequence's first one; last: whether any tile is split
+  uint32_t* split;     // whether any tile has several runs
 };
 constexpr uint32_t NO_TILE = 0xFFFFFFFFu;
 
