@@ -64,6 +64,7 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
   }
   const uint64_t tiles = (uint64_t)a.b.T * a.group / a.tile_rows + a.b.B;  // no batch has more
   uint64_t most = a.b.max_kv;  // keys of a tile
+  bool windowed = false;       // a window bounds them
   if (sight) {
     if (p.latent || !std::isfinite(sight->cap) || sight->cap < 0) return false;
     if ((reinterpret_cast<uintptr_t>(sight->slopes) | reinterpret_cast<uintptr_t>(sight->first) |
@@ -85,7 +86,9 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
     a.end = sight->end;
     a.unit_log = p.step ? 7 : 6;
     a.align = p.step || a.b.bt % (512 / p.dim) ? 1 : 512 / p.dim;  // rows that a wavefront loads at once from a page
-    if (a.window && !a.end) most = std::min<uint64_t>(most, (uint64_t)a.window + a.b.max_new);
+    windowed = a.window && !a.end;
+    if (windowed)  // the tokens of a tile and a window before them
+      most = std::min<uint64_t>(most, (uint64_t)a.window + std::min(a.b.max_new, (a.tile_rows - 1) / a.group + 2));
     most += a.align;
   }
   // Items that fill the chip a few times over (measured on decode steps, chunks and mixed
@@ -110,6 +113,18 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
   // about 500 21.7 and 32.1, of 1000 39.1 and 45.2, of 2000 (up to 5000) 82.0 and 74.6; 64 of
   // 500 31.2 and 37.9, of 1000 (up to 3000) 67.3 and 60.1.
   if (sight && p.step && most <= (tiles * a.kv_heads < 256 ? 768 : 2048)) a.splits = 0;
+  // Nor are tiles of few keys: the choice of the runs and the join take 7 us.  Tiles of 128
+  // rows, 128 wide, whole and split: 20 workgroups of 500 keys 24.8 and 27.5 us, of 1000 35.6
+  // and 30.5; 64 of 700 29.4 and 32.6, of 1000 36.3 and 35.4; 128 of 1000 36.9 and 43.8, of
+  // 2000 57.3 and 53.3; 176 of 1000 36.6 and 40.4, of 1400 45.4 and 43.5; 256 of 2000 58.9 and
+  // 65.3, of 3000 80.3 and 87.5, of 4000 101 and 94.  That is for tiles alike, by a window;
+  // else one may have most of the keys: 30 sequences behind 500 keys (up to 1100) 56.1 and
+  // 64.1, but 8 of these 48.3 and 41.0; 16 with a window of 2400 and documents 78.1 and 63.2.
+  if (sight && !p.step) {
+    const uint64_t groups = tiles * a.kv_heads;
+    const bool alike = windowed && !a.first;
+    if (most <= (groups < 256 ? (alike && groups >= 128 ? 1024u : 768u) : alike ? 2560u : 1280u)) a.splits = 0;
+  }
   // runs have `least` units or more, so short contexts give fewer items than slots
   const uint64_t runs = tiles * ((most + a.unit - 1) / a.unit) / a.least;
   const uint64_t items = tiles + (a.splits ? std::min<uint64_t>(a.slots, runs + 1) : 0);
