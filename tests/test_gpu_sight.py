@@ -445,3 +445,30 @@ def test_pages_behind_four_gigabytes():
         assert torch.equal(*out) and torch.isfinite(out[0]).all()
         del pool
         torch.cuda.empty_cache()
+
+
+# n, length, kv, q heads, dim, bt: tiles of which some or all have several runs
+SPLIT = {
+    "odd_pages": ([45, 3], [1900, 1111], 2, 6, 128, 7),
+    "odd_pages_64": ([33], [2050], 3, 9, 64, 24),
+    "many_runs": ([40], [20000], 1, 2, 64, 64),  # more than a wavefront has lanes
+    "many_runs_128": ([17, 1], [17500, 300], 1, 8, 128, 16),
+    "many_tiles": ([30] * 33, [900 + 37 * i for i in range(33)], 1, 9, 128, 16),
+    "a_long_one": ([20] * 35 + [300], [20 + i for i in range(35)] + [2900], 1, 8, 128, 32),
+    "last_rows": ([27, 43], [1500, 1501], 1, 5, 64, 16),  # tiles of 7 and 87 rows
+}
+
+
+@pytest.mark.parametrize("sight", ["cap", "slopes", "window_of_2000", "long_documents", "prefix", "everything"])
+@pytest.mark.parametrize("form", SPLIT)
+def test_split_tiles(form, sight):
+    n, length, kv, H, dim, bt = SPLIT[form]
+    inst = R.instance(len(form) * 7 + len(sight), n, length, kv=kv, dim=dim, dtype=F16 if len(form + sight) % 2 else BF16, bt=bt)
+    compare(inst, queries(inst, H, 8.0 if "cap" in sight else 2.5), dim ** -0.5, **SIGHTS[sight](inst, H))
+
+
+@pytest.mark.parametrize("window", [640, 730, 770, 900, 1030, 1300])
+def test_windows_around_the_choice_to_split(window):
+    for n, kv in ((40, 2), (600, 4)):  # few workgroups, and over 128
+        inst = R.instance(window + n, [n] * 3, [window + n, 2500, n], kv=kv, dim=64, dtype=BF16, bt=16)
+        compare(inst, queries(inst, 2 * kv), 0.125, window=window, slopes=slopes_of(2 * kv))
