@@ -120,10 +120,15 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
   // 65.3, of 3000 80.3 and 87.5, of 4000 101 and 94.  That is for tiles alike, by a window;
   // else one may have most of the keys: 30 sequences behind 500 keys (up to 1100) 56.1 and
   // 64.1, but 8 of these 48.3 and 41.0; 16 with a window of 2400 and documents 78.1 and 63.2.
+  // A chip of 512 at a time that is about full is left so for longer: 440 of 4000 keys 131
+  // and 137, 512 134 and 140, 648 145 and 152; of 5500 and capped 440 224 and 217, 512 225 and
+  // 221, 648 209 and 214; but 388 of 4000 120 and 113, 752 capped 275 and 268.
   if (sight && !p.step) {
     const uint64_t groups = tiles * a.kv_heads;
     const bool alike = windowed && !a.first;
-    if (most <= (groups < 256 ? (alike && groups >= 128 ? 1024u : 768u) : alike ? 2560u : 1280u)) a.splits = 0;
+    uint64_t whole = groups < 256 ? 768 : 1280;
+    if (alike && groups >= 128) whole = groups < 256 ? 1024 : groups < 400 || groups > 640 ? 2560 : 5120;
+    if (most <= whole) a.splits = 0;
   }
   // runs have `least` units or more, so short contexts give fewer items than slots
   const uint64_t runs = tiles * ((most + a.unit - 1) / a.unit) / a.least;
