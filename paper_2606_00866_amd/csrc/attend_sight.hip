@@ -11,9 +11,9 @@
 // splitting at all costs the second kernel, about two steps, and every 88 items of split
 // tiles one step to write and join 64 KiB of partial sums each.  32 lengths from the
 // shortest allowed to 15 times that are tried, two a wavefront, and the one with the
-// least time is taken.  Four chunks (1700 tokens, 8 key heads) with a window of 4096 are
-// left whole so, 456 workgroups of 65 steps: 155 us, 235 where 1536 workgroups were aimed
-// at (three rounds and a bit, and 31 us of joins).  The kernel itself takes 8.9 us there.
+// least time is taken.  456 workgroups of 65 steps come out whole so, 155 us; 235 where 1536
+// workgroups were aimed at (three rounds and a bit, and 31 us of joins).  The kernel takes
+// 5 to 7 us, 9 where it makes the tiles of four sequences of 430 tokens too.
 #include "sight.h"
 
 namespace mori {
