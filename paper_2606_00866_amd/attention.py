@@ -431,8 +431,9 @@ def _attend_desc(geom, q: torch.Tensor, scale: float | None) -> M.mori_attend:
 
 def _sight(geom, batch: TokenBatch, heads: int, cap, slopes, window, first, end) -> M.mori_sight:
     _need(geom.planes == 2, "kv_attend: caps, slopes, windows and ranges are for K/V pools")
-    _need(cap is None or 0 < cap < float("inf"), "kv_attend: cap is a finite number above 0")
-    _need(window is None or 0 < window < 1 << 32, "kv_attend: window is a number of positions, its own among them")
+    _need(cap is None or 2.0 ** -126 <= cap < float("inf"), "kv_attend: cap is a finite number above 0, in 32 bits too")
+    _need(window is None or 0 < window < 1 << 32 and int(window) == window,
+          "kv_attend: window is a number of positions, its own among them")
     for name, x, dtype, n in (("slopes", slopes, torch.float32, heads), ("first", first, torch.int32, batch.num_tokens),
                               ("end", end, torch.int32, batch.num_tokens)):
         if x is not None and not (x.dtype == dtype and x.shape == (n,) and x.is_contiguous() and x.device == batch.device):

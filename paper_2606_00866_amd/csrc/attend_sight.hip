@@ -77,37 +77,25 @@ __device__ inline uint32_t scan_before(uint32_t v, uint32_t* s_wave, uint32_t* t
   return before;
 }
 
-// The tiles by this workgroup, their units and first rows in LDS; their number.
+// The tiles by this workgroup (FEW at most), their units and first rows in LDS; their number.
 __device__ inline uint32_t write_tiles(const SightArgs& a, uint32_t* s_units, uint32_t* s_row0, uint32_t* s_wave) {
-  __shared__ uint4 s_seq[MOST];                    // t0, n, len, tbl
-  __shared__ uint32_t s_tile0[MOST];
+  __shared__ uint4 s_seq[FEW];  // t0, n, len, tbl
+  __shared__ uint32_t s_tile0[FEW];
   const uint32_t tid = threadIdx.x, lane = tid & 63, wv = wave_index();
-  // sequences: there are fewer of them than tiles may be
-  uint32_t mine = 0, err = 0, have[K];
-#pragma unroll
-  for (uint32_t k = 0; k < K; ++k) {
-    const uint32_t b = K * tid + k;
-    have[k] = 0;
-    if (b >= a.b.B) continue;
-    const Seq s = checked_sequence(a.b, read_sequence(a.b, b));
-    err |= s.error;
-    s_seq[b] = uint4{s.t0, s.n, s.len, s.tbl};  // len 0 where something is wrong: padding
-    have[k] = (s.n * a.group + a.tile_rows - 1) / a.tile_rows;
-    mine += have[k];
+  // sequences: there are no more of them than tiles may be
+  uint32_t have = 0, err = 0;
+  if (tid < a.b.B) {
+    const Seq q = checked_sequence(a.b, read_sequence(a.b, tid));
+    err = q.error;
+    s_seq[tid] = uint4{q.t0, q.n, q.len, q.tbl};  // len 0 where something is wrong: padding
+    have = (q.n * a.group + a.tile_rows - 1) / a.tile_rows;
   }
   err = wave::all_or(err);
   if (lane == 0) report(a.b, err);
   uint32_t tiles;
-  uint32_t at = scan_before(mine, s_wave, &tiles);
+  const uint32_t at = scan_before(have, s_wave, &tiles);
   tiles = min(tiles, a.tiles);  // more only where sequences overlap
-#pragma unroll
-  for (uint32_t k = 0; k < K; ++k) {
-    const uint32_t b = K * tid + k;
-    if (b < a.b.B) {
-      s_tile0[b] = at;
-    }
-    at += have[k];
-  }
+  if (tid < a.b.B) s_tile0[tid] = at;
   __syncthreads();
   // tiles, a wavefront each
   for (uint32_t tile = wv; tile < tiles; tile += WAVES) {

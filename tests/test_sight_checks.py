@@ -135,3 +135,32 @@ def test_definition():
             want = torch.einsum("htl,lhd->thd", torch.softmax(s, -1).nan_to_num(0), v.repeat_interleave(2, 1))
             assert np.allclose(out[t], want, atol=1e-12) and np.allclose(lse[t], s.logsumexp(-1).t(), atol=1e-12)
         assert (bound > 0).all() and (bound < 0.3).all()
+
+
+@pytest.mark.parametrize("bad", [dict(cap=1e-50), dict(cap=2.0 ** -150), dict(window=0.5), dict(window=4.5),
+                                 dict(window=float("nan"))], ids=str)
+def test_numbers_that_would_be_rounded_away_are_refused(calls, bad):
+    """As 32 bits, or cut to an integer, they would say nothing, or something else."""
+    with pytest.raises(MoriError) as e:
+        attend(**bad)
+    assert e.value.code == M.MORI_EINVAL and not calls
+
+
+def test_a_workspace_for_no_sight_holds_all():
+    """Whether tiles are split depends on the window and the ranges too."""
+    g = np.random.default_rng(1)
+    for _ in range(3000):
+        B, kv = int(g.integers(1, 80)), int(2 ** g.integers(0, 4))
+        T = int(B * 2 ** g.uniform(0, 11))
+        tokens = dict(num_seqs=B, num_tokens=T, max_new=int(g.integers(-(-T // B), T + 1)), num_programs=B,
+                      max_kv=int(2 ** g.uniform(0, 16)))
+        tokens["max_new"] = min(tokens["max_new"], tokens["max_kv"])
+        a = desc(q_heads=kv * int(g.integers(1, 9)), kv_heads=kv)
+        pool_ = dict(row_bytes=128 * kv)
+        rc, most = size(dict(), tokens, pool_, a)
+        if rc != M.MORI_OK:
+            continue
+        for more in (dict(), dict(first=4096), dict(end=4096), dict(cap=3.0), dict(slopes=4096)):
+            for window in (0, 1, int(2 ** g.uniform(0, 13)), 700, 2000, 5000):
+                rc, n = size(dict(window=window, **more), tokens, pool_, a)
+                assert rc == M.MORI_OK and n <= most, (tokens, kv, more, window, n, most)
