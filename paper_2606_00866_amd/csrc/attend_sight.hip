@@ -7,13 +7,20 @@
 // the tiles' keys.
 //
 // The length of the runs.  An item's time is its steps and a fixed part of about three;
-// 512 of them run at a time (two workgroups a CU), 256 of them in two thirds of the time;
-// splitting at all costs the second kernel, about two steps, and every 88 items of split
-// tiles one step to write and join 64 KiB of partial sums each.  32 lengths from the
-// shortest allowed to 15 times that are tried, two a wavefront, and the one with the
-// least time is taken.  456 workgroups of 65 steps come out whole so, 155 us; 235 where 1536
-// workgroups were aimed at (three rounds and a bit, and 31 us of joins).  The kernel takes
-// 5 to 7 us, 9 where it makes the tiles of four sequences of 430 tokens too.
+// 512 of them run at a time (two workgroups a CU), 256 of them in two thirds of the time.
+// Rounds of the longest are one bound of the whole, all items' steps shared out and half
+// of an item, for the last to start, another; the lesser counts, so prompts, whose tiles
+// see half of their keys at the mean, are not taken for as many long ones (3000 tokens in
+// each of three sequences, capped, 302 us by the first alone, 244 so; 3 of 3219 and 17
+// that decode 363 and 288; a prompt of 4000 236 and 206; but documents of unlike lengths
+// in 36 x 650 tokens 168 and 177, short ones in 3 x 3000 85 and 95; with three quarters of
+// an item or a whole one the first three stay as they were).  Splitting at all costs the join, about two steps, and every 88 items
+// one step to write and join 64 KiB of partial sums each (counted for split tiles' items
+// only, too much was split: 282 us for the first of these).  32 lengths from the shortest
+// allowed to 15 times that are tried, two a wavefront, and the one with the least time is
+// taken.  456 workgroups of 65 steps come out whole so, 155 us; 235 where 1536 workgroups
+// were aimed at (three rounds and a bit, and 31 us of joins).  The kernel takes 5 to 7 us,
+// 9 where it makes the tiles of four sequences of 430 tokens too.
 #include "sight.h"
 
 namespace mori {
@@ -75,6 +82,17 @@ __device__ inline uint32_t scan_before(uint32_t v, uint32_t* s_wave, uint32_t* t
   *total = all;
   __syncthreads();
   return before;
+}
+
+__device__ inline uint32_t most_of(uint32_t v, uint32_t* s_wave) {
+  v = wave_max(v);
+  if ((threadIdx.x & 63) == 0) s_wave[threadIdx.x >> 6] = v;
+  __syncthreads();
+  uint32_t most = 0;
+#pragma unroll
+  for (uint32_t i = 0; i < WAVES; ++i) most = max(most, s_wave[i]);
+  __syncthreads();
+  return most;
 }
 
 // The tiles by this workgroup (FEW at most), their units and first rows in LDS; their number.
@@ -157,6 +175,7 @@ __global__ __launch_bounds__(NT) void sight_items_kernel(SightArgs a) {
   }
   scan_before(units[0] + units[1], s_wave, &total);
   const uint32_t least = max(a.least, (total + a.slots - 1) / a.slots);
+  const uint32_t longest = most_of(max(units[0], units[1]), s_wave);
   float best = 3.0e38f;
   uint32_t run = least;
   for (uint32_t j = 2 * wv; j < 2 * wv + 2; ++j) {
@@ -164,9 +183,12 @@ __global__ __launch_bounds__(NT) void sight_items_kernel(SightArgs a) {
     uint32_t n = 0;
     for (uint32_t t = lane; t < tiles; t += 64) n += (s_units[t] + c - 1) / c;
     n = wave::sum(n);
-    const uint32_t groups = n * a.kv_heads, rest = groups % 512;
-    const float rounds = (float)(groups / 512) + (rest == 0 ? 0.f : rest <= 256 ? 0.65f : 1.f);
-    const float cost = rounds * (float)(c + 3) + (n > tiles ? 2.f + (float)groups / 88.f : 0.f);
+    const uint32_t groups = n * a.kv_heads, rest = groups % 512, steps = min(c, longest) + 3;
+    // by their number, and by their steps with half of one as the last ones' wait
+    const float alike = (float)(groups / 512) + (rest == 0 ? 0.f : rest <= 256 ? 0.65f : 1.f);
+    const float unlike = fmaxf((float)(total + 3 * n) / (float)steps * (float)a.kv_heads / 512.f + 0.5f, 1.f);
+    const float rounds = groups > 512 ? fminf(alike, unlike) : alike;
+    const float cost = rounds * (float)steps + (n > tiles ? 2.f + (float)groups / 88.f : 0.f);
     if (cost < best) {
       best = cost;
       run = c;
