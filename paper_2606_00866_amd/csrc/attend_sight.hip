@@ -10,17 +10,18 @@
 // 512 of them run at a time (two workgroups a CU), 256 of them in two thirds of the time.
 // Rounds of the longest are one bound of the whole, all items' steps shared out and half
 // of an item, for the last to start, another; the lesser counts, so prompts, whose tiles
-// see half of their keys at the mean, are not taken for as many long ones (3000 tokens in
-// each of three sequences, capped, 302 us by the first alone, 244 so; 3 of 3219 and 17
-// that decode 363 and 288; a prompt of 4000 236 and 206; but documents of unlike lengths
-// in 36 x 650 tokens 168 and 177, short ones in 3 x 3000 85 and 95; with three quarters of
-// an item or a whole one the first three stay as they were).  Splitting at all costs the join, about two steps, and every 88 items
-// one step to write and join 64 KiB of partial sums each (counted for split tiles' items
-// only, too much was split: 282 us for the first of these).  32 lengths from the shortest
-// allowed to 15 times that are tried, two a wavefront, and the one with the least time is
-// taken.  456 workgroups of 65 steps come out whole so, 155 us; 235 where 1536 workgroups
-// were aimed at (three rounds and a bit, and 31 us of joins).  The kernel takes 5 to 7 us,
-// 9 where it makes the tiles of four sequences of 430 tokens too.
+// see half of their keys at the mean, are not taken for as many long ones: 3000 tokens in
+// each of three sequences, capped, 302 us by the first bound alone, 244 so; 3 of 3219 and
+// 17 that decode 363 and 288; a prompt of 4000 236 and 206; but documents of unlike lengths
+// in 36 x 650 tokens 168 and 177, short ones in 3 x 3000 85 and 95.  (With three quarters of
+// an item, or a whole one, the first and the third stay at 302 and 236.)  Splitting at all
+// costs the join, about two steps, and every 88 items one step to write and join 64 KiB of
+// partial sums each (counting split tiles' items only splits too much: 282 us for the
+// first of these).  32 lengths from the shortest allowed to 15 times that are tried, two a
+// wavefront, and the one with the least time is taken.  456 workgroups of 65 steps come out
+// whole so, 155 us; 235 where 1536 workgroups were aimed at (three rounds and a bit, and
+// 31 us of joins).  The kernel takes 5 to 7 us, 9 where it makes the tiles of four
+// sequences of 430 tokens too.
 #include "sight.h"
 
 namespace mori {
