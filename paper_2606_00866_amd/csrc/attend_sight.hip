@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256) void sight_tiles_kernel(SightArgs a) {
 // are taken by a kernel of their own: documents in 36 sequences 197 us so, 246 with one
 // workgroup; 3 long and 17 short ones 271 and 305.
 constexpr uint32_t FEW = 64;
-constexpr uint32_t NT = 1024, WAVES = NT / 64, MOST = 2048, K = MOST / NT;
+constexpr uint32_t NT = 1024, WAVES = NT / 64, MOST = 2048, K = MOST / NT, KINDS = 8;
 
 __device__ inline uint32_t scan_before(uint32_t v, uint32_t* s_wave, uint32_t* total) {
   const uint32_t lane = threadIdx.x & 63, wv = threadIdx.x >> 6, in = wave::incl_add(v);
@@ -147,6 +147,7 @@ __device__ inline uint32_t write_tiles(const SightArgs& a, uint32_t* s_units, ui
 template <bool READY>
 __global__ __launch_bounds__(NT) void sight_items_kernel(SightArgs a) {
   __shared__ uint32_t s_units[MOST], s_row0[MOST], s_wave[WAVES], s_run[WAVES];
+  __shared__ uint32_t s_kind[KINDS * WAVES];
   __shared__ float s_cost[WAVES];
   const uint32_t tid = threadIdx.x, lane = tid & 63, wv = wave_index();
   uint32_t tiles;
@@ -207,21 +208,42 @@ __global__ __launch_bounds__(NT) void sight_items_kernel(SightArgs a) {
       best = s_cost[i];
       run = s_run[i];
     }
-  // items
-  uint32_t runs[K], items;
+  // items, those of longer tiles first: by eighths of the longest, else in order
+  uint32_t runs[K], kind[K], at[K]{};
 #pragma unroll
-  for (uint32_t k = 0; k < K; ++k) runs[k] = (units[k] + run - 1) / run;
-  uint32_t at = scan_before(runs[0] + runs[1], s_wave, &items);
+  for (uint32_t k = 0; k < K; ++k) {
+    runs[k] = (units[k] + run - 1) / run;
+    kind[k] = (longest - units[k]) * KINDS / max(longest, 1u);
+  }
+#pragma unroll
+  for (uint32_t c = 0; c < KINDS; ++c) {
+    uint32_t mine = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < K; ++k) mine += kind[k] == c ? runs[k] : 0;
+    const uint32_t in = wave::incl_add(mine);
+    if (lane == 63) s_kind[c * WAVES + wv] = in;
+    uint32_t before = in - mine;
+#pragma unroll
+    for (uint32_t k = 0; k < K; ++k) {
+      if (kind[k] != c) continue;
+      at[k] = before;
+      before += runs[k];
+    }
+  }
+  __syncthreads();
+  static_assert(KINDS * WAVES == 128, "two a lane");
+  const uint32_t x = s_kind[2 * lane], y = s_kind[2 * lane + 1], in = wave::incl_add(x + y), items = wave::lane63(in);
 #pragma unroll
   for (uint32_t k = 0; k < K; ++k) {
     const uint32_t t = K * tid + k;
+    // no runs: of no kind
+    at[k] += (uint32_t)__shfl((int)(wv & 1 ? in - y : in - y - x), (int)(min(kind[k], KINDS - 1) * WAVES + wv) / 2);
     if (t < tiles) {
-      reinterpret_cast<uint4*>(a.tile + t)[2] = uint4{s_row0[t], at, runs[k], run};
-      for (uint32_t i = at; i < min(at + runs[k], a.items); ++i) a.list[i] = t;
+      reinterpret_cast<uint4*>(a.tile + t)[2] = uint4{s_row0[t], at[k], runs[k], run};
+      for (uint32_t i = at[k]; i < min(at[k] + runs[k], a.items); ++i) a.list[i] = t;
     } else if (!READY && t < a.tiles) {
       reinterpret_cast<uint4*>(a.tile + t)[2] = uint4{0, 0, 0, 0};
     }
-    at += runs[k];
   }
   for (uint32_t i = items + tid; i < a.items; i += NT) a.list[i] = NO_TILE;
   if (tid == 0) *a.split = items > tiles;
