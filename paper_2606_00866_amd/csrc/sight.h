@@ -44,7 +44,7 @@ struct SightArgs : AttendArgs {
   uint32_t align;      // a tile's keys are taken from a multiple of this power of two on
   uint32_t unit_log;
   struct SightTile* tile;  // [tiles]
-  uint32_t* list;      // [items] an item's tile; without splits it is the item itself
+  uint32_t* list;      // [items] an item's tile; no array: it is the item itself
   uint32_t* split;     // whether any tile has several runs
 };
 constexpr uint32_t NO_TILE = 0xFFFFFFFFu;
@@ -198,7 +198,7 @@ __device__ inline Work tile_work(const SightArgs& a, uint32_t block) {
   Work w{};
   w.item = divide(block, a.by_kv);
   w.kv = block - w.item * a.kv_heads;
-  const uint32_t tile = a.splits ? same(a.list[w.item]) : w.item;
+  const uint32_t tile = a.list ? same(a.list[w.item]) : w.item;
   if (tile >= a.tiles) return w;
   const uint4* const at = reinterpret_cast<const uint4*>(a.tile + tile);
   const uint4 x = at[0], y = at[1], z = at[2];

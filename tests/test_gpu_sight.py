@@ -472,3 +472,25 @@ def test_windows_around_the_choice_to_split(window):
     for n, kv in ((40, 2), (600, 4)):  # few workgroups, and over 128
         inst = R.instance(window + n, [n] * 3, [window + n, 2500, n], kv=kv, dim=64, dtype=BF16, bt=16)
         compare(inst, queries(inst, 2 * kv), 0.125, window=window, slopes=slopes_of(2 * kv))
+
+
+@pytest.mark.parametrize("sight", ["cap", "slopes", "window", "documents", "long_documents", "prefix", "everything"])
+@pytest.mark.parametrize("seqs,kv,dim", [(70, 32, 64), (9, 128, 64), (40, 32, 128), (50, 64, 64)])
+def test_whole_tiles_in_the_order_of_their_length(seqs, kv, dim, sight):
+    """More workgroups than are split, of a few tiles; the longest run first."""
+    g = np.random.default_rng(seqs)
+    n = g.integers(0, 18, seqs).tolist()
+    n[seqs // 2] = 17  # 34 rows or more
+    length = [a + int(b) for a, b in zip(n, g.integers(0, 230, seqs))]
+    length[0] = n[0]
+    inst = R.instance(seqs + len(sight), n, length, kv=kv, dim=dim, dtype=F16 if len(sight) % 2 else BF16, bt=16)
+    H = kv * (4 if kv < 64 else 2)
+    assert (sum(n) * (H // kv) // 128 + seqs) * kv >= 1024
+    compare(inst, queries(inst, H, 8.0 if "cap" in sight else 2.5), dim ** -0.5, **SIGHTS[sight](inst, H))
+
+
+def test_whole_tiles_of_one_prompt():
+    """Documents in a prompt whose tiles fill the chip many times."""
+    inst = R.instance(5, [700], [760], kv=32, dim=64, dtype=BF16, bt=16)
+    q = queries(inst, 64 * 6)
+    compare(inst, q, 0.125, first=documents(inst, 90), slopes=slopes_of(64 * 6))
