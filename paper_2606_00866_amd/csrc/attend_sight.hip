@@ -12,15 +12,15 @@
 //
 // The length of the runs.  An item's time is its steps and a fixed part of about three;
 // 512 of them run at a time (two workgroups a CU), 256 of them in two thirds of the time.
-// Rounds of the longest are one bound of the whole, all items' steps shared out and half
-// of an item, for the last to start, another; the lesser counts, so prompts, whose tiles
-// see half of their keys at the mean, are not taken for as many long ones: 3000 tokens in
-// each of three sequences, capped, 302 us by the first bound alone, 244 so; 3 of 3219 and
-// 17 that decode 363 and 288; a prompt of 4000 236 and 206; but documents of unlike lengths
-// in 36 x 650 tokens 168 and 177, short ones in 3 x 3000 85 and 95.  (With three quarters of
-// an item, or a whole one, the first and the third stay at 302 and 236.)  Splitting at all
-// costs the join, about two steps, and every 88 items one step to write and join 64 KiB of
-// partial sums each (counting split tiles' items only splits too much: 282 us for the
+// Rounds of the longest are one bound of the whole, all items' steps shared out and a fifth
+// of an item, for the last to end, another; the lesser counts, so prompts, whose tiles see
+// half of their keys at the mean, are not taken for as many long ones.  Capped, 3000 tokens
+// in each of three sequences 302 us by the first bound alone and in the tiles' order; longest
+// first 239 so, 240 with half of an item, 311 with three quarters; 50 sequences of 150
+// behind 3000 468, 534 and 532; 36 of 650 with documents of 1500 222, 249 and 280; but 8 of
+// 500 with these 114, 108 and 111.  Splitting at all costs the join, about two steps, and
+// every 88 items one step to write and join 64 KiB of partial sums each (counting split
+// tiles' items only splits too much: 282 us, in the tiles' order, where 244 are taken, for the
 // first of these).  32 lengths from the shortest allowed to 15 times that are tried, two a
 // wavefront, and the one with the least time is taken.  456 workgroups of 65 steps come out
 // whole so, 155 us; 235 where 1536 workgroups were aimed at (three rounds and a bit, and
@@ -190,9 +190,9 @@ __global__ __launch_bounds__(NT) void sight_items_kernel(SightArgs a) {
     for (uint32_t t = lane; t < tiles; t += 64) n += (s_units[t] + c - 1) / c;
     n = wave::sum(n);
     const uint32_t groups = n * a.kv_heads, rest = groups % 512, steps = min(c, longest) + 3;
-    // by their number, and by their steps with half of one as the last ones' wait
+    // by their number, and by their steps and what the last ones take longer
     const float alike = (float)(groups / 512) + (rest == 0 ? 0.f : rest <= 256 ? 0.65f : 1.f);
-    const float unlike = fmaxf((float)(total + 3 * n) / (float)steps * (float)a.kv_heads / 512.f + 0.5f, 1.f);
+    const float unlike = fmaxf((float)(total + 3 * n) / (float)steps * (float)a.kv_heads / 512.f + 0.2f, 1.f);
     const float rounds = groups > 512 ? fminf(alike, unlike) : alike;
     const float cost = rounds * (float)steps + (n > tiles ? 2.f + (float)groups / 88.f : 0.f);
     if (cost < best) {
