@@ -130,14 +130,18 @@ class TokenBatch:
     @classmethod
     def of(cls, tier_pool, programs, new_tokens, kv_len) -> "TokenBatch":
         """A batch of a ``TierPool``'s programs from host numbers: new_tokens[i] new
-        tokens of programs[i], which then holds kv_len[i]."""
+        tokens of programs[i], which then holds kv_len[i].  Where that is more than the
+        programs are known to hold, and they may have grown on the device, their sizes
+        are read first, which waits for the current stream."""
         n, length = np.asarray(new_tokens, np.int64), np.asarray(kv_len, np.int64)
         prog = np.asarray(programs, np.int64)
         _need(n.ndim == 1 and n.shape == length.shape == prog.shape, "TokenBatch: one number per sequence")
         _need(bool((n >= 0).all() and (length >= 0).all() and (prog >= 0).all() and (prog < tier_pool.P).all()),
               "TokenBatch: numbers out of range")
-        _need(bool((length <= tier_pool.nblk[prog] * tier_pool.geom.block_tokens).all()),
-              "TokenBatch: more tokens than the program's blocks hold")
+        fits = lambda: bool((length <= tier_pool.nblk[prog] * tier_pool.geom.block_tokens).all())
+        if not fits() and tier_pool.tbl.numel() > tier_pool.nblk.sum():  # they may have grown since
+            tier_pool.read_sizes()
+        _need(fits(), "TokenBatch: more tokens than the program's blocks hold")
         dev = lambda a: torch.from_numpy(a.astype(np.int32)).to(tier_pool.device)
         off = np.concatenate([[0], np.cumsum(n)])
         return cls(tier_pool.geom, tier_pool.tbl_off, tier_pool.tbl, dev(off), dev(length), dev(prog),
@@ -251,7 +255,6 @@ class TokenGrowth:
            num_tokens: int, max_new: int, max_kv: int) -> "TokenGrowth":
         """Of a ``TierPool``'s programs, in place; those on the GPU grow.  Make room in the
         table first (``TierPool.reserve``), and run it when a step's swaps have ended."""
-        tier_pool.grows = True  # its sizes are read back before the next swaps
         growth = cls(tier_pool.geom, tier_pool.tbl_off, tier_pool.tbl, tier_pool.free_map, held, new_tokens, program,
                      tier=tier_pool.tier, num_tokens=num_tokens, max_new=max_new, max_kv=max_kv)
         growth._tier_pool = tier_pool

@@ -163,7 +163,6 @@ class TierPool:
         check(M.mori_register(self.ctx, self.arena.ptr, self.arena.nbytes), "mori_register(arena)")
         self._keep = []
         self.plan = None
-        self.grows = False  # programs' sizes change on the device
 
     def reserve(self, entries: int) -> None:
         """Room for `entries` table entries in all, for programs that grow.  The table moves:
@@ -175,10 +174,12 @@ class TierPool:
         self.tbl_len = max(self.tbl_len, entries)
 
     def read_sizes(self) -> None:
-        """The programs' blocks as the device has them now (waits for the current stream)."""
+        """The programs' blocks (`nblk`) as the device has them now (waits for the current
+        stream).  Where programs grow on the device, `nblk` is else as of the last plan."""
         self.nblk = np.diff(self.tbl_off.cpu().numpy().view(np.uint32).astype(np.int64))
 
     # ---- host extents -------------------------------------------------------
+    # They go by the sizes of the last plan, which are those that its swaps move.
     def program_bytes(self, p: int) -> int:
         return int(self.nblk[p]) * self.geom.block_bytes
 
@@ -212,8 +213,13 @@ class TierPool:
         return M.mori_rank_partition(self.ctx, prog, budget, _stream(stream))
 
     def plan_wait(self):
+        """Waits for the plan; the programs' sizes are then those that it placed, whatever
+        they grew by on the device before it."""
         rc, p = M.mori_plan_wait(self.ctx)
         self.plan = p
+        if rc == M.MORI_OK and self.P:
+            by_rank = np.diff(np.ctypeslib.as_array(p.prefix, shape=(self.P,)), prepend=np.uint64(0))
+            self.nblk[np.ctypeslib.as_array(p.order, shape=(self.P,))] = by_rank // np.uint64(self.geom.block_bytes)
         return rc, p
 
     def plan_arrays(self, p=None) -> dict:
@@ -259,8 +265,6 @@ class TierPool:
         rc, p = self.plan_wait()
         if rc != M.MORI_OK:
             raise MoriError("mori_plan_wait", rc, p.device_error)
-        if self.grows:
-            self.read_sizes()
         self.place_host_buffers()
         check(self.swap_out(mode, s_out), "mori_kv_swap_out")
         check(self.swap_in(mode, s_in if s_in is not None else s_out), "mori_kv_swap_in")
