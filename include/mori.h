@@ -463,8 +463,9 @@ typedef struct {
  * An old block of a new token without a page (or with one past the pool) gives slot -1
  * and MORI_DEV_NOT_RESIDENT (MORI_DEV_PAGE_RANGE); the rest stands.
  *
- * Swaps of a plan read its tables and may still be reading pages that it has marked
- * free: grow once both swaps are enqueued, ordered behind MORI_Q_OUT_EVENT. */
+ * A plan's swap-out may still be reading pages that the plan has marked free: grow once
+ * it is enqueued, ordered behind MORI_Q_OUT_EVENT.  Swaps move what the plan placed, so a
+ * program that is on its way in may grow. */
 typedef struct {
   uint32_t num_seqs;          /* B, 1..MORI_MAX_PROGRAMS */
   uint32_t num_tokens;        /* T, places of slots and positions */

@@ -117,7 +117,6 @@ struct mori_ctx {
   bool have_plan = false, out_enqueued = false, in_enqueued = false;
   bool out_recorded = false, in_recorded = false, addr_pending[2] = {false, false};
   uint32_t P = 0;
-  const uint32_t* tbl_off = nullptr;
   uint32_t tbl_len = 0;
   int last_hip_error = 0;
   uint32_t last_mode = 0;
@@ -433,7 +432,6 @@ extern "C" int mori_rank_partition(mori_ctx* ctx, const mori_programs* pr, const
   ctx->have_plan = true;
   ctx->out_enqueued = ctx->in_enqueued = false;
   ctx->P = P;
-  ctx->tbl_off = pr->tbl_off;
   ctx->tbl_len = pr->tbl_len;
   return MORI_OK;
 }
@@ -602,7 +600,6 @@ int translate(mori_ctx* c, int d, const uint64_t* addr, hipStream_t s) {
   t.LC = c->LC;
   t.prog = c->dev<uint32_t>(d ? c->L.in_prog : c->L.out_prog);
   t.dir_in = d;
-  t.tbl_off = c->tbl_off;
   t.block_bytes = c->block_bytes;
   t.addr_in = c->addr_pinned_dev + (size_t)d * c->max_programs;
   t.addr_out = c->addr_dev[d];

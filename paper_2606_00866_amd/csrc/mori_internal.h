@@ -124,7 +124,6 @@ struct TranslateArgs {
   uint32_t LC;
   const uint32_t* prog;     // out_prog or in_prog (count n_out / n_in)
   int dir_in;               // 0 out, 1 in
-  const uint32_t* tbl_off;
   uint64_t block_bytes;
   const uint64_t* addr_in;  // [P] caller addresses, in pinned host memory
   uint64_t* addr_out;       // [P] translated device addresses

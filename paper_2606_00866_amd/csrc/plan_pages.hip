@@ -283,6 +283,7 @@ __global__ __launch_bounds__(WG) void clear_owner_kernel(PlanArgs a) {
 // Resolves every moving program's caller address through the registered
 // ranges; a buffer that is not 16-B aligned or not wholly inside one range
 // sets MORI_DEV_HOST_ADDR and the swap kernels then do nothing.
+// A program's size is what the plan placed: its tables may have grown since.
 // It also leaves the direction's unit ranges for the swap kernels.
 __global__ __launch_bounds__(WG) void translate_kernel(TranslateArgs t) {
   const bool first = blockIdx.x == 0 && threadIdx.x == 0;
@@ -304,7 +305,7 @@ __global__ __launch_bounds__(WG) void translate_kernel(TranslateArgs t) {
   uint32_t err = 0;
   for (uint32_t j = blockIdx.x * WG + threadIdx.x; j < n; j += gridDim.x * WG) {
     const uint32_t p = t.prog[j];
-    const uint64_t bytes = (uint64_t)(t.tbl_off[p + 1] - t.tbl_off[p]) * t.block_bytes;
+    const uint64_t bytes = (uint64_t)(t.pg_base[j + 1] - t.pg_base[j]) * t.block_bytes;
     const uint64_t h = t.addr_in[p];
     uint64_t dev = 0;
     bool ok = (h & 15ull) == 0 && h != 0;

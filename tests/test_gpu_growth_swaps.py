@@ -112,3 +112,47 @@ def test_batches_from_host_numbers_after_a_growth():
         assert torch.equal(rows[0, 1, g.slots], k)
     finally:
         tp.close()
+
+
+def streams_apart():
+    """Two that do not share a hardware queue: one runs while the other is busy."""
+    busy = torch.cuda.Stream()
+    for _ in range(16):
+        other = torch.cuda.Stream()
+        with torch.cuda.stream(busy):
+            torch.cuda._sleep(20_000_000)
+            slept = busy.record_event()
+        other.record_event().synchronize()
+        if not slept.query():
+            return other, busy
+    pytest.skip("every stream waits for the others here")
+
+
+def test_growth_behind_the_swap_out_while_the_swap_in_waits():
+    """Swaps move what the plan placed: a program that is on its way in may grow behind the
+    swap-out, its host buffer being no larger than it was."""
+    tp = tier_pool([3, 2], 40, 20, 3)  # the arena ends with program 0's buffer
+    s_out, s_in = streams_apart()
+    held = torch.tensor([40, 20], dtype=torch.int32, device="cuda")
+    far, near = torch.tensor([0.9, 0.1], device="cuda"), torch.tensor([0.1, 0.2], device="cuda")
+    try:
+        tp.pool.random_(0, 256)
+        want = [bytes_of(tp, p) for p in (0, 1)]
+        torch.cuda.synchronize()
+        assert move(tp, far, 2, s_out, s_in).n_out == 1
+        tp.synchronize()
+        g = growth(tp, held, [70], [0], False)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s_in):
+            torch.cuda._sleep(200_000_000)
+            slept = s_in.record_event()
+        assert move(tp, near, 20, s_out, s_in).n_in == 1
+        g.run(stream=s_out)
+        s_out.synchronize()
+        assert not slept.query()  # the growth came first
+        tp.synchronize()
+        g.batch.check()
+        assert np.diff(tp.tbl_off.cpu().numpy()).tolist() == [7, 2]
+        assert torch.equal(bytes_of(tp, 0)[:, :3], want[0]) and torch.equal(bytes_of(tp, 1), want[1])
+    finally:
+        tp.close()
