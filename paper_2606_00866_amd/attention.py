@@ -247,7 +247,7 @@ class TokenGrowth:
         # other streams' calls keep all of it from reuse
         self.batch._keep += (tbl_off, tbl, free_map, held, new_tokens, tier, *to[2:], self.slots, self.positions,
                              self._workspace)
-        self._tier_pool, self._tbl = None, tbl
+        self._tables = (tbl, to[1])
         self._written = (*to, self.batch.seq_off, self.batch.kv_len, self.slots, self.positions)
 
     @classmethod
@@ -255,15 +255,13 @@ class TokenGrowth:
            num_tokens: int, max_new: int, max_kv: int) -> "TokenGrowth":
         """Of a ``TierPool``'s programs, in place; those on the GPU grow.  Make room in the
         table first (``TierPool.reserve``), and run it when a step's swaps have ended."""
-        growth = cls(tier_pool.geom, tier_pool.tbl_off, tier_pool.tbl, tier_pool.free_map, held, new_tokens, program,
-                     tier=tier_pool.tier, num_tokens=num_tokens, max_new=max_new, max_kv=max_kv)
-        growth._tier_pool = tier_pool
-        return growth
+        return cls(tier_pool.geom, tier_pool.tbl_off, tier_pool.tbl, tier_pool.free_map, held, new_tokens, program,
+                   tier=tier_pool.tier, num_tokens=num_tokens, max_new=max_new, max_kv=max_kv)
 
     def run(self, stream=None) -> TokenBatch:
         """Calls that may overlap, on other streams, need a growth each (and tables)."""
         batch = self.batch
-        if self._tier_pool is not None and self._tier_pool.tbl is not self._tbl:
+        if any(getattr(x, "moved", False) for x in self._tables):
             raise MoriError("TokenGrowth: the pool's table has moved (reserve) since this was made", M.MORI_EINVAL)
         if _current_device() != batch.index:  # launches go to the current device
             with torch.cuda.device(batch.index):

@@ -166,10 +166,17 @@ class TierPool:
 
     def reserve(self, entries: int) -> None:
         """Room for `entries` table entries in all, for programs that grow.  The table moves:
-        batches made before keep the old one."""
+        batches made before keep the old one, growths made before are refused, and graphs that
+        hold one are captured anew.  Waits for a plan that is under way and for the current
+        stream, behind which what grows programs has to be; any stream may use the table then."""
         if entries > self.tbl.numel():
+            if getattr(self, "ctx", None) is not None:
+                M.mori_plan_wait(self.ctx)  # it rewrites the table, on whichever stream
             more = torch.full((entries,), -1, dtype=torch.int32, device=self.device)
             more[:self.tbl_len] = self.tbl[:self.tbl_len]
+            if self.device.type == "cuda":
+                torch.cuda.current_stream(self.device).synchronize()
+            self.tbl.moved = True
             self.tbl = more
         self.tbl_len = max(self.tbl_len, entries)
 

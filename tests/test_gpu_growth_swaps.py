@@ -6,7 +6,7 @@ import torch
 
 from paper_2606_00866_amd import attention as A
 from paper_2606_00866_amd import mori as M
-from paper_2606_00866_amd.tiering import TierPool, check
+from paper_2606_00866_amd.tiering import MoriError, TierPool, check
 from workload import Geometry
 
 pytestmark = pytest.mark.gpu
@@ -154,5 +154,45 @@ def test_growth_behind_the_swap_out_while_the_swap_in_waits():
         g.batch.check()
         assert np.diff(tp.tbl_off.cpu().numpy()).tolist() == [7, 2]
         assert torch.equal(bytes_of(tp, 0)[:, :3], want[0]) and torch.equal(bytes_of(tp, 1), want[1])
+    finally:
+        tp.close()
+
+
+def test_a_growth_of_the_pools_tensors_ends_with_the_table_it_was_made_on():
+    tp = tier_pool([1] * 3, 30, 5, 30)
+    held = torch.zeros(3, dtype=torch.int32, device="cuda")
+    try:
+        for direct in (True, False):
+            g = growth(tp, held, [3], [0], direct)
+            g.run().check()
+            before = [x.clone() for x in (tp.tbl_off, tp.tbl, tp.free_map, held)]
+            tp.reserve(tp.tbl_len + 4)
+            with pytest.raises(MoriError) as e:
+                g.run()
+            assert e.value.code == M.MORI_EINVAL
+            after = (tp.tbl_off, tp.tbl[:before[1].numel()], tp.free_map, held)
+            assert all(torch.equal(x, y) for x, y in zip(before, after))
+    finally:
+        tp.close()
+
+
+def test_a_moved_table_is_there_for_every_stream():
+    """A plan on another stream right behind a move that the current stream was busy before."""
+    tp = tier_pool([1] * 8, 60, 0, 30)
+    s_out, s_in = torch.cuda.Stream(), torch.cuda.Stream()
+    idle = torch.arange(8, device="cuda") / 8.0
+    try:
+        tp.pool.random_(0, 256)
+        want = [bytes_of(tp, p) for p in range(8)]
+        torch.cuda.synchronize()
+        torch.cuda._sleep(20_000_000)
+        tp.reserve(50)
+        assert move(tp, idle, 5, s_out, s_in).n_out == 3
+        tp.synchronize()
+        for p in range(8):
+            if p < 5:
+                assert torch.equal(bytes_of(tp, p), want[p])
+            else:
+                assert np.array_equal(tp.host_view(p), want[p].cpu().numpy().reshape(-1))
     finally:
         tp.close()
