@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void sight_tiles_kernel(SightArgs a) {
   AttendArgs whole = a;  // a tile is one run here
   whole.splits = 0;
   const Item it = find_item(whole, lane, [&](uint32_t first, uint32_t n, uint32_t) { return tile - first < n; });
-  if (tile == 0 && it.bad && lane == 0) report(a.b, MORI_DEV_BAD_TOKENS);
+  if (tile == 0 && it.bad) report(a.b, MORI_DEV_BAD_TOKENS);  // a lane knows of its own sequences
   uint4* const to = reinterpret_cast<uint4*>(a.tile + tile);
   if (!it.found) {
     if (lane == 0) to[2] = uint4{0, 0, 0, 0};
