@@ -611,8 +611,8 @@ int mori_kv_attend(const mori_pool* pool, uint32_t layer, const mori_tokens* tok
  * with end[t] = i + 1 unless it is given, so one may also see what is behind it.  Ranges
  * make documents that do not see each other (first: where a token's document starts),
  * prefixes that all of it see (end: the larger of the prefix's and the token's own) and
- * the like.  A token that sees nothing gets 0, lse -inf.  Keys that no token sees are not
- * read: their pages need not be there. */
+ * the like.  A token that sees nothing gets 0, lse -inf.  Pages of which no token of the
+ * sequence sees a key need not be there. */
 typedef struct {
   float cap;            /* 0: none; finite, not negative */
   uint32_t window;      /* positions up to and with the token's own; 0: all */

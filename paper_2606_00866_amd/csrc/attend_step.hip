@@ -215,7 +215,10 @@ __global__ __launch_bounds__(64 * NW) void attend_step_kernel(Args a) {
       k0 = next;
     }
   }
-  if (__any(err != 0)) report(a.b, err);
+  if (__any(err != 0)) {
+    if constexpr (SIGHT) err = w.s.error | seen_errors(a, w, lane);
+    report(a.b, err);
+  }
   if (differ(w) && __syncthreads_or(odd)) {
     rows_one_by_one<DT, D, D>(a, w, wv, NW, lane);
     return;

@@ -312,7 +312,10 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_tile_kernel(Args a) {
       if ((k0 += STEP) >= w.hi) break;
     }
   }
-  if (__any(x.err != 0)) report(a.b, x.err);
+  if (__any(x.err != 0)) {
+    if constexpr (SIGHT) x.err = seen_errors(a, w, lane);
+    report(a.b, x.err);
+  }
   if (differ(w) && __syncthreads_or(x.odd)) {
     rows_one_by_one<DT, D, D>(a, w, wv, NW, lane);
     return;

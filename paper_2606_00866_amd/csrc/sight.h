@@ -216,6 +216,33 @@ __device__ inline Work tile_work(const SightArgs& a, uint32_t block) {
   return w;
 }
 
+// A tile's keys are what its rows see together, so pages of which none sees a key may lie
+// between.  Where reading the run's keys met pages that are not there, those that count: of
+// which a row sees a key.  Rare, so no step pays for it.
+__device__ inline uint32_t seen_errors(const SightArgs& a, const Work& w, uint32_t lane) {
+  const uint32_t lo = max(w.lo, w.key0);
+  if (lo >= w.hi) return 0;
+  uint32_t err = 0;
+  const uint32_t last = divide(w.hi - 1, a.b.by_bt);
+  for (uint32_t b0 = divide(lo, a.b.by_bt); b0 <= last; b0 += 64) {
+    uint32_t mine = 0;
+    if (b0 + lane <= last) checked_page(a.b, a.b.tbl[w.s.tbl + b0 + lane], &mine);
+    for (uint64_t bad = __ballot(mine != 0); bad; bad &= bad - 1) {
+      const int at = __ffsll((unsigned long long)bad) - 1;
+      const uint32_t bit = (uint32_t)__builtin_amdgcn_readlane((int)mine, at);
+      if (err & bit) continue;
+      const uint32_t k0 = (b0 + at) * a.b.bt, first = max(k0, lo), end = w.hi - k0 < a.b.bt ? w.hi : k0 + a.b.bt;
+      bool sees = false;
+      for (uint32_t r = lane; r < w.rows; r += 64) {
+        const Keys k = row_keys(a, w, r);
+        sees |= max(k.lo, first) < min(k.hi, end);
+      }
+      if (__any(sees)) err |= bit;
+    }
+  }
+  return err;
+}
+
 // cap * tanh(scale * s / cap) - ref from a product s, with an error of 2^-22 of the cap
 // and with one of 2^-20 of the score.
 __device__ inline float capped_any(const SightArgs& a, float s, float ref) {

@@ -73,3 +73,75 @@ def alone(inst, b):
     """A batch of one of its sequences."""
     return R.Inst(inst.geom, inst.dtype, inst.kv, inst.dim, inst.n[b:b + 1], inst.length[b:b + 1], inst.prog[b:b + 1],
                   inst.tbl_off, inst.tbl, np.array([0, inst.n[b]]), inst.pool, inst.layer)
+
+
+# ---- pages that no token sees ----------------------------------------------------------
+
+GAPS = {
+    "step": ([2, 1, 2], [900, 40, 700], 2, 8, 64, 16),
+    "step_long": ([2], [6000], 1, 8, 128, 16),
+    "few_32": ([4], [900], 1, 8, 64, 24),
+    "tile": ([40], [700], 1, 4, 128, 16),
+    "tile_split": ([40], [6000], 1, 4, 128, 16),
+    "tile_odd_pages": ([40], [3000], 1, 8, 128, 7),
+    "tile_64": ([40, 3], [5000, 900], 1, 4, 64, 32),
+    "tile_large_pages": ([40], [4000], 1, 4, 128, 256),
+}
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(cap=9.0), dict(slopes=True)], ids=["plain", "cap", "slopes"])
+@pytest.mark.parametrize("form", GAPS)
+def test_pages_between_ranges_need_not_be_there(form, kw):
+    """Tokens of one sequence that see its first keys, and others that see its last: pages
+    between have no id, or one past the pool.  Nothing is reported, and one that some token
+    sees is."""
+    n, length, kv, H, dim, bt = GAPS[form]
+    inst = R.instance(5, n, length, kv=kv, dim=dim, bt=bt)
+    q = queries(inst, H)
+    kw = {m: slopes_of(H) if m == "slopes" else x for m, x in kw.items()}
+    T, first, end = q.shape[0], [], []
+    for m, L in zip(n, length):
+        i = np.arange(m)
+        first.append(np.where(i % 2, L - 20, 3))
+        end.append(np.where(i % 2, L, 19))
+    first, end = (np.concatenate(x).astype(np.int32) for x in (first, end))
+    want, _, bound, _ = S.attend(inst, q, 0.1, first=first, end=end, **kw)
+    b = int(np.argmax(length))
+    p, L = int(inst.prog[b]), length[b]
+    e0 = int(inst.tbl_off[p])
+    lo, hi = -(-19 // bt), (L - 20) // bt  # blocks that nobody sees
+    assert hi - lo >= 1
+    good = inst.tbl.copy()
+    for page in (R.NONE, inst.geom.num_blocks + 5):
+        inst.tbl[e0 + lo:e0 + hi] = page
+        assert (np.abs(run(inst, q, 0.1, first=first, end=end, **kw)[0] - want) <= bound).all()
+        for block, seen in ((lo - 1, True), (hi, True), (lo, False)):
+            inst.tbl = good.copy()
+            inst.tbl[e0 + lo:e0 + hi] = R.NONE
+            inst.tbl[e0 + block] = page
+            if seen:
+                with pytest.raises(MoriError) as e:
+                    run(inst, q, 0.1, first=first, end=end, **kw)
+                assert e.value.detail == (M.MORI_DEV_NOT_RESIDENT if page == R.NONE else M.MORI_DEV_PAGE_RANGE)
+            else:
+                run(inst, q, 0.1, first=first, end=end, **kw)
+        inst.tbl = good.copy()
+
+
+def test_pages_between_ranges_whose_stand_in_is_not_finite():
+    """What an absent page's rows are taken from reaches nobody, NaN or not."""
+    for form in ("step", "tile", "tile_odd_pages"):
+        n, length, kv, H, dim, bt = GAPS[form]
+        inst = R.instance(6, n, length, kv=kv, dim=dim, bt=bt)
+        q = queries(inst, H)
+        i = np.concatenate([np.arange(m) for m in n])
+        L = np.repeat(length, n)
+        first, end = np.where(i % 2, L - 20, 3).astype(np.int32), np.where(i % 2, L, 19).astype(np.int32)
+        b = int(np.argmax(length))
+        e0 = int(inst.tbl_off[inst.prog[b]])
+        want, _, bound, _ = S.attend(inst, q, 0.1, first=first, end=end)
+        inst.tbl[e0 - (-19 // bt):e0 + (length[b] - 20) // bt] = R.NONE
+        if 0 not in inst.tbl:
+            inst.pool[:, :, 0] = float("nan")
+        out, _ = run(inst, q, 0.1, first=first, end=end)
+        assert (np.abs(out - want) <= bound).all()
