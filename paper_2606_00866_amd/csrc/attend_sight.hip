@@ -183,7 +183,7 @@ __global__ __launch_bounds__(NT) void sight_items_kernel(SightArgs a) {
   const uint32_t least = max(a.least, (total + a.slots - 1) / a.slots);
   const uint32_t longest = most_of(max(units[0], units[1]), s_wave);
   float best = 3.0e38f;
-  uint32_t run = a.splits ? least : longest;
+  uint32_t run = a.splits ? least : max(longest, 1u);  // of an empty batch there is none
   for (uint32_t j = 2 * wv; a.splits && j < 2 * wv + 2; ++j) {
     const uint32_t c = (uint32_t)((float)least * __builtin_amdgcn_exp2f(0.125f * (float)j) + 0.999f);
     uint32_t n = 0;

@@ -75,6 +75,26 @@ def alone(inst, b):
                   inst.tbl_off, inst.tbl, np.array([0, inst.n[b]]), inst.pool, inst.layer)
 
 
+# ---- an empty batch -------------------------------------------------------------------
+
+def test_an_empty_batch_lists_no_items():
+    """Offsets and lengths of 0, as a growth that did not fit leaves them, where whole tiles are
+    listed: every item names no tile, outputs stay."""
+    inst = R.instance(4, [5] * 70, [300] * 70, kv=32, dim=64)
+    q = queries(inst, 256).cuda()
+    b = R.batch(inst)
+    tiles, _, split, listed = how(inst, q, b, cap=5.0)
+    assert listed and not split
+    ws = torch.zeros(A.kv_attend_workspace(inst.geom, b, q, sight=True).numel(), dtype=torch.uint8, device="cuda")
+    b.seq_off.zero_()
+    b.kv_len.zero_()
+    out = torch.full_like(q, 7.0)
+    A.kv_attend(inst.pool.cuda(), inst.geom, 1, b, q, scale=0.1, out=out, workspace=ws, cap=5.0)
+    b.check()
+    assert (out == 7).all()
+    assert (ws[48 * tiles:52 * tiles].view(torch.int32) == -1).all()
+
+
 # ---- pages that no token sees ----------------------------------------------------------
 
 GAPS = {
