@@ -165,3 +165,82 @@ def test_pages_between_ranges_whose_stand_in_is_not_finite():
             inst.pool[:, :, 0] = float("nan")
         out, _ = run(inst, q, 0.1, first=first, end=end)
         assert (np.abs(out - want) <= bound).all()
+
+
+# ---- split and whole --------------------------------------------------------------------
+
+def test_split_and_whole_tiles_of_the_same_programs():
+    """Few workgroups, whose tiles are split, and four times as many, whose are not."""
+    kw = dict(cap=20.0)
+    inst = R.instance(91, [900, 20, 700], [900, 400, 1500], kv=16, dim=64, bt=16)
+    q = queries(inst, 48)
+    assert how(inst, q, **kw)[1:3] == (40 * 16, True)
+    a = run(inst, q, 0.1, **kw)
+    big = R.instance(91, [900, 20, 700] * 4, [900, 400, 1500] * 4, kv=16, dim=64, bt=16)
+    for b in range(12):  # the same programs four times
+        for p in (0, 1):
+            j = np.arange(int(big.length[b]))
+            pages = big.tbl[big.tbl_off[big.prog[b]] + j // 16]
+            big.pool[1, p, torch.from_numpy(pages), torch.from_numpy(j % 16)] = torch.from_numpy(inst.rows(p, b % 3, j.size)).bfloat16()
+    tiles, groups, split, listed = how(big, q.repeat(4, 1, 1), **kw)
+    assert groups >= 2048 and not split and listed
+    out, lse = run(big, q.repeat(4, 1, 1), 0.1, **kw)
+    T = q.shape[0]
+    rows = np.array([0, 1, 400, 899, 900, 919, 920, 1300, 1619])
+    heads = [0, 23, 47]
+    for t in rows:
+        b = int(np.searchsorted(inst.seq_off, t, side="right")) - 1
+        pos = int(inst.length[b] - inst.n[b] + t - inst.seq_off[b])
+        for h in heads:
+            k, v = (inst.rows(p, b, pos + 1)[:, h // 3] for p in (0, 1))
+            s = 20.0 * np.tanh(k @ q[t, h].double().numpy() * 0.1 / 20.0)
+            w = np.exp(s - s.max())
+            top = s.max() + np.log(w.sum())
+            w /= w.sum()
+            # weights and results rounded to 16 bits, scores of about 8 to 2^-14
+            bound = 2.0 ** -8 * 1.1 * (w @ np.abs(v) + np.abs(w @ v)) + 2.0 ** -10
+            for o, l, at in ((a[0], a[1], t), *((out, lse, i * T + t) for i in range(4))):
+                assert (np.abs(o[at, h] - w @ v) <= bound).all()
+                assert abs(l[at, h] - top) <= 2.0 ** -10
+    for i in range(1, 4):  # the same runs in other places: the same bits
+        assert np.array_equal(out[i * T:(i + 1) * T], out[:T]) and np.array_equal(lse[i * T:(i + 1) * T], lse[:T])
+
+
+@pytest.mark.parametrize("sight", ["cap", "slopes", "window", "documents"])
+@pytest.mark.parametrize("seqs,kv,dim", [(18, 128, 64), (66, 32, 128), (40, 64, 128)])
+def test_whole_tiles_in_the_order_of_their_length(seqs, kv, dim, sight):
+    g = np.random.default_rng(seqs)
+    n = g.integers(0, 18, seqs).tolist()
+    n[seqs // 2] = 17  # 34 rows or more
+    length = [a + int(b) for a, b in zip(n, g.integers(0, 230, seqs))]
+    length[0] = n[0]
+    inst = R.instance(seqs + len(sight), n, length, kv=kv, dim=dim, dtype=F16 if len(sight) % 2 else BF16, bt=16)
+    H = kv * (4 if kv < 64 else 2)
+    kw = {"cap": dict(cap=20.0), "slopes": dict(slopes=slopes_of(H)), "window": dict(window=37),
+          "documents": dict(first=documents(inst, 30))}[sight]
+    q = queries(inst, H, 8.0 if sight == "cap" else 2.5)
+    _, groups, split, listed = how(inst, q, **kw)
+    assert groups >= 2048 and not split and listed
+    compare(inst, q, dim ** -0.5, **kw)
+
+
+# workgroups of a batch, and the keys up to which windows' tiles stay whole there
+BANDS = {"128": (8, 1024), "256": (16, 2560), "about_full": (24, 5120), "above": (40, 2560)}
+
+
+@pytest.mark.parametrize("more", [False, True])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("band", BANDS)
+def test_windows_on_both_sides_of_the_choice_to_split(band, dim, more):
+    kv, keys = BANDS[band]
+    window = keys - 17 - (8 if dim == 64 else 4) + more  # with a tile's 17 tokens and a load's rows
+    n = [17] * 16
+    length = [17 + 5 * i for i in range(15)] + [window + 300]
+    inst = R.instance(kv + window, n, length, kv=kv, dim=dim, dtype=BF16, bt=16, layers=1, layer=0)
+    H = 2 * kv
+    q = queries(inst, H)
+    tiles, groups, split, _ = how(inst, q, window=window, slopes=slopes_of(H))
+    assert {"128": 128 <= groups < 256, "256": 256 <= groups < 400, "about_full": 400 <= groups <= 640,
+            "above": 640 < groups < 2048}[band]
+    assert split == more
+    compare(inst, q, dim ** -0.5, window=window, slopes=slopes_of(H))
