@@ -27,6 +27,7 @@ DTYPES = {torch.float16: M.MORI_DT_F16, torch.bfloat16: M.MORI_DT_BF16}
 STYLES = {"half": M.MORI_ROPE_HALF, "pairs": M.MORI_ROPE_PAIRS}
 _current_device = torch._C._cuda_getDevice
 ORDERS = {"blocks": M.MORI_AXES_BLOCKS, "turns": M.MORI_AXES_TURNS}
+MAX_PAIRS = 2048  # of a head of 4096 elements, the widest
 LATENT_ROPE = 64  # rotated elements behind the latent part of a latent row
 
 
@@ -42,7 +43,8 @@ def rope_table(positions: int, rot_dim: int, theta: float = 10000.0, device="cud
     frequencies start anew each, as if n pairs were all (theta^(-2i / 2n)): for axes with
     frequencies of their own."""
     parts = [(rot_dim + 1) // 2] if restart is None else list(restart)
-    _need(restart is None or 2 * sum(parts) == rot_dim, "rope_table: restart gives the pairs of every part")
+    _need(restart is None or (parts and min(parts) >= 0 and 2 * sum(parts) == rot_dim),
+          "rope_table: restart gives the pairs of every part")
     share = torch.cat([torch.arange(0, 2 * n, 2, dtype=torch.float64, device=device) /
                        (rot_dim if restart is None else 2 * n) for n in parts])
     angle = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * theta ** -share
@@ -401,7 +403,8 @@ def _axes(positions, sections, order, batch: TokenBatch, rot: int) -> M.mori_axe
 
 def pair_axes(sections, order: str = "blocks") -> list:
     """The axis that every pair turns by."""
-    if order not in ORDERS or not 0 < len(sections) <= M.MORI_MAX_AXES or any(int(n) != n or n < 0 for n in sections):
+    if order not in ORDERS or not 0 < len(sections) <= M.MORI_MAX_AXES or \
+            any(not 0 <= n <= MAX_PAIRS or int(n) != n for n in sections):
         raise MoriError("kv_append: up to four sections, order 'blocks' or 'turns'", M.MORI_EINVAL)
     if order == "blocks":
         return [a for a, n in enumerate(sections) for _ in range(int(n))]
