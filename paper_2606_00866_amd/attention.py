@@ -113,7 +113,8 @@ class TokenBatch:
             _need(x.dtype == torch.int32 and x.is_contiguous() and x.dim() == 1 and x.device.type == "cuda" and
                   x.device == kv_len.device, f"TokenBatch: {name} is a contiguous int32 vector on the batch's device")
             _need(n is None or x.numel() == n, f"TokenBatch: {name} has {x.numel()} entries, not {n}")
-        _need(num_tokens >= 0 and max_new >= 0 and 0 < max_kv < 1 << 31, "TokenBatch: bounds out of range")
+        _need(0 <= num_tokens < 1 << 31 and 0 <= max_new < 1 << 32 and 0 < max_kv < 1 << 31,
+              "TokenBatch: bounds out of range")
         _need(tbl_off.numel() >= 2, "TokenBatch: tbl_off is empty")
         self.device = kv_len.device
         self.index = kv_len.device.index
@@ -226,7 +227,8 @@ class TokenGrowth:
             _need(n is None or x.numel() == n, f"TokenGrowth: {name} has {x.numel()} entries, not {n}")
         _need(0 < P <= M.MORI_MAX_PROGRAMS and 0 < B <= M.MORI_MAX_PROGRAMS and (program is not None or B <= P),
               "TokenGrowth: programs or sequences out of range")
-        _need(0 <= num_tokens < 1 << 31, "TokenGrowth: bounds out of range")
+        _need(0 <= num_tokens < 1 << 31 and 0 <= max_new < 1 << 32 and 0 < max_kv < 1 << 31,
+              "TokenGrowth: bounds out of range")
         _need(dev.type == "cuda", "TokenGrowth: its tensors are on a GPU")
         _need(_apart(to, (tbl_off, tbl, free_map, held), [x for x in (new_tokens, program, tier) if x is not None]),
               "TokenGrowth: into is the tensors themselves or some that overlap no others")
