@@ -214,7 +214,7 @@ class TierPool:
         prog = M.mori_programs(self.P, k, window.data_ptr() if window is not None else None,
                                idleness.data_ptr() if idleness is not None else None,
                                status.data_ptr() if status is not None else None, self.tbl_off.data_ptr(),
-                               self.tbl_len, self.tbl.data_ptr(), self.tier.data_ptr(), self.free_map.data_ptr())
+                               self.tbl.numel(), self.tbl.data_ptr(), self.tier.data_ptr(), self.free_map.data_ptr())
         self._keep = [window, idleness, status]
         budget = M.mori_budget(int(gpu_bytes), int(cpu_bytes), int(flags), int(ssd_bytes))
         return M.mori_rank_partition(self.ctx, prog, budget, _stream(stream))
@@ -290,7 +290,8 @@ class TierPool:
 
     # ---- state readback ---------------------------------------------------------
     def state(self):
-        tbl = self.tbl.cpu().numpy().view(np.uint32)[: self.tbl_len].copy()
+        n = max(self.tbl_len, int(self.tbl_off[-1]))  # a pool without blocks has an entry to grow into all the same
+        tbl = self.tbl.cpu().numpy().view(np.uint32)[:n].copy()
         return tbl, self.tier.cpu().numpy().copy(), self.free_map.cpu().numpy().copy()
 
     def close(self) -> None:

@@ -196,3 +196,25 @@ def test_a_moved_table_is_there_for_every_stream():
                 assert np.array_equal(tp.host_view(p), want[p].cpu().numpy().reshape(-1))
     finally:
         tp.close()
+
+
+def test_a_pool_without_blocks_grows_into_its_only_entry():
+    """A table of no entries is given one: a growth may take it, and plans know of it."""
+    tp = tier_pool([0, 0], 8, 0, 8)
+    held = torch.zeros(2, dtype=torch.int32, device="cuda")
+    s_out, s_in = torch.cuda.Stream(), torch.cuda.Stream()
+    idle = torch.tensor([0.1, 0.9], device="cuda")
+    try:
+        growth(tp, held, [5], [1], False).run().check()
+        tp.pool.random_(0, 256)
+        want = bytes_of(tp, 1)
+        torch.cuda.synchronize()
+        assert tp.state()[0].size == 1 and want.shape[1] == 1
+        assert move(tp, idle, 0, s_out, s_in).n_out == 1
+        tp.synchronize()
+        assert np.array_equal(tp.host_view(1), want.cpu().numpy().reshape(-1))
+        move(tp, idle, 4, s_out, s_in)
+        tp.synchronize()
+        assert torch.equal(bytes_of(tp, 1), want)
+    finally:
+        tp.close()
