@@ -114,21 +114,22 @@ bool plan_of(const mori_pool* pool, uint32_t layer, const mori_tokens* tokens, c
   // about 500 21.7 and 32.1, of 1000 39.1 and 45.2, of 2000 (up to 5000) 82.0 and 74.6; 64 of
   // 500 31.2 and 37.9, of 1000 (up to 3000) 67.3 and 60.1.
   if (sight && p.step && most <= (tiles * a.kv_heads < 256 ? 768 : 2048)) a.splits = 0;
-  // Nor are tiles of few keys: the choice of the runs and the join take 7 us.  Tiles of 128
-  // rows, 128 wide, whole and split: 20 workgroups of 500 keys 24.8 and 27.5 us, of 1000 35.6
-  // and 30.5; 64 of 700 29.4 and 32.6, of 1000 36.3 and 35.4; 128 of 1000 36.9 and 43.8, of
-  // 2000 57.3 and 53.3; 176 of 1000 36.6 and 40.4, of 1400 45.4 and 43.5; 256 of 2000 58.9 and
-  // 65.3, of 3000 80.3 and 87.5, of 4000 101 and 94.  That is for tiles alike, by a window;
-  // else one may have most of the keys: 30 sequences behind 500 keys (up to 1100) 56.1 and
-  // 64.1, but 8 of these 48.3 and 41.0; 16 with a window of 2400 and documents 78.1 and 63.2.
-  // A chip of 512 at a time that is about full is left so for longer: 440 of 4000 keys 131
-  // and 137, 512 134 and 140, 648 145 and 152; of 5500 and capped 440 224 and 217, 512 225 and
-  // 221, 648 209 and 214; but 388 of 4000 120 and 113, 752 capped 275 and 268.
+  // Nor are tiles of few keys: the choice of the runs and the join take 7 to 9 us.  Tiles of
+  // 128 rows, 128 wide, whole and split: 20 workgroups of 500 keys 24.8 and 27.5 us, of 1000
+  // 35.6 and 30.5; 64 of 700 29.4 and 32.6, of 1000 36.3 and 35.4; 30 sequences behind 500 keys
+  // (up to 1100) 56.1 and 64.1, but 8 of these 48.3 and 41.0; 16 with a window of 2400 and
+  // documents 78.1 and 63.2.
+  // A window makes tiles alike, so more of them stay whole.  128 wide, and 64 wide in brackets:
+  // 160 workgroups of 1100 keys 37 and 43 us (27 and 33), of 2000 55 and 51 (40 and 41); 272 of
+  // 2500 69 and 75 (51 and 57), of 5000 119 and 116 (89 and 82).  From 400 on the chip, 512 at
+  // a time, is about full: of 5000 keys 472 173 and 182 (112 and 120), 656 257 and 265 (136 and
+  // 144), 1136 437 and 447 (248 and 257); of 6000 416, capped, 245 and 237 (200 and 185), 824 358
+  // and 348; of 12000 552 620 and 540 (322 and 320), 1136 947 and 868 (513 and 499).
   if (sight && !p.step) {
     const uint64_t groups = tiles * a.kv_heads;
     const bool alike = windowed && !a.first;
     uint64_t whole = groups < 256 ? 768 : 1280;
-    if (alike && groups >= 128) whole = groups < 256 ? 1024 : groups < 400 || groups > 640 ? 2560 : 5120;
+    if (alike && groups >= 128) whole = groups < 256 ? 1024 : groups < 400 ? 2560 : 5120;
     if (most <= whole) a.splits = 0;
   }
   // runs have `least` units or more, so short contexts give fewer items than slots

@@ -225,7 +225,7 @@ def test_whole_tiles_in_the_order_of_their_length(seqs, kv, dim, sight):
 
 
 # workgroups of a batch, and the keys up to which windows' tiles stay whole there
-BANDS = {"128": (8, 1024), "256": (16, 2560), "about_full": (24, 5120), "above": (40, 2560)}
+BANDS = {"128": (8, 1024), "256": (16, 2560), "about_full": (24, 5120), "above": (40, 5120)}
 
 
 @pytest.mark.parametrize("more", [False, True])
