@@ -20,21 +20,22 @@
 //
 // Three prompts of 19215 tokens in all (32 heads over 8 key heads of 128; 1.05
 // TFLOP): 1070 to 1119 us, 937 to 979 TFLOP/s of the 1330 that a large product reaches;
-// the matrix units are busy 44 to 49% of the cycles.  What bounds it is the clock that the
-// chip's power leaves: the same kernel over keys and values of zeros takes 781 us where
-// it takes 1304 on normal ones (prompts of 20600 tokens), without the weights' arithmetic
-// 1107, with loads for its first steps only 1200.  So what does less work is faster and
-// what only hides latency is not: reading operands of the scores six products ahead
-// changed nothing, values four ahead, table entries looked up before the weights and
-// not before the wait, and products at a higher priority 1% on chunks and 5% on mixed
-// batches.  Chunks of four sequences (0.2 TFLOP): 281 us, 702 TFLOP/s, with uneven last
-// items and the join; decode steps and chunks mixed (32 sequences, 0.51 GB, 0.12 TFLOP):
-// 258 us.
+// the matrix units are busy 44 to 49% of the cycles.  A part of it is the clock that the
+// chip's power leaves: prompts of 20600 tokens take 1288 us on one card and 1470 on another,
+// over a pool and queries of zeros 1064 and 1070; without the weights' arithmetic 1303 and
+// 993 on the second.  So what does less work is faster and what only hides latency is not:
+// reading operands of the scores six products ahead changed nothing, values four ahead,
+// table entries looked up before the weights and not before the wait, and products at a
+// higher priority 1% on chunks and 5% on mixed batches.  Chunks of four sequences (0.2
+// TFLOP): 281 us, 702 TFLOP/s, with uneven last items and the join; decode steps and chunks
+// mixed (32 sequences, 0.51 GB, 0.12 TFLOP): 258 us.
 //
 // With a sight (sight.h) a workgroup's keys are those its rows see; scores that are
 // capped or biased cost what they add to the weights: prompts of 20600 tokens (1.25
 // TFLOP) 1303 us with a window past all of them, 1440 with a bias, 1547 with a cap, 1748
-// with both.
+// with both.  Prompts with documents take 571 to 636 us by the card, 500 over zeros, 463
+// without the weights' arithmetic either; with a prefix and a bias 440 to 508, 401 and 308;
+// capped chunks in a window 180 to 205, 165 and 119.
 #include "sight.h"
 
 namespace mori {

@@ -12,9 +12,11 @@
 //
 // Items.  As in attend.h, but a tile's keys are those its rows see, so a window over a
 // long context gives as many items as the window has work for.  Batches whose sequences
-// are one tile each (decode steps) find that from the lengths and ranges themselves;
-// the others have their tiles and items written down by a small kernel first
-// (attend_sight.hip), since every workgroup would read all tokens' ranges otherwise.
+// are one tile each (decode steps) find that from the lengths and ranges themselves: every
+// workgroup reads those of all tokens, which are few.  A step of 64 sequences takes 60 us
+// with documents and 59 without, of 400 281 and 271, of 400 of four tokens 368 and 297, of
+// 1000 921 and 787 (8 key heads of 128, 700 to 1000 keys each).  The others have their tiles
+// and items written down by a small kernel first (attend_sight.hip).
 //
 // tanh.  cap * tanh(x) = cap - 2 cap / (e^2x + 1): an exponential, a reciprocal and three
 // more instructions, with an error of 2^-22 of the cap.  For caps up to 64 that is 2^-16

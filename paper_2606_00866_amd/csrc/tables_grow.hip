@@ -9,9 +9,9 @@
 //   slot_t  = page of t's block * block_tokens + its row,  position_t = held_p + i
 //
 // One or two launches, bound by their latency and dependent reads: a byte of the free map
-// per page, an entry of the tables in and out, 12 bytes a token.  A step of 8 programs
-// (600 pages) takes 6.1 us, of 400 of 1024 (300 000 pages) 10.9, of 3000 of 4096 16.6;
-// chunks of 24 of 64 programs (60 000 tokens, 4000 pages) 9.
+// per page, an entry of the tables in and out, 12 bytes a token.  A step of 8 programs (a
+// pool of 401 pages) takes 6.1 us, of 400 of 1024 (309 450 pages) 11.2, of 3000 of 4096
+// 16.6; chunks of 24 of 64 programs (72 620 tokens, about 4540 of 87 830 pages) 9.
 //   grow_small   everything, in one workgroup, for small pools and batches
 //   grow_count   one workgroup checks and scans the sequences and programs; the others
 //                count free pages, 512 at a time, and, where the tables grow in place,
@@ -30,7 +30,7 @@ namespace {
 
 constexpr uint32_t NT = 256;
 // Pages of a count: the smallest tile.  A tile's workgroup also writes the slots of all
-// tokens in its pages: with 4096 pages a tile chunks of 60 000 tokens took 28 us there,
+// tokens in its pages: with 4096 pages a tile chunks of 72 620 tokens took 28 us there,
 // with 512 5.5.
 constexpr uint32_t COUNTED = 512;
 constexpr uint32_t ENTRIES = 1024;  // table entries of a workgroup
@@ -481,8 +481,8 @@ __global__ __launch_bounds__(NT) void grow_assign_kernel(GrowArgs a, uint32_t mo
 // tokens and a program a thread at most): one launch, no workspace.  What the scan finds
 // and the grown table lie in LDS, and tokens find their pages there whether their blocks
 // are new or old.  Everything is read before the first barrier, so in place is as good.
-// A pool of 600 pages, 8 programs that take a token each: 6.1 us a call (64 threads; 6.5
-// with 256), 8.7 with the two launches, which in a graph take 5.6.
+// A pool of 401 pages and 377 entries, 8 programs that take a token each: 6.1 us a call (64
+// threads; 6.5 with 256), 8.7 with the two launches, which in a graph take 5.6.
 template <int W>
 __global__ __launch_bounds__(W) void grow_small_kernel(GrowArgs a) {
   constexpr uint32_t E = 8;
