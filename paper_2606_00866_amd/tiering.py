@@ -224,7 +224,7 @@ class TierPool:
         they grew by on the device before it."""
         rc, p = M.mori_plan_wait(self.ctx)
         self.plan = p
-        if rc == M.MORI_OK and self.P:
+        if rc == M.MORI_OK and p.num_programs == self.P > 0:
             by_rank = np.diff(np.ctypeslib.as_array(p.prefix, shape=(self.P,)), prepend=np.uint64(0))
             self.nblk[np.ctypeslib.as_array(p.order, shape=(self.P,))] = by_rank // np.uint64(self.geom.block_bytes)
         return rc, p

@@ -100,3 +100,10 @@ def test_batches_of_grown_programs(monkeypatch):
     with pytest.raises(MoriError):
         A.TokenBatch.of(full, [0], [1], [17])
     assert 2 not in reads  # no room to have grown
+
+
+def test_a_plan_of_other_programs_says_nothing_of_sizes(monkeypatch):
+    """One enqueued through the library with fewer of them: what it left behind those is not read."""
+    tp = tier_pool([1, 2, 3])
+    monkeypatch.setattr(M, "mori_plan_wait", plan_of([1, 0], [7, 7], [0, 0]))
+    assert tp.plan_wait()[0] == M.MORI_OK and tp.nblk.tolist() == [1, 2, 3]
